@@ -319,6 +319,82 @@ int lagkv_gather_paged(lagkv_plan_t plan, const void *K_pool, const void *V_pool
                        void *cuda_stream);
 
 /*
+ * ---- Attention over the cache ---------------------------------------------------------------
+ * The compress pass shortens a cache so that the attention reading it gets cheaper; the entry
+ * points from here on are that attention, the choice of blocks it may be limited to, and the pages
+ * the pass frees.  They take the same plan (its B, H_kv, D, strides, dtype and device; sink, lag and
+ * keep_ratio play no part) and the same caches, one layer per call.
+ *
+ * Queries: T tokens per sequence, H_q heads; query head h reads KV head h / (H_q / H_kv).  Q and the
+ * output are bf16 for bf16 and fp8 caches, fp16 for fp16 caches.  Products of queries and keys,
+ * softmax statistics and sums are fp32; probabilities are rounded to the 16-bit type of the matrix
+ * products (fp16 for fp8 caches, whose rows widen to fp16 exactly).
+ */
+typedef struct {
+    int32_t T;         /* query tokens per sequence, 1..64                                      */
+    int32_t H_q;       /* query heads: H_kv times 1..64                                         */
+    double scale;      /* factor of q.k before the softmax, > 0; 0 = 1/sqrt(D)                  */
+    double k_scale;    /* what a stored K element of 1 stands for (fp8 caches), > 0; 0 = 1      */
+    double v_scale;    /* the same for V                                                        */
+    int64_t stride_b;  /* strides of Q in elements, multiples of 8; all 0 = contiguous          */
+    int64_t stride_t;  /* [B, T, H_q, D]; channel stride 1, 16-byte aligned base                */
+    int64_t stride_h;
+} lagkv_query;
+
+/*
+ * Bytes of workspace for lagkv_attend_tree() (blocks = keep = 0) or the attention over chosen blocks
+ * (blocks = blocks per sequence of its bounds, keep as in its choice) with up to T tokens and H_q
+ * heads; 0 = bad arguments.  A workspace may serve every smaller call, tree and blocks alike.  256-byte aligned,
+ * cleared once with lagkv_attend_workspace_init() (async on the stream; the kernels leave what they
+ * need cleared); starts with a status block that lagkv_read_status() reads.
+ */
+size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, int64_t blocks, int32_t keep);
+int lagkv_attend_workspace_init(lagkv_plan_t plan, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Attention of a tree of drafted tokens (T = 1: an ordinary decode step).  seq_len[B] (DEVICE int32)
+ * counts the valid rows of each sequence, the drafted tokens' own rows included: those are its last
+ * draft_len[b] rows (DEVICE int32 [B], 0..T; NULL = T everywhere).  Token t of sequence b sees row r when
+ *     r < seq_len[b] - draft_len[b]          (everything before the draft), or
+ *     r = seq_len[b] - draft_len[b] + j and bit j of tree_mask[b*T + t] is set.
+ * tree_mask (DEVICE uint64 [B, T]): NULL = a chain, token t sees drafted rows 0..t.  Rows at or behind
+ * seq_len[b], and drafted rows a token does not see, never reach it, whatever they hold.
+ *   out      [B, T, H_q, D] contiguous; lse_out fp32 [B, T, H_q] or NULL: natural log of the sum of
+ *            exp(scale*k_scale*q.k) over the rows seen.  A token that sees no row, and the padding
+ *            tokens t >= draft_len[b], get out = 0 and lse = -infinity.
+ * seq_len[b] outside [0, S_cap], draft_len[b] outside [0, T] or above seq_len[b]: that sequence counts as
+ * without tokens and LAGKV_EINVAL is recorded in the status block.
+ * One launch with the same arguments for every length; results do not depend on the schedule.
+ */
+int lagkv_attend_tree(lagkv_plan_t plan, const lagkv_query *query, const void *Q, const void *K, const void *V,
+                      int64_t S_cap, const int32_t *seq_len, const int32_t *draft_len, const uint64_t *tree_mask,
+                      void *out, float *lse_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The same on a paged cache.  num_pages = pages of the pools: a table entry outside [0, num_pages) that
+ * a sequence's length reaches is not read; its rows count as not there and LAGKV_EINVAL is recorded.
+ */
+int lagkv_attend_tree_paged(lagkv_plan_t plan, const lagkv_query *query, const void *Q, const void *K_pool,
+                            const void *V_pool, const lagkv_paged_layout *layout, int64_t num_pages,
+                            const int32_t *seq_len, const int32_t *draft_len, const uint64_t *tree_mask, void *out,
+                            float *lse_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Keep the accepted path of each tree: with base = seq_len[b] - draft_len[b] the rows
+ * base + accepted[b*T + j], j < n_accepted[b], move to base + j in K and V (every KV head), and
+ * seq_len[b] becomes base + n_accepted[b].  accepted (DEVICE int32 [B, T]) ascends strictly inside
+ * [0, draft_len[b]).  A sequence whose lengths or path are not of that form is left untouched and
+ * LAGKV_EINVAL is recorded.  draft_len as above, T 1..64.  The workspace needs its status block only.
+ */
+int lagkv_tree_commit(lagkv_plan_t plan, void *K_cache, void *V_cache, int64_t S_cap, int32_t *seq_len,
+                      const int32_t *draft_len, int32_t T, const int32_t *accepted, const int32_t *n_accepted,
+                      void *workspace, size_t workspace_bytes, void *cuda_stream);
+int lagkv_tree_commit_paged(lagkv_plan_t plan, void *K_pool, void *V_pool, const lagkv_paged_layout *layout,
+                            int64_t num_pages, int32_t *seq_len, const int32_t *draft_len, int32_t T,
+                            const int32_t *accepted, const int32_t *n_accepted, void *workspace,
+                            size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Synchronise cuda_stream, copy the status block to the host and clear it.  workspace == NULL
  * names the status block of the library's built-in scratch on the plan's device (the one
  * lagkv_compress_append_noalloc() uses).

@@ -31,6 +31,8 @@ EXPORTS = (
     "lagkv_compress_prefill", "lagkv_compress_prefill_host", "lagkv_host_staging_bytes",
     "lagkv_compress_append", "lagkv_compress_append_noalloc", "lagkv_compress_prefill_paged",
     "lagkv_compress_append_paged", "lagkv_gather", "lagkv_gather_paged",
+    "lagkv_attend_workspace_bytes", "lagkv_attend_workspace_init", "lagkv_attend_tree", "lagkv_attend_tree_paged",
+    "lagkv_tree_commit", "lagkv_tree_commit_paged",
     "lagkv_read_status",
     "lagkv_launch_info", "lagkv_plan_tune", "lagkv_selftest_bounded_wait", "lagkv_status_string", "lagkv_version",
 )
@@ -57,6 +59,14 @@ class lagkv_paged_layout(ctypes.Structure):
     _fields_ = [
         ("block_table", ctypes.c_void_p), ("max_blocks", ctypes.c_int32), ("page_size", ctypes.c_int32),
         ("stride_page", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_s", ctypes.c_int64),
+    ]
+
+
+class lagkv_query(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("H_q", ctypes.c_int32),
+        ("scale", ctypes.c_double), ("k_scale", ctypes.c_double), ("v_scale", ctypes.c_double),
+        ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64),
     ]
 
 
@@ -110,6 +120,19 @@ def load_library() -> ctypes.CDLL:
     lib.lagkv_gather_paged.argtypes = [vp, vp, vp, ctypes.POINTER(lagkv_paged_layout), i64, vp, i64, vp, vp, vp, vp]
     lib.lagkv_gather.restype = ctypes.c_int
     lib.lagkv_gather.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    query, layout = ctypes.POINTER(lagkv_query), ctypes.POINTER(lagkv_paged_layout)
+    lib.lagkv_attend_workspace_bytes.restype = sz
+    lib.lagkv_attend_workspace_bytes.argtypes = [vp, i32, i32, i64, i32]
+    lib.lagkv_attend_workspace_init.restype = ctypes.c_int
+    lib.lagkv_attend_workspace_init.argtypes = [vp, vp, sz, vp]
+    lib.lagkv_attend_tree.restype = ctypes.c_int
+    lib.lagkv_attend_tree.argtypes = [vp, query, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_attend_tree_paged.restype = ctypes.c_int
+    lib.lagkv_attend_tree_paged.argtypes = [vp, query, vp, vp, vp, layout, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_tree_commit.restype = ctypes.c_int
+    lib.lagkv_tree_commit.argtypes = [vp, vp, vp, i64, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.lagkv_tree_commit_paged.restype = ctypes.c_int
+    lib.lagkv_tree_commit_paged.argtypes = [vp, vp, vp, layout, i64, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.lagkv_read_status.restype = ctypes.c_int
     lib.lagkv_read_status.argtypes = [vp, vp, vp, ctypes.POINTER(i32 * 4)]
     lib.lagkv_launch_info.restype = ctypes.c_int
@@ -372,6 +395,145 @@ class Plan:
                                    _ptr(workspace), _stream(dev))
         _check(rc, "lagkv_gather")
         return K_out, V_out
+
+    # ---- attention over the cache
+    def new_attend_workspace(self, T: int, H_q: int, blocks: int = 0, keep: int = 0) -> torch.Tensor:
+        """Workspace for ``attend_tree`` (and, with ``blocks`` and ``keep``, ``attend_blocks``) calls of up
+        to ``T`` tokens and ``H_q`` query heads."""
+        nbytes = int(self.lib.lagkv_attend_workspace_bytes(self.handle, int(T), int(H_q), int(blocks), int(keep)))
+        if nbytes == 0:
+            raise LagKVError(LAGKV_EINVAL, "lagkv_attend_workspace_bytes")
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self._dev())
+        _check(self.lib.lagkv_attend_workspace_init(self.handle, _ptr(ws), ws.numel(), _stream(self._dev())),
+               "lagkv_attend_workspace_init")
+        return ws
+
+    def _check_ints(self, t, name: str, shape, dtype=torch.int32):
+        if t is None:
+            return
+        if t.dtype != dtype or not t.is_cuda or t.device.index != self.device or tuple(t.shape) != tuple(shape) or \
+                not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor {tuple(shape)} on device {self.device}")
+
+    def _check_contiguous_cache(self, t, name: str):
+        """A cache ``[B, H, S_cap, D]`` whose strides are the plan's (0 = contiguous)."""
+        self._check_cache(t, name)
+        c = self.cfg
+        if t.dim() != 4 or t.shape[0] != c.B or t.shape[1] != c.H_kv or t.shape[3] != c.D:
+            raise TypeError(f"{name} must be [{c.B}, {c.H_kv}, S_cap, {c.D}]")
+        ss = c.stride_s or c.D
+        sh = c.stride_h or t.shape[2] * ss
+        want = (c.stride_b or c.H_kv * sh, sh, ss, 1)
+        if any(n > 1 and have != w for n, have, w in zip(t.shape, t.stride(), want)):
+            raise TypeError(f"{name} has strides {t.stride()}, the plan says {want}")
+
+    def _query(self, Q, scale, k_scale, v_scale) -> lagkv_query:
+        c = self.cfg
+        want = torch.float16 if self.dtype == torch.float16 else torch.bfloat16
+        if Q.dtype != want or not Q.is_cuda or Q.device.index != self.device or Q.dim() != 4 or Q.shape[0] != c.B or \
+                Q.shape[3] != c.D or Q.stride(3) != 1:
+            raise TypeError(f"Q must be a {want} CUDA tensor [{c.B}, T, H_q, {c.D}] with channel stride 1")
+        T, H_q = int(Q.shape[1]), int(Q.shape[2])
+        strides = (0, 0, 0) if Q.is_contiguous() else tuple(int(Q.stride(i)) for i in range(3))
+        return lagkv_query(T, H_q, 0.0 if scale is None else float(scale), float(k_scale), float(v_scale), *strides)
+
+    def _attend_out(self, Q, out, want_lse):
+        if out is None:
+            out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        elif out.dtype != Q.dtype or out.shape != Q.shape or not out.is_contiguous() or out.device != Q.device:
+            raise TypeError("out must be a contiguous tensor like Q")
+        lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if want_lse else None
+        return out, lse
+
+    def _paged_pool(self, K_pool, V_pool, block_table, strides, num_pages):
+        """Layout and page count of a pool, checked against the tensors."""
+        self._check_cache(K_pool, "K_pool")
+        if V_pool is not None:
+            self._check_cache(V_pool, "V_pool")
+            if V_pool.shape != K_pool.shape or V_pool.stride() != K_pool.stride():
+                raise TypeError("K_pool and V_pool must have the same shape and strides")
+        if block_table.device.index != self.device:
+            raise TypeError(f"block_table must be on device {self.device}")
+        if strides is None:
+            c = self.cfg
+            if K_pool.dim() != 4 or K_pool.shape[1] != c.H_kv or K_pool.shape[3] != c.D or not K_pool.is_contiguous():
+                raise TypeError(f"the pools must be contiguous [num_pages, {c.H_kv}, page_size, {c.D}]; pass strides for others")
+            num_pages = K_pool.shape[0]
+        elif num_pages is None:
+            raise TypeError("num_pages is needed with strides")
+        return self._paged(K_pool, block_table, strides), int(num_pages)
+
+    def attend_tree(self, Q, K, V, seq_len, workspace, draft_len=None, tree_mask=None, scale=None, k_scale=1.0,
+                    v_scale=1.0, want_lse=False, out=None):
+        """``lagkv_attend_tree``: attention of ``Q [B, T, H_q, D]`` (T = 1: a decode step) over a cache whose last
+        ``draft_len[b]`` rows of ``seq_len[b]`` are the tokens' own.  ``tree_mask`` int64 ``[B, T]`` (bit j: the token
+        sees drafted row j; None: a chain).  Returns ``{"out", "lse"}`` (``lse`` when asked for)."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        self._check_contiguous_cache(K, "K")
+        self._check_contiguous_cache(V, "V")
+        B = self.cfg.B
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(draft_len, "draft_len", (B,))
+        self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
+        if V.shape != K.shape:
+            raise TypeError("K and V must have the same shape")
+        out, lse = self._attend_out(Q, out, want_lse)
+        rc = self.lib.lagkv_attend_tree(
+            self.handle, ctypes.byref(q), _ptr(Q), _ptr(K), _ptr(V), int(K.shape[2]), _ptr(seq_len), _ptr(draft_len),
+            _ptr(tree_mask), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_attend_tree")
+        return {"out": out, "lse": lse} if want_lse else {"out": out}
+
+    def attend_tree_paged(self, Q, K_pool, V_pool, block_table, seq_len, workspace, draft_len=None, tree_mask=None,
+                          scale=None, k_scale=1.0, v_scale=1.0, want_lse=False, out=None, strides=None, num_pages=None):
+        """``lagkv_attend_tree_paged``: the same over pools ``[num_pages, H, page_size, D]`` (``strides`` and
+        ``num_pages`` for another arrangement) behind ``block_table [B, max_blocks]``."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, num_pages)
+        B = self.cfg.B
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(draft_len, "draft_len", (B,))
+        self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
+        out, lse = self._attend_out(Q, out, want_lse)
+        rc = self.lib.lagkv_attend_tree_paged(
+            self.handle, ctypes.byref(q), _ptr(Q), _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(seq_len),
+            _ptr(draft_len), _ptr(tree_mask), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
+            _stream(self._dev()))
+        _check(rc, "lagkv_attend_tree_paged")
+        return {"out": out, "lse": lse} if want_lse else {"out": out}
+
+    def _check_commit(self, seq_len, draft_len, accepted, n_accepted):
+        B = self.cfg.B
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(draft_len, "draft_len", (B,))
+        self._check_ints(n_accepted, "n_accepted", (B,))
+        if accepted.dim() != 2:
+            raise TypeError("accepted must be [B, T]")
+        self._check_ints(accepted, "accepted", (B, accepted.shape[1]))
+        return int(accepted.shape[1])
+
+    def tree_commit(self, K_cache, V_cache, seq_len, accepted, n_accepted, workspace, draft_len=None):
+        """``lagkv_tree_commit``: the first ``n_accepted[b]`` entries of ``accepted [B, T]`` (ascending drafted rows)
+        move to the front of the draft, in place, and ``seq_len`` ends behind them."""
+        T = self._check_commit(seq_len, draft_len, accepted, n_accepted)
+        self._check_contiguous_cache(K_cache, "K_cache")
+        self._check_contiguous_cache(V_cache, "V_cache")
+        if V_cache.shape != K_cache.shape:
+            raise TypeError("K_cache and V_cache must have the same shape")
+        rc = self.lib.lagkv_tree_commit(
+            self.handle, _ptr(K_cache), _ptr(V_cache), int(K_cache.shape[2]), _ptr(seq_len), _ptr(draft_len), T,
+            _ptr(accepted), _ptr(n_accepted), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_tree_commit")
+
+    def tree_commit_paged(self, K_pool, V_pool, block_table, seq_len, accepted, n_accepted, workspace, draft_len=None,
+                          strides=None, num_pages=None):
+        """``lagkv_tree_commit_paged``: the same inside the sequences' own pages."""
+        T = self._check_commit(seq_len, draft_len, accepted, n_accepted)
+        lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, num_pages)
+        rc = self.lib.lagkv_tree_commit_paged(
+            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(seq_len), _ptr(draft_len), T,
+            _ptr(accepted), _ptr(n_accepted), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_tree_commit_paged")
 
 
 # ---- C-named thin functions ---------------------------------------------------------------

@@ -1,0 +1,269 @@
+// Attention over the cache -- host side of the C ABI: argument checks, workspace layout, launches.
+#include "lagkv.h"
+
+#include <cmath>
+#include <cstring>
+
+#include "lagkv_attend_tables.h"
+#include "lagkv_plan.h"
+#include "lagkv_tree_kernels.cuh"
+
+using namespace lagkv;
+
+namespace {
+
+const AttendEntry* find_attend(int D, int dtype, int rows_wanted, int* index) {
+    const AttendEntry* t;
+    const int n = dtype == LAGKV_DTYPE_BF16   ? attend_bf16_kernels(&t)
+                  : dtype == LAGKV_DTYPE_FP16 ? attend_fp16_kernels(&t)
+                                              : attend_fp8_kernels(&t);
+    // the smallest unit that holds all query rows, else the largest there is
+    const AttendEntry* best = nullptr;
+    for (int i = 0; i < n; ++i) {
+        if (t[i].D != D) continue;
+        const bool fits = t[i].rows >= rows_wanted, best_fits = best && best->rows >= rows_wanted;
+        if (best == nullptr || (fits && (!best_fits || t[i].rows < best->rows)) || (!fits && !best_fits && t[i].rows > best->rows)) {
+            best = t + i;
+            *index = i;
+        }
+    }
+    return best;
+}
+
+// Workspace: [status block | counters, a sixteenth of the rest | partials | block choice].  The counters'
+// place depends on the workspace's size alone, so calls of different shapes find them cleared.
+constexpr size_t kHead = kStatusWords * sizeof(int32_t);
+size_t counter_bytes(size_t workspace_bytes) { return ((workspace_bytes - kHead) / 16) & ~size_t(255); }
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+size_t partial_bytes(const lagkv_plan_s* plan, const AttendEntry& e) {
+    return up256(size_t(plan->sm_count) * e.ctas_per_sm * 2 * e.rows * (plan->cfg.D + 2) * sizeof(float));
+}
+long long attend_units(const lagkv_plan_s* plan, const AttendEntry& e, int query_rows, int tokens) {
+    return (long long)plan->cfg.B * plan->cfg.H_kv * tokens * ((query_rows + e.rows - 1) / e.rows);
+}
+// T tokens of G query heads per KV head are well formed
+bool query_shape_ok(const lagkv_config& c, int T, int H_q) {
+    return T >= 1 && T <= 64 && H_q >= c.H_kv && H_q % c.H_kv == 0 && H_q / c.H_kv <= 64;
+}
+size_t choice_bytes(const lagkv_config& c, int T, int64_t blocks, int keep) {
+    if (blocks == 0) return 0;
+    const size_t units = size_t(c.B) * T * c.H_kv;
+    return up256(units * size_t(keep) * sizeof(int32_t)) + up256(units * size_t(blocks) * sizeof(double));
+}
+
+int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, void* out, float* lse, AttendParams* P) {
+    const lagkv_config& c = plan->cfg;
+    if (q == nullptr || Q == nullptr || out == nullptr || c.device < 0) return LAGKV_EINVAL;
+    if (!query_shape_ok(c, q->T, q->H_q)) return LAGKV_EINVAL;
+    if (!aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || Q == out) return LAGKV_EINVAL;
+    const double scale = q->scale == 0.0 ? 1.0 / std::sqrt(double(c.D)) : q->scale;
+    const double ks = q->k_scale == 0.0 ? 1.0 : q->k_scale, vs = q->v_scale == 0.0 ? 1.0 : q->v_scale;
+    if (!(scale > 0.0) || !(ks > 0.0) || !(vs > 0.0) || !std::isfinite(float(scale * ks)) || !std::isfinite(float(vs)))
+        return LAGKV_EINVAL;
+    const int64_t sh = q->stride_h ? q->stride_h : c.D;
+    const int64_t st = q->stride_t ? q->stride_t : (int64_t)q->H_q * sh;
+    const int64_t sb = q->stride_b ? q->stride_b : (int64_t)q->T * st;
+    if (sh < 0 || st < 0 || sb < 0 || sh % 8 || st % 8 || sb % 8) return LAGKV_EINVAL;
+    std::memset(P, 0, sizeof *P);
+    P->Q = static_cast<const uint16_t*>(Q);
+    P->out = static_cast<uint16_t*>(out);
+    P->lse = lse;
+    P->q_sb = sb;
+    P->q_st = st;
+    P->q_sh = sh;
+    P->B = c.B;
+    P->H = c.H_kv;
+    P->G = q->H_q / c.H_kv;
+    P->T = q->T;
+    P->scale_log2 = float(scale * ks * 1.4426950408889634);
+    P->v_scale = float(vs);
+    return LAGKV_OK;
+}
+
+// The cache of a call: contiguous (layout == nullptr) or paged.
+int fill_cache(const lagkv_plan_s* plan, const void* K, const void* V, int64_t S_cap, const lagkv_paged_layout* layout,
+               int64_t num_pages, AttendParams* P) {
+    const lagkv_config& c = plan->cfg;
+    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V)) return LAGKV_EINVAL;
+    Strides st;
+    if (layout != nullptr) {
+        if (layout->page_size < 1 || layout->max_blocks < 1 || num_pages < 1) return LAGKV_EINVAL;
+        S_cap = (int64_t)layout->max_blocks * layout->page_size;
+    }
+    if (S_cap < 1 || S_cap > 0x7fffffffll - 65536) return LAGKV_EINVAL;
+    if (layout != nullptr) {
+        if (resolve_paged(c, layout, S_cap, &st) != LAGKV_OK) return LAGKV_EINVAL;
+    } else if (resolve_strides(c, S_cap, &st) != LAGKV_OK) {
+        return LAGKV_EINVAL;
+    }
+    P->K = static_cast<const uint8_t*>(K);
+    P->V = static_cast<const uint8_t*>(V);
+    P->S_cap = int(S_cap);
+    P->sb = st.sb * 2;
+    P->sh = st.sh * 2;
+    P->ss = st.ss * 2;
+    P->page_stride = st.page_stride * 2;
+    P->block_table = st.block_table;
+    P->max_blocks = st.max_blocks;
+    P->page_shift = st.page_shift;
+    P->num_pages = num_pages;
+    return LAGKV_OK;
+}
+
+int workspace_ok(const void* workspace, size_t bytes, size_t need) {
+    if (workspace == nullptr || bytes < need) return LAGKV_EWORKSPACE;
+    return (reinterpret_cast<uintptr_t>(workspace) & 255u) ? LAGKV_EINVAL : LAGKV_OK;
+}
+
+// Picks the kernel, finds room in the workspace and launches.  `extra`: bytes of the workspace behind
+// the partials that the call uses itself.
+int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, size_t extra, void* workspace, size_t bytes,
+                   AttendParams* P, const AttendEntry** entry, unsigned char** rest) {
+    int index = 0;
+    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, query_rows, &index);
+    if (e == nullptr) return LAGKV_EUNSUPPORTED;
+    const long long units = attend_units(plan, *e, query_rows, tokens);
+    int rc = workspace_ok(workspace, bytes, kHead + 4096);
+    if (rc != LAGKV_OK) return rc;
+    const size_t cb = counter_bytes(bytes), pb = partial_bytes(plan, *e);
+    if (size_t(units) * sizeof(int32_t) > cb || kHead + cb + pb + extra > bytes) return LAGKV_EWORKSPACE;
+    unsigned char* base = static_cast<unsigned char*>(workspace);
+    P->status = reinterpret_cast<int32_t*>(base);
+    P->counters = reinterpret_cast<int32_t*>(base + kHead);
+    P->partials = reinterpret_cast<float*>(base + kHead + cb);
+    P->mtiles = (query_rows + e->rows - 1) / e->rows;
+    *entry = e;
+    *rest = base + kHead + cb + pb;
+    if (!(plan->attend_ready.load(std::memory_order_acquire) >> index & 1)) {
+        if (!raise_smem_limit(reinterpret_cast<const void*>(e->fn), e->smem)) return LAGKV_ECUDA;
+        plan->attend_ready.fetch_or(1ull << index, std::memory_order_release);
+    }
+    return LAGKV_OK;
+}
+int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cudaStream_t stream) {
+    void* args[] = {&P};
+    if (cudaLaunchKernel(reinterpret_cast<const void*>(e.fn), dim3((unsigned)(plan->sm_count * e.ctas_per_sm)),
+                         dim3(e.threads), args, e.smem, stream) != cudaSuccess)
+        return LAGKV_ECUDA;
+    return check_launch();
+}
+
+int attend_tree(lagkv_plan_t plan, const lagkv_query* query, const void* Q, const void* K, const void* V, int64_t S_cap,
+                const lagkv_paged_layout* layout, int64_t num_pages, const int32_t* seq_len, const int32_t* draft_len,
+                const uint64_t* tree_mask, void* out, float* lse, void* workspace, size_t bytes, void* cuda_stream) {
+    if (plan == nullptr || seq_len == nullptr) return LAGKV_EINVAL;
+    AttendParams P;
+    int rc = fill_query(plan, query, Q, out, lse, &P);
+    if (rc == LAGKV_OK) rc = fill_cache(plan, K, V, S_cap, layout, num_pages, &P);
+    if (rc != LAGKV_OK) return rc;
+    if ((reinterpret_cast<uintptr_t>(seq_len) & 3u) || (reinterpret_cast<uintptr_t>(draft_len) & 3u) ||
+        (reinterpret_cast<uintptr_t>(tree_mask) & 7u))
+        return LAGKV_EINVAL;
+    P.seq_len = seq_len;
+    P.draft_len = draft_len;
+    P.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
+    DeviceGuard guard(plan->cfg.device);
+    const AttendEntry* e;
+    unsigned char* rest;
+    rc = attend_prepare(plan, P.T * P.G, 1, 0, workspace, bytes, &P, &e, &rest);
+    if (rc != LAGKV_OK) return rc;
+    return attend_launch(plan, *e, P, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int tree_commit(lagkv_plan_t plan, void* K, void* V, int64_t S_cap, const lagkv_paged_layout* layout, int64_t num_pages,
+                int32_t* seq_len, const int32_t* draft_len, int32_t T, const int32_t* accepted, const int32_t* n_accepted,
+                void* workspace, size_t bytes, void* cuda_stream) {
+    if (plan == nullptr || plan->cfg.device < 0 || seq_len == nullptr || accepted == nullptr || n_accepted == nullptr ||
+        T < 1 || T > 64 || K == V)
+        return LAGKV_EINVAL;
+    AttendParams P;
+    std::memset(&P, 0, sizeof P);
+    int rc = fill_cache(plan, K, V, S_cap, layout, num_pages, &P);
+    if (rc == LAGKV_OK) rc = workspace_ok(workspace, bytes, kHead);
+    if (rc != LAGKV_OK) return rc;
+    if ((reinterpret_cast<uintptr_t>(seq_len) & 3u) || (reinterpret_cast<uintptr_t>(draft_len) & 3u) ||
+        (reinterpret_cast<uintptr_t>(accepted) & 3u) || (reinterpret_cast<uintptr_t>(n_accepted) & 3u))
+        return LAGKV_EINVAL;
+    P.draft_len = draft_len;
+    P.status = static_cast<int32_t*>(workspace);
+    P.B = plan->cfg.B;
+    P.H = plan->cfg.H_kv;
+    P.T = T;
+    DeviceGuard guard(plan->cfg.device);
+    lagkv_tree_commit_kernel<<<plan->cfg.B, kCommitThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+        P, static_cast<uint8_t*>(K), static_cast<uint8_t*>(V), int(row_bytes(plan->cfg) / 16), seq_len, accepted, n_accepted);
+    return check_launch();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, int64_t blocks, int32_t keep) {
+    if (plan == nullptr || !query_shape_ok(plan->cfg, T, H_q) || blocks < 0 || keep < 0) return 0;
+    if (blocks > 0 && (keep < 1 || blocks > 0x7fffffffll / 16)) return 0;
+    const int G = H_q / plan->cfg.H_kv;
+    // every smaller call of either kind: one token per unit with few query rows, all rows in one unit
+    size_t partials = 0, units = 0;
+    for (int rows = 1; rows <= T * G; rows = rows < 128 ? rows * 2 : T * G + 1) {
+        for (int r : {rows, T * G, G}) {
+            int index;
+            const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, r, &index);
+            if (e == nullptr) return 0;
+            if (partial_bytes(plan, *e) > partials) partials = partial_bytes(plan, *e);
+        }
+    }
+    const size_t most = size_t(T) * ((G + 15) / 16);  // units per (sequence, KV head): no unit has fewer than 16 rows
+    const size_t dense = (size_t(T) * G + 15) / 16;
+    units = size_t(plan->cfg.B) * plan->cfg.H_kv * (most > dense ? most : dense);
+    const size_t rest = partials + choice_bytes(plan->cfg, T, blocks, keep), counters = up256(units * sizeof(int32_t));
+    size_t body = rest + rest / 15 + 4096;          // a sixteenth of the body goes to the counters
+    if (body < 16 * (counters + 256)) body = 16 * (counters + 256);
+    if (body - counter_bytes(kHead + body) < rest) body += body / 8;
+    return kHead + up256(body);
+}
+
+int lagkv_attend_workspace_init(lagkv_plan_t plan, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (plan == nullptr || plan->cfg.device < 0) return LAGKV_EINVAL;
+    const int rc = workspace_ok(workspace, workspace_bytes, kHead);
+    if (rc != LAGKV_OK) return rc;
+    DeviceGuard guard(plan->cfg.device);
+    const size_t clear = kHead + counter_bytes(workspace_bytes);
+    return cudaMemsetAsync(workspace, 0, clear, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LAGKV_OK
+                                                                                                        : LAGKV_ECUDA;
+}
+
+int lagkv_attend_tree(lagkv_plan_t plan, const lagkv_query* query, const void* Q, const void* K, const void* V,
+                      int64_t S_cap, const int32_t* seq_len, const int32_t* draft_len, const uint64_t* tree_mask,
+                      void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return attend_tree(plan, query, Q, K, V, S_cap, nullptr, 0, seq_len, draft_len, tree_mask, out, lse_out, workspace,
+                       workspace_bytes, cuda_stream);
+}
+
+int lagkv_attend_tree_paged(lagkv_plan_t plan, const lagkv_query* query, const void* Q, const void* K_pool,
+                            const void* V_pool, const lagkv_paged_layout* layout, int64_t num_pages,
+                            const int32_t* seq_len, const int32_t* draft_len, const uint64_t* tree_mask, void* out,
+                            float* lse_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (layout == nullptr) return LAGKV_EINVAL;
+    return attend_tree(plan, query, Q, K_pool, V_pool, 0, layout, num_pages, seq_len, draft_len, tree_mask, out, lse_out,
+                       workspace, workspace_bytes, cuda_stream);
+}
+
+int lagkv_tree_commit(lagkv_plan_t plan, void* K_cache, void* V_cache, int64_t S_cap, int32_t* seq_len,
+                      const int32_t* draft_len, int32_t T, const int32_t* accepted, const int32_t* n_accepted,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return tree_commit(plan, K_cache, V_cache, S_cap, nullptr, 0, seq_len, draft_len, T, accepted, n_accepted, workspace,
+                       workspace_bytes, cuda_stream);
+}
+
+int lagkv_tree_commit_paged(lagkv_plan_t plan, void* K_pool, void* V_pool, const lagkv_paged_layout* layout,
+                            int64_t num_pages, int32_t* seq_len, const int32_t* draft_len, int32_t T,
+                            const int32_t* accepted, const int32_t* n_accepted, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream) {
+    if (layout == nullptr) return LAGKV_EINVAL;
+    return tree_commit(plan, K_pool, V_pool, 0, layout, num_pages, seq_len, draft_len, T, accepted, n_accepted, workspace,
+                       workspace_bytes, cuda_stream);
+}
+
+}  // extern "C"

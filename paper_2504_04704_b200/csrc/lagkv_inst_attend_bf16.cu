@@ -1,0 +1,13 @@
+// Attention kernels for bf16 caches, every head_dim.
+#include "lagkv_attend_tables.h"
+
+namespace lagkv {
+namespace {
+const AttendEntry kTable[] = {LAGKV_ATTEND_ENTRIES(0)};
+}  // namespace
+
+int attend_bf16_kernels(const AttendEntry** table) {
+    *table = kTable;
+    return int(sizeof(kTable) / sizeof(kTable[0]));
+}
+}  // namespace lagkv
