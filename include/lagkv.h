@@ -342,9 +342,9 @@ typedef struct {
 } lagkv_query;
 
 /*
- * Bytes of workspace for lagkv_attend_tree() (blocks = keep = 0) or the attention over chosen blocks
- * (blocks = blocks per sequence of its bounds, keep as in its choice) with up to T tokens and H_q
- * heads; 0 = bad arguments.  A workspace may serve every smaller call, tree and blocks alike.  256-byte aligned,
+ * Bytes of workspace for lagkv_attend_tree() (blocks = keep = 0) or lagkv_attend_blocks() (blocks =
+ * blocks per sequence of its bounds, keep as in its choice) with up to T tokens and H_q heads; 0 = bad
+ * arguments.  A workspace may serve every smaller call, tree and blocks alike.  256-byte aligned,
  * cleared once with lagkv_attend_workspace_init() (async on the stream; the kernels leave what they
  * need cleared); starts with a status block that lagkv_read_status() reads.
  */
@@ -362,6 +362,7 @@ int lagkv_attend_workspace_init(lagkv_plan_t plan, void *workspace, size_t works
  *   out      [B, T, H_q, D] contiguous; lse_out fp32 [B, T, H_q] or NULL: natural log of the sum of
  *            exp(scale*k_scale*q.k) over the rows seen.  A token that sees no row, and the padding
  *            tokens t >= draft_len[b], get out = 0 and lse = -infinity.
+ * seq_len[b] = 0 is an empty slot of the batch (no tokens when draft_len is NULL).
  * seq_len[b] outside [0, S_cap], draft_len[b] outside [0, T] or above seq_len[b]: that sequence counts as
  * without tokens and LAGKV_EINVAL is recorded in the status block.
  * One launch with the same arguments for every length; results do not depend on the schedule.
@@ -393,6 +394,53 @@ int lagkv_tree_commit_paged(lagkv_plan_t plan, void *K_pool, void *V_pool, const
                             int64_t num_pages, int32_t *seq_len, const int32_t *draft_len, int32_t T,
                             const int32_t *accepted, const int32_t *n_accepted, void *workspace,
                             size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Bounds of the blocks of a cache: block j of a (sequence, KV head) is its rows [j*block_rows,
+ * (j+1)*block_rows) below seq_len[b]; bounds[b][h][j][0] and [1] are the per-channel minimum and maximum of
+ * their K rows, in the plan's storage format (exact), [B, H_kv, blocks, 2, D] contiguous.
+ *   from_len  DEVICE int32 [B] or NULL (0): rows below it have not changed since the bounds were last
+ *             written; blocks that end at or before it are left as they are.  After a token has been
+ *             appended this is the old length, after lagkv_compress_append() the static_len before it.
+ *   block_rows  16, 32, 64 or 128; blocks*block_rows >= S_cap.
+ * Blocks behind the last row are not written.  NaN in a seen K row leaves that channel undefined.
+ */
+int lagkv_block_bounds(lagkv_plan_t plan, const void *K, int64_t S_cap, const int32_t *from_len,
+                       const int32_t *seq_len, int32_t block_rows, void *bounds, int64_t blocks, void *workspace,
+                       size_t workspace_bytes, void *cuda_stream);
+int lagkv_block_bounds_paged(lagkv_plan_t plan, const void *K_pool, const lagkv_paged_layout *layout,
+                             int64_t num_pages, const int32_t *from_len, const int32_t *seq_len, int32_t block_rows,
+                             void *bounds, int64_t blocks, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+typedef struct {
+    int32_t block_rows;     /* rows per block of the bounds: 16, 32, 64 or 128                          */
+    int32_t keep;           /* blocks each (token, KV head) attends to, at most 4096                    */
+    int32_t sink_blocks;    /* of these, the first ones of the sequence, always kept ...                */
+    int32_t recent_blocks;  /* ... and the last ones; sink_blocks + recent_blocks <= keep               */
+    int64_t blocks;         /* blocks per (sequence, KV head) of the bounds, at most 24576              */
+} lagkv_block_choice;
+
+/*
+ * Attention to a choice of blocks.  Token t of sequence b sees the rows below end = seq_len[b] - (T-1-t)
+ * (its own row is the last of them) that lie in the blocks chosen for it and for each KV head: the
+ * first sink_blocks and the last recent_blocks of its ceil(end/block_rows) blocks, and of the others
+ * those with the largest score
+ *     max over the query heads g of the KV head of  sum_c max(q_gc*min_c, q_gc*max_c)
+ * (no logit of the block is larger), `keep` in all, the lower block among equals.  Scores are summed in
+ * 64 bits.  bounds must cover every row below seq_len[b].  Rows at or behind `end` never reach a token.
+ *   idx_out  int32 [B, T, H_kv, keep] or NULL: the chosen blocks, ascending, -1 behind the last.
+ * seq_len[b] outside [0, S_cap], or in 1..T-1: LAGKV_EINVAL is recorded; such a sequence and an empty one
+ * (seq_len[b] = 0) get out = 0, lse = -infinity, idx = -1.
+ * out, lse_out and the rest as for lagkv_attend_tree().  Three launches.
+ */
+int lagkv_attend_blocks(lagkv_plan_t plan, const lagkv_query *query, const lagkv_block_choice *choice, const void *Q,
+                        const void *K, const void *V, int64_t S_cap, const int32_t *seq_len, const void *bounds,
+                        void *out, float *lse_out, int32_t *idx_out, void *workspace, size_t workspace_bytes,
+                        void *cuda_stream);
+int lagkv_attend_blocks_paged(lagkv_plan_t plan, const lagkv_query *query, const lagkv_block_choice *choice,
+                              const void *Q, const void *K_pool, const void *V_pool, const lagkv_paged_layout *layout,
+                              int64_t num_pages, const int32_t *seq_len, const void *bounds, void *out, float *lse_out,
+                              int32_t *idx_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
  * Synchronise cuda_stream, copy the status block to the host and clear it.  workspace == NULL

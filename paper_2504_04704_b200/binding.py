@@ -32,7 +32,8 @@ EXPORTS = (
     "lagkv_compress_append", "lagkv_compress_append_noalloc", "lagkv_compress_prefill_paged",
     "lagkv_compress_append_paged", "lagkv_gather", "lagkv_gather_paged",
     "lagkv_attend_workspace_bytes", "lagkv_attend_workspace_init", "lagkv_attend_tree", "lagkv_attend_tree_paged",
-    "lagkv_tree_commit", "lagkv_tree_commit_paged",
+    "lagkv_tree_commit", "lagkv_tree_commit_paged", "lagkv_block_bounds", "lagkv_block_bounds_paged",
+    "lagkv_attend_blocks", "lagkv_attend_blocks_paged",
     "lagkv_read_status",
     "lagkv_launch_info", "lagkv_plan_tune", "lagkv_selftest_bounded_wait", "lagkv_status_string", "lagkv_version",
 )
@@ -67,6 +68,13 @@ class lagkv_query(ctypes.Structure):
         ("T", ctypes.c_int32), ("H_q", ctypes.c_int32),
         ("scale", ctypes.c_double), ("k_scale", ctypes.c_double), ("v_scale", ctypes.c_double),
         ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+    ]
+
+
+class lagkv_block_choice(ctypes.Structure):
+    _fields_ = [
+        ("block_rows", ctypes.c_int32), ("keep", ctypes.c_int32), ("sink_blocks", ctypes.c_int32),
+        ("recent_blocks", ctypes.c_int32), ("blocks", ctypes.c_int64),
     ]
 
 
@@ -133,6 +141,15 @@ def load_library() -> ctypes.CDLL:
     lib.lagkv_tree_commit.argtypes = [vp, vp, vp, i64, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.lagkv_tree_commit_paged.restype = ctypes.c_int
     lib.lagkv_tree_commit_paged.argtypes = [vp, vp, vp, layout, i64, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.lagkv_block_bounds.restype = ctypes.c_int
+    lib.lagkv_block_bounds.argtypes = [vp, vp, i64, vp, vp, i32, vp, i64, vp, sz, vp]
+    lib.lagkv_block_bounds_paged.restype = ctypes.c_int
+    lib.lagkv_block_bounds_paged.argtypes = [vp, vp, layout, i64, vp, vp, i32, vp, i64, vp, sz, vp]
+    choice = ctypes.POINTER(lagkv_block_choice)
+    lib.lagkv_attend_blocks.restype = ctypes.c_int
+    lib.lagkv_attend_blocks.argtypes = [vp, query, choice, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_attend_blocks_paged.restype = ctypes.c_int
+    lib.lagkv_attend_blocks_paged.argtypes = [vp, query, choice, vp, vp, vp, layout, i64, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lagkv_read_status.restype = ctypes.c_int
     lib.lagkv_read_status.argtypes = [vp, vp, vp, ctypes.POINTER(i32 * 4)]
     lib.lagkv_launch_info.restype = ctypes.c_int
@@ -534,6 +551,90 @@ class Plan:
             self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(seq_len), _ptr(draft_len), T,
             _ptr(accepted), _ptr(n_accepted), _ptr(workspace), workspace.numel(), _stream(self._dev()))
         _check(rc, "lagkv_tree_commit_paged")
+
+    # ---- blocks
+    def new_block_bounds(self, S_cap: int, block_rows: int = 64) -> torch.Tensor:
+        """Bounds ``[B, H, blocks, 2, D]`` for a cache of ``S_cap`` rows, in the plan's storage format."""
+        c = self.cfg
+        return torch.zeros((c.B, c.H_kv, -(-int(S_cap) // int(block_rows)), 2, c.D), dtype=torch.uint8 if self.dtype ==
+                           torch.float8_e4m3fn else self.dtype, device=self._dev()).view(self.dtype)
+
+    def _check_bounds(self, bounds):
+        c = self.cfg
+        self._check_cache(bounds, "bounds")
+        if bounds.dim() != 5 or (bounds.shape[0], bounds.shape[1], bounds.shape[3], bounds.shape[4]) != (c.B, c.H_kv, 2, c.D) or \
+                not bounds.is_contiguous():
+            raise TypeError(f"bounds must be contiguous [{c.B}, {c.H_kv}, blocks, 2, {c.D}]")
+        return int(bounds.shape[2])
+
+    def block_bounds(self, K, seq_len, bounds, workspace, block_rows=64, from_len=None):
+        """``lagkv_block_bounds``: per-channel minimum and maximum of each block of ``block_rows`` K rows below
+        ``seq_len`` (blocks that end at or before ``from_len`` stay as they are)."""
+        self._check_contiguous_cache(K, "K")
+        blocks = self._check_bounds(bounds)
+        self._check_ints(seq_len, "seq_len", (self.cfg.B,))
+        self._check_ints(from_len, "from_len", (self.cfg.B,))
+        rc = self.lib.lagkv_block_bounds(self.handle, _ptr(K), int(K.shape[2]), _ptr(from_len), _ptr(seq_len), int(block_rows),
+                                         _ptr(bounds), blocks, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_block_bounds")
+
+    def block_bounds_paged(self, K_pool, block_table, seq_len, bounds, workspace, block_rows=64, from_len=None, strides=None,
+                           num_pages=None):
+        """``lagkv_block_bounds_paged``: the same over a pool of pages."""
+        lay, pages = self._paged_pool(K_pool, None, block_table, strides, num_pages)
+        blocks = self._check_bounds(bounds)
+        self._check_ints(seq_len, "seq_len", (self.cfg.B,))
+        self._check_ints(from_len, "from_len", (self.cfg.B,))
+        rc = self.lib.lagkv_block_bounds_paged(
+            self.handle, _ptr(K_pool), ctypes.byref(lay), pages, _ptr(from_len), _ptr(seq_len), int(block_rows), _ptr(bounds),
+            blocks, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_block_bounds_paged")
+
+    def _blocks_out(self, Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse, want_idx):
+        blocks = self._check_bounds(bounds)
+        self._check_ints(seq_len, "seq_len", (self.cfg.B,))
+        choice = lagkv_block_choice(int(block_rows), int(keep), int(sink_blocks), int(recent_blocks), blocks)
+        out, lse = self._attend_out(Q, out, want_lse)
+        idx = torch.empty((self.cfg.B, Q.shape[1], self.cfg.H_kv, int(keep)), dtype=torch.int32, device=Q.device) if want_idx else None
+        got = {"out": out}
+        if want_lse:
+            got["lse"] = lse
+        if want_idx:
+            got["idx"] = idx
+        return choice, got, lse, idx
+
+    def attend_blocks(self, Q, K, V, seq_len, bounds, workspace, block_rows=64, keep=32, sink_blocks=1, recent_blocks=2,
+                      scale=None, k_scale=1.0, v_scale=1.0, want_lse=False, want_idx=False, out=None):
+        """``lagkv_attend_blocks``: ``Q [B, T, H_q, D]`` (the last T tokens of each sequence) attends to the rows of
+        ``keep`` blocks per token and KV head: the first ``sink_blocks``, the last ``recent_blocks`` and those whose
+        bounds promise the largest logit.  Returns ``{"out", "lse", "idx"}`` (the last two when asked for)."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        self._check_contiguous_cache(K, "K")
+        self._check_contiguous_cache(V, "V")
+        if V.shape != K.shape:
+            raise TypeError("K and V must have the same shape")
+        choice, got, lse, idx = self._blocks_out(Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse,
+                                                 want_idx)
+        rc = self.lib.lagkv_attend_blocks(
+            self.handle, ctypes.byref(q), ctypes.byref(choice), _ptr(Q), _ptr(K), _ptr(V), int(K.shape[2]), _ptr(seq_len),
+            _ptr(bounds), _ptr(got["out"]), _ptr(lse), _ptr(idx), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_attend_blocks")
+        return got
+
+    def attend_blocks_paged(self, Q, K_pool, V_pool, block_table, seq_len, bounds, workspace, block_rows=64, keep=32,
+                            sink_blocks=1, recent_blocks=2, scale=None, k_scale=1.0, v_scale=1.0, want_lse=False,
+                            want_idx=False, out=None, strides=None, num_pages=None):
+        """``lagkv_attend_blocks_paged``: the same over pools of pages."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, num_pages)
+        choice, got, lse, idx = self._blocks_out(Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse,
+                                                 want_idx)
+        rc = self.lib.lagkv_attend_blocks_paged(
+            self.handle, ctypes.byref(q), ctypes.byref(choice), _ptr(Q), _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages,
+            _ptr(seq_len), _ptr(bounds), _ptr(got["out"]), _ptr(lse), _ptr(idx), _ptr(workspace), workspace.numel(),
+            _stream(self._dev()))
+        _check(rc, "lagkv_attend_blocks_paged")
+        return got
 
 
 # ---- C-named thin functions ---------------------------------------------------------------

@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "lagkv_attend_tables.h"
+#include "lagkv_block_kernels.cuh"
 #include "lagkv_plan.h"
 #include "lagkv_tree_kernels.cuh"
 
@@ -81,11 +82,13 @@ int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, vo
     return LAGKV_OK;
 }
 
+constexpr int kMaxKeep = 4096, kMaxBlocks = 24576;  // the choice holds a unit's keys in shared memory
+
 // The cache of a call: contiguous (layout == nullptr) or paged.
 int fill_cache(const lagkv_plan_s* plan, const void* K, const void* V, int64_t S_cap, const lagkv_paged_layout* layout,
                int64_t num_pages, AttendParams* P) {
     const lagkv_config& c = plan->cfg;
-    if (K == nullptr || V == nullptr || !aligned16(K) || !aligned16(V)) return LAGKV_EINVAL;
+    if (K == nullptr || !aligned16(K) || !aligned16(V)) return LAGKV_EINVAL;
     Strides st;
     if (layout != nullptr) {
         if (layout->page_size < 1 || layout->max_blocks < 1 || num_pages < 1) return LAGKV_EINVAL;
@@ -152,7 +155,7 @@ int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cuda
 int attend_tree(lagkv_plan_t plan, const lagkv_query* query, const void* Q, const void* K, const void* V, int64_t S_cap,
                 const lagkv_paged_layout* layout, int64_t num_pages, const int32_t* seq_len, const int32_t* draft_len,
                 const uint64_t* tree_mask, void* out, float* lse, void* workspace, size_t bytes, void* cuda_stream) {
-    if (plan == nullptr || seq_len == nullptr) return LAGKV_EINVAL;
+    if (plan == nullptr || seq_len == nullptr || V == nullptr) return LAGKV_EINVAL;
     AttendParams P;
     int rc = fill_query(plan, query, Q, out, lse, &P);
     if (rc == LAGKV_OK) rc = fill_cache(plan, K, V, S_cap, layout, num_pages, &P);
@@ -175,7 +178,7 @@ int tree_commit(lagkv_plan_t plan, void* K, void* V, int64_t S_cap, const lagkv_
                 int32_t* seq_len, const int32_t* draft_len, int32_t T, const int32_t* accepted, const int32_t* n_accepted,
                 void* workspace, size_t bytes, void* cuda_stream) {
     if (plan == nullptr || plan->cfg.device < 0 || seq_len == nullptr || accepted == nullptr || n_accepted == nullptr ||
-        T < 1 || T > 64 || K == V)
+        T < 1 || T > 64 || V == nullptr || K == V)
         return LAGKV_EINVAL;
     AttendParams P;
     std::memset(&P, 0, sizeof P);
@@ -196,13 +199,108 @@ int tree_commit(lagkv_plan_t plan, void* K, void* V, int64_t S_cap, const lagkv_
     return check_launch();
 }
 
+int block_shift_of(int rows) { return rows == 16 ? 4 : rows == 32 ? 5 : rows == 64 ? 6 : rows == 128 ? 7 : -1; }
+
+int block_bounds(lagkv_plan_t plan, const void* K, int64_t S_cap, const lagkv_paged_layout* layout, int64_t num_pages,
+                 const int32_t* from_len, const int32_t* seq_len, int32_t block_rows, void* bounds, int64_t blocks,
+                 void* workspace, size_t bytes, void* cuda_stream) {
+    if (plan == nullptr || plan->cfg.device < 0 || seq_len == nullptr || bounds == nullptr || !aligned16(bounds))
+        return LAGKV_EINVAL;
+    const lagkv_config& c = plan->cfg;
+    AttendParams P;
+    std::memset(&P, 0, sizeof P);
+    int rc = fill_cache(plan, K, nullptr, S_cap, layout, num_pages, &P);
+    if (rc == LAGKV_OK) rc = workspace_ok(workspace, bytes, kHead);
+    if (rc != LAGKV_OK) return rc;
+    P.block_shift = block_shift_of(block_rows);
+    if (P.block_shift < 0 || blocks < 1 || (blocks << P.block_shift) < P.S_cap || K == bounds) return LAGKV_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(seq_len) & 3u) || (reinterpret_cast<uintptr_t>(from_len) & 3u)) return LAGKV_EINVAL;
+    P.seq_len = seq_len;
+    P.status = static_cast<int32_t*>(workspace);
+    P.B = c.B;
+    P.H = c.H_kv;
+    DeviceGuard guard(c.device);
+    // CTAs per (sequence, KV head): many for a whole cache, so that ragged lengths even out, few when only
+    // the last rows have changed (each CTA's eight warps walk the blocks in strides either way)
+    const long long units = (long long)c.B * c.H_kv, want = (long long)plan->sm_count * (from_len ? 4 : 32);
+    const long long most = ((long long)P.S_cap + (8ll << P.block_shift) - 1) / (8ll << P.block_shift);
+    long long per = (want + units - 1) / units;
+    if (per > most) per = most;
+    if (units * per > 0x7fffffffll) return LAGKV_EINVAL;
+    const int cpr = int(row_bytes(c) / 16);
+    const dim3 grid((unsigned)(units * per));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (c.dtype == LAGKV_DTYPE_BF16)
+        lagkv_block_bounds_kernel<0><<<grid, kBoundsThreads, 0, stream>>>(P, from_len, static_cast<uint8_t*>(bounds), blocks, int(per), cpr);
+    else if (c.dtype == LAGKV_DTYPE_FP16)
+        lagkv_block_bounds_kernel<1><<<grid, kBoundsThreads, 0, stream>>>(P, from_len, static_cast<uint8_t*>(bounds), blocks, int(per), cpr);
+    else
+        lagkv_block_bounds_kernel<2><<<grid, kBoundsThreads, 0, stream>>>(P, from_len, static_cast<uint8_t*>(bounds), blocks, int(per), cpr);
+    return check_launch();
+}
+
+int attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block_choice* choice, const void* Q,
+                  const void* K, const void* V, int64_t S_cap, const lagkv_paged_layout* layout, int64_t num_pages,
+                  const int32_t* seq_len, const void* bounds, void* out, float* lse, int32_t* idx_out, void* workspace,
+                  size_t bytes, void* cuda_stream) {
+    if (plan == nullptr || seq_len == nullptr || V == nullptr || choice == nullptr || bounds == nullptr || !aligned16(bounds))
+        return LAGKV_EINVAL;
+    AttendParams P;
+    int rc = fill_query(plan, query, Q, out, lse, &P);
+    if (rc == LAGKV_OK) rc = fill_cache(plan, K, V, S_cap, layout, num_pages, &P);
+    if (rc != LAGKV_OK) return rc;
+    P.block_shift = block_shift_of(choice->block_rows);
+    if (P.block_shift < 0 || choice->keep < 1 || choice->sink_blocks < 0 || choice->recent_blocks < 0 ||
+        (int64_t)choice->sink_blocks + choice->recent_blocks > choice->keep || choice->blocks < 1)
+        return LAGKV_EINVAL;
+    if (choice->keep > kMaxKeep || choice->blocks > kMaxBlocks) return LAGKV_EUNSUPPORTED;
+    if ((choice->blocks << P.block_shift) < P.S_cap) return LAGKV_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(seq_len) & 3u) || (reinterpret_cast<uintptr_t>(idx_out) & 3u)) return LAGKV_EINVAL;
+    const lagkv_config& c = plan->cfg;
+    P.seq_len = seq_len;
+    P.keep = choice->keep;
+    const long long units = (long long)P.B * P.T * P.H;
+    const int chunks = int((choice->blocks + kScoreBlocks - 1) / kScoreBlocks);
+    if (units * chunks > 0x7fffffffll) return LAGKV_EINVAL;
+    DeviceGuard guard(c.device);
+    const AttendEntry* e;
+    unsigned char* rest;
+    rc = attend_prepare(plan, P.G, P.T, choice_bytes(c, P.T, choice->blocks, choice->keep), workspace, bytes, &P, &e, &rest);
+    if (rc != LAGKV_OK) return rc;
+    int32_t* idx = idx_out ? idx_out : reinterpret_cast<int32_t*>(rest);
+    unsigned long long* keys = reinterpret_cast<unsigned long long*>(rest + up256(size_t(units) * P.keep * sizeof(int32_t)));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const uint8_t* bd = static_cast<const uint8_t*>(bounds);
+    const size_t score_smem = size_t(kScoreHeads) * (c.D + 2) * sizeof(double);
+    const dim3 sgrid((unsigned)(units * chunks));
+    if (c.dtype == LAGKV_DTYPE_BF16)
+        lagkv_block_score_kernel<0><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
+    else if (c.dtype == LAGKV_DTYPE_FP16)
+        lagkv_block_score_kernel<1><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
+    else
+        lagkv_block_score_kernel<2><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
+    const size_t select_smem = size_t(choice->blocks) * sizeof(unsigned long long);
+    constexpr unsigned long long kSelectReady = 1ull << 63;
+    if (!(plan->attend_ready.load(std::memory_order_acquire) & kSelectReady)) {
+        if (!raise_smem_limit(reinterpret_cast<const void*>(&lagkv_block_select_kernel), size_t(kMaxBlocks) * sizeof(unsigned long long)))
+            return LAGKV_ECUDA;
+        plan->attend_ready.fetch_or(kSelectReady, std::memory_order_release);
+    }
+    lagkv_block_select_kernel<<<dim3((unsigned)units), kSelectThreads, select_smem, stream>>>(
+        P, keys, choice->blocks, choice->sink_blocks, choice->recent_blocks, idx);
+    rc = check_launch();
+    if (rc != LAGKV_OK) return rc;
+    P.idx = idx;
+    return attend_launch(plan, *e, P, stream);
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, int64_t blocks, int32_t keep) {
     if (plan == nullptr || !query_shape_ok(plan->cfg, T, H_q) || blocks < 0 || keep < 0) return 0;
-    if (blocks > 0 && (keep < 1 || blocks > 0x7fffffffll / 16)) return 0;
+    if (blocks > 0 && (keep < 1 || keep > kMaxKeep || blocks > kMaxBlocks)) return 0;
     const int G = H_q / plan->cfg.H_kv;
     // every smaller call of either kind: one token per unit with few query rows, all rows in one unit
     size_t partials = 0, units = 0;
@@ -264,6 +362,38 @@ int lagkv_tree_commit_paged(lagkv_plan_t plan, void* K_pool, void* V_pool, const
     if (layout == nullptr) return LAGKV_EINVAL;
     return tree_commit(plan, K_pool, V_pool, 0, layout, num_pages, seq_len, draft_len, T, accepted, n_accepted, workspace,
                        workspace_bytes, cuda_stream);
+}
+
+int lagkv_block_bounds(lagkv_plan_t plan, const void* K, int64_t S_cap, const int32_t* from_len, const int32_t* seq_len,
+                       int32_t block_rows, void* bounds, int64_t blocks, void* workspace, size_t workspace_bytes,
+                       void* cuda_stream) {
+    return block_bounds(plan, K, S_cap, nullptr, 0, from_len, seq_len, block_rows, bounds, blocks, workspace,
+                        workspace_bytes, cuda_stream);
+}
+
+int lagkv_block_bounds_paged(lagkv_plan_t plan, const void* K_pool, const lagkv_paged_layout* layout, int64_t num_pages,
+                             const int32_t* from_len, const int32_t* seq_len, int32_t block_rows, void* bounds,
+                             int64_t blocks, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (layout == nullptr) return LAGKV_EINVAL;
+    return block_bounds(plan, K_pool, 0, layout, num_pages, from_len, seq_len, block_rows, bounds, blocks, workspace,
+                        workspace_bytes, cuda_stream);
+}
+
+int lagkv_attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block_choice* choice, const void* Q,
+                        const void* K, const void* V, int64_t S_cap, const int32_t* seq_len, const void* bounds,
+                        void* out, float* lse_out, int32_t* idx_out, void* workspace, size_t workspace_bytes,
+                        void* cuda_stream) {
+    return attend_blocks(plan, query, choice, Q, K, V, S_cap, nullptr, 0, seq_len, bounds, out, lse_out, idx_out,
+                         workspace, workspace_bytes, cuda_stream);
+}
+
+int lagkv_attend_blocks_paged(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block_choice* choice,
+                              const void* Q, const void* K_pool, const void* V_pool, const lagkv_paged_layout* layout,
+                              int64_t num_pages, const int32_t* seq_len, const void* bounds, void* out, float* lse_out,
+                              int32_t* idx_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (layout == nullptr) return LAGKV_EINVAL;
+    return attend_blocks(plan, query, choice, Q, K_pool, V_pool, 0, layout, num_pages, seq_len, bounds, out, lse_out,
+                         idx_out, workspace, workspace_bytes, cuda_stream);
 }
 
 }  // extern "C"

@@ -155,7 +155,7 @@ struct AttendSeq {
 __device__ __forceinline__ AttendSeq attend_seq(const AttendParams& P, int b, bool report) {
     AttendSeq s;
     s.len = __ldg(P.seq_len + b);
-    s.tokens = P.draft_len ? __ldg(P.draft_len + b) : P.T;
+    s.tokens = P.draft_len ? __ldg(P.draft_len + b) : s.len == 0 ? 0 : P.T;  // an empty slot of the batch is no error
     if (s.len < 0 || s.len > P.S_cap || s.tokens < 0 || s.tokens > P.T || s.tokens > s.len) {
         if (report) record_status(P.status, ST_EINVAL, b);
         s.len = s.tokens = 0;
