@@ -192,7 +192,7 @@ def _prepare_pages(s, case, lens, g, rng, dev, dtype):
     if own:
         from paper_2504_04704_b200 import binding
         s["plan"] = binding.Plan(B, H, D, sink=16, lag=128, dtype=dtype, device=torch.cuda.current_device())
-        s["ws"] = s["plan"].new_pages_workspace(pages, nb)
+        s["ws"] = s["plan"].new_pages_workspace(pages)
     return s
 
 
