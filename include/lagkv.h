@@ -443,6 +443,63 @@ int lagkv_attend_blocks_paged(lagkv_plan_t plan, const lagkv_query *query, const
                               int32_t *idx_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * ---- Pages --------------------------------------------------------------------------------
+ * A pool of num_pages pages, block tables over it (lagkv_paged_layout; entries are -1 where a sequence
+ * has no page) and refs (DEVICE int32 [num_pages]): refs[p] = table entries that name page p, 0 = free.
+ * The four calls below keep the three in step; the block table they are given is written.  Pages are
+ * handed out lowest first, so the result depends on the state alone.  Tables of several layers (folded
+ * into B) may share one pool and one refs.  num_pages < 2^30.
+ * Workspace: at least lagkv_pages_workspace_bytes() (0 = bad arguments), 256-byte aligned, cleared once
+ * with lagkv_pages_workspace_init(); lagkv_read_status() reads its status block.
+ */
+size_t lagkv_pages_workspace_bytes(lagkv_plan_t plan, int64_t num_pages);
+int lagkv_pages_workspace_init(lagkv_plan_t plan, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Give back the pages that lie wholly at or behind row keep_len[b] (DEVICE int32 [B]; 0 frees the
+ * sequence): their entries become -1 and refs go down by one each.  After lagkv_compress_append_paged()
+ * keep_len = seq_len frees what the pass has emptied.  keep_len[b] outside [0, max_blocks*page_size], an
+ * entry outside the pool, or a page that refs counts as free: recorded as LAGKV_EINVAL and left alone.
+ */
+int lagkv_pages_release(lagkv_plan_t plan, int32_t *block_table, int32_t max_blocks, int32_t page_size,
+                        int64_t num_pages, int32_t *refs, const int32_t *keep_len, void *workspace,
+                        size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Room for want_len[b] rows (DEVICE int32 [B]): every entry of the first ceil(want_len[b]/page_size) blocks
+ * that is negative gets a free page, in the order (sequence, block); pages already there stay, and
+ * so do those behind.  Too few free pages: LAGKV_ECAPACITY is recorded and nothing changes.  want_len[b]
+ * outside [0, max_blocks*page_size]: LAGKV_EINVAL is recorded, that sequence gets nothing.
+ */
+int lagkv_pages_reserve(lagkv_plan_t plan, int32_t *block_table, int32_t max_blocks, int32_t page_size,
+                        int64_t num_pages, int32_t *refs, const int32_t *want_len, void *workspace,
+                        size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Fork sequences: for i < n (at most B) sequence dst[i], which holds no pages, becomes a copy of sequence
+ * src[i] (DEVICE int32 [n] each), seq_len and static_len (DEVICE int32 [B]) included.  Pages wholly below
+ * min(seq_len, static_len) are shared: those rows are never rewritten, not by the compress pass, not by
+ * new rows, not by lagkv_tree_commit().  The others are copied to free pages, whole, in the order (i, block), so
+ * that both sequences may go on on their own.  (A cache that is never compressed: static_len = seq_len.)
+ * A pair is refused (LAGKV_EINVAL recorded, the others done) when an index is outside [0, B), dst[i] holds a
+ * page or is the target of an earlier pair, or a page that src[i]'s length needs is not a counted page
+ * of the pool.  Too few free pages: LAGKV_ECAPACITY is recorded and nothing changes.  Two launches.
+ */
+int lagkv_pages_fork(lagkv_plan_t plan, void *K_pool, void *V_pool, const lagkv_paged_layout *layout,
+                     int64_t num_pages, int32_t *refs, int32_t *seq_len, int32_t *static_len, const int32_t *src,
+                     const int32_t *dst, int32_t n, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Make the pool dense: with `live` pages in use, each one numbered live or higher moves, in ascending
+ * order, to the lowest free numbers; K, V, refs and the block table follow.  Afterwards the pages [live,
+ * num_pages) are free.  live_out: DEVICE int32 [1].  Every table that names pages of this pool has to be
+ * in the call.  An entry that names a page which refs does not count: recorded as LAGKV_EINVAL, left alone.
+ */
+int lagkv_pages_compact(lagkv_plan_t plan, void *K_pool, void *V_pool, const lagkv_paged_layout *layout,
+                        int64_t num_pages, int32_t *refs, int32_t *live_out, void *workspace, size_t workspace_bytes,
+                        void *cuda_stream);
+
+/*
  * Synchronise cuda_stream, copy the status block to the host and clear it.  workspace == NULL
  * names the status block of the library's built-in scratch on the plan's device (the one
  * lagkv_compress_append_noalloc() uses).

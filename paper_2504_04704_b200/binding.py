@@ -33,7 +33,8 @@ EXPORTS = (
     "lagkv_compress_append_paged", "lagkv_gather", "lagkv_gather_paged",
     "lagkv_attend_workspace_bytes", "lagkv_attend_workspace_init", "lagkv_attend_tree", "lagkv_attend_tree_paged",
     "lagkv_tree_commit", "lagkv_tree_commit_paged", "lagkv_block_bounds", "lagkv_block_bounds_paged",
-    "lagkv_attend_blocks", "lagkv_attend_blocks_paged",
+    "lagkv_attend_blocks", "lagkv_attend_blocks_paged", "lagkv_pages_workspace_bytes", "lagkv_pages_workspace_init",
+    "lagkv_pages_release", "lagkv_pages_reserve", "lagkv_pages_fork", "lagkv_pages_compact",
     "lagkv_read_status",
     "lagkv_launch_info", "lagkv_plan_tune", "lagkv_selftest_bounded_wait", "lagkv_status_string", "lagkv_version",
 )
@@ -150,6 +151,17 @@ def load_library() -> ctypes.CDLL:
     lib.lagkv_attend_blocks.argtypes = [vp, query, choice, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lagkv_attend_blocks_paged.restype = ctypes.c_int
     lib.lagkv_attend_blocks_paged.argtypes = [vp, query, choice, vp, vp, vp, layout, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_pages_workspace_bytes.restype = sz
+    lib.lagkv_pages_workspace_bytes.argtypes = [vp, i64]
+    lib.lagkv_pages_workspace_init.restype = ctypes.c_int
+    lib.lagkv_pages_workspace_init.argtypes = [vp, vp, sz, vp]
+    for name in ("lagkv_pages_release", "lagkv_pages_reserve"):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [vp, vp, i32, i32, i64, vp, vp, vp, sz, vp]
+    lib.lagkv_pages_fork.restype = ctypes.c_int
+    lib.lagkv_pages_fork.argtypes = [vp, vp, vp, layout, i64, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.lagkv_pages_compact.restype = ctypes.c_int
+    lib.lagkv_pages_compact.argtypes = [vp, vp, vp, layout, i64, vp, vp, vp, sz, vp]
     lib.lagkv_read_status.restype = ctypes.c_int
     lib.lagkv_read_status.argtypes = [vp, vp, vp, ctypes.POINTER(i32 * 4)]
     lib.lagkv_launch_info.restype = ctypes.c_int
@@ -635,6 +647,70 @@ class Plan:
             _stream(self._dev()))
         _check(rc, "lagkv_attend_blocks_paged")
         return got
+
+    # ---- pages
+    def new_pages_workspace(self, num_pages: int) -> torch.Tensor:
+        """Workspace of the ``pages_*`` calls on a pool of ``num_pages`` pages."""
+        nbytes = int(self.lib.lagkv_pages_workspace_bytes(self.handle, int(num_pages)))
+        if nbytes == 0:
+            raise LagKVError(LAGKV_EINVAL, "lagkv_pages_workspace_bytes")
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self._dev())
+        _check(self.lib.lagkv_pages_workspace_init(self.handle, _ptr(ws), ws.numel(), _stream(self._dev())),
+               "lagkv_pages_workspace_init")
+        return ws
+
+    def _check_table(self, block_table, refs, num_pages=None):
+        if block_table.dim() != 2:
+            raise TypeError("block_table must be [B, max_blocks]")
+        self._check_ints(block_table, "block_table", (self.cfg.B, block_table.shape[1]))
+        if refs.dim() != 1:
+            raise TypeError("refs must be [num_pages]")
+        self._check_ints(refs, "refs", (refs.shape[0] if num_pages is None else num_pages,))
+
+    def pages_release(self, block_table, refs, keep_len, workspace, page_size) -> None:
+        """``lagkv_pages_release``: pages wholly behind row ``keep_len[b]`` go back to the pool."""
+        self._check_table(block_table, refs)
+        self._check_ints(keep_len, "keep_len", (self.cfg.B,))
+        rc = self.lib.lagkv_pages_release(
+            self.handle, _ptr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _ptr(refs),
+            _ptr(keep_len), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_pages_release")
+
+    def pages_reserve(self, block_table, refs, want_len, workspace, page_size) -> None:
+        """``lagkv_pages_reserve``: free pages, lowest first, for the blocks below row ``want_len[b]`` that lack one."""
+        self._check_table(block_table, refs)
+        self._check_ints(want_len, "want_len", (self.cfg.B,))
+        rc = self.lib.lagkv_pages_reserve(
+            self.handle, _ptr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _ptr(refs),
+            _ptr(want_len), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_pages_reserve")
+
+    def pages_fork(self, K_pool, V_pool, block_table, refs, seq_len, static_len, src, dst, workspace, strides=None) -> None:
+        """``lagkv_pages_fork``: sequence ``dst[i]`` becomes a copy of ``src[i]``; pages below ``static_len`` are shared, the
+        others copied."""
+        lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, refs.shape[0])
+        self._check_table(block_table, refs, pages)
+        self._check_ints(seq_len, "seq_len", (self.cfg.B,))
+        self._check_ints(static_len, "static_len", (self.cfg.B,))
+        n = int(src.numel())
+        self._check_ints(src, "src", (n,))
+        self._check_ints(dst, "dst", (n,))
+        rc = self.lib.lagkv_pages_fork(
+            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(refs), _ptr(seq_len), _ptr(static_len),
+            _ptr(src), _ptr(dst), n, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_pages_fork")
+
+    def pages_compact(self, K_pool, V_pool, block_table, refs, workspace, strides=None, live_out=None) -> torch.Tensor:
+        """``lagkv_pages_compact``: the pages in use move to the lowest numbers; returns their count (int32 ``[1]``)."""
+        lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, refs.shape[0])
+        self._check_table(block_table, refs, pages)
+        live = torch.empty(1, dtype=torch.int32, device=refs.device) if live_out is None else live_out
+        self._check_ints(live, "live_out", (1,))
+        rc = self.lib.lagkv_pages_compact(
+            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(refs), _ptr(live), _ptr(workspace),
+            workspace.numel(), _stream(self._dev()))
+        _check(rc, "lagkv_pages_compact")
+        return live
 
 
 # ---- C-named thin functions ---------------------------------------------------------------
