@@ -13,7 +13,7 @@ using namespace lagkv;
 
 namespace {
 
-const AttendEntry* find_attend(int D, int dtype, int rows_wanted, int* index) {
+const AttendEntry* find_attend(int D, int dtype, int rows_wanted, bool blocks, int* index) {
     const AttendEntry* t;
     const int n = dtype == LAGKV_DTYPE_BF16   ? attend_bf16_kernels(&t)
                   : dtype == LAGKV_DTYPE_FP16 ? attend_fp16_kernels(&t)
@@ -21,7 +21,7 @@ const AttendEntry* find_attend(int D, int dtype, int rows_wanted, int* index) {
     // the smallest unit that holds all query rows, else the largest there is
     const AttendEntry* best = nullptr;
     for (int i = 0; i < n; ++i) {
-        if (t[i].D != D) continue;
+        if (t[i].D != D || (blocks && t[i].wide)) continue;
         const bool fits = t[i].rows >= rows_wanted, best_fits = best && best->rows >= rows_wanted;
         if (best == nullptr || (fits && (!best_fits || t[i].rows < best->rows)) || (!fits && !best_fits && t[i].rows > best->rows)) {
             best = t + i;
@@ -38,7 +38,7 @@ size_t counter_bytes(size_t workspace_bytes) { return ((workspace_bytes - kHead)
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
 size_t partial_bytes(const lagkv_plan_s* plan, const AttendEntry& e) {
-    return up256(size_t(plan->sm_count) * e.ctas_per_sm * 2 * e.rows * (plan->cfg.D + 2) * sizeof(float));
+    return up256(size_t(plan->sm_count) * e.ctas_per_sm * 2 * e.partial_words * sizeof(float));
 }
 long long attend_units(const lagkv_plan_s* plan, const AttendEntry& e, int query_rows, int tokens) {
     return (long long)plan->cfg.B * plan->cfg.H_kv * tokens * ((query_rows + e.rows - 1) / e.rows);
@@ -121,10 +121,10 @@ int workspace_ok(const void* workspace, size_t bytes, size_t need) {
 
 // Picks the kernel, finds room in the workspace and launches.  `extra`: bytes of the workspace behind
 // the partials that the call uses itself.
-int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, size_t extra, void* workspace, size_t bytes,
+int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, size_t extra, void* workspace, size_t bytes,
                    AttendParams* P, const AttendEntry** entry, unsigned char** rest) {
     int index = 0;
-    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, query_rows, &index);
+    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, query_rows, blocks, &index);
     if (e == nullptr) return LAGKV_EUNSUPPORTED;
     const long long units = attend_units(plan, *e, query_rows, tokens);
     int rc = workspace_ok(workspace, bytes, kHead + 4096);
@@ -169,7 +169,7 @@ int attend_tree(lagkv_plan_t plan, const lagkv_query* query, const void* Q, cons
     DeviceGuard guard(plan->cfg.device);
     const AttendEntry* e;
     unsigned char* rest;
-    rc = attend_prepare(plan, P.T * P.G, 1, 0, workspace, bytes, &P, &e, &rest);
+    rc = attend_prepare(plan, P.T * P.G, 1, false, 0, workspace, bytes, &P, &e, &rest);
     if (rc != LAGKV_OK) return rc;
     return attend_launch(plan, *e, P, static_cast<cudaStream_t>(cuda_stream));
 }
@@ -265,7 +265,7 @@ int attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block
     DeviceGuard guard(c.device);
     const AttendEntry* e;
     unsigned char* rest;
-    rc = attend_prepare(plan, P.G, P.T, choice_bytes(c, P.T, choice->blocks, choice->keep), workspace, bytes, &P, &e, &rest);
+    rc = attend_prepare(plan, P.G, P.T, true, choice_bytes(c, P.T, choice->blocks, choice->keep), workspace, bytes, &P, &e, &rest);
     if (rc != LAGKV_OK) return rc;
     int32_t* idx = idx_out ? idx_out : reinterpret_cast<int32_t*>(rest);
     unsigned long long* keys = reinterpret_cast<unsigned long long*>(rest + up256(size_t(units) * P.keep * sizeof(int32_t)));
@@ -304,10 +304,11 @@ size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, i
     const int G = H_q / plan->cfg.H_kv;
     // every smaller call of either kind: one token per unit with few query rows, all rows in one unit
     size_t partials = 0, units = 0;
-    for (int rows = 1; rows <= T * G; rows = rows < 128 ? rows * 2 : T * G + 1) {
-        for (int r : {rows, T * G, G}) {
+    for (int rows : {1, 17, 33, 129, T * G}) {
+        if (rows > T * G) continue;
+        for (bool chosen : {false, true}) {
             int index;
-            const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, r, &index);
+            const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows, chosen, &index);
             if (e == nullptr) return 0;
             if (partial_bytes(plan, *e) > partials) partials = partial_bytes(plan, *e);
         }

@@ -42,7 +42,7 @@ struct AttendParams {
     int keep, block_shift;
 };
 
-constexpr int kAttendTile = 64;     // rows of the unit of scheduling
+constexpr int kAttendTile = 64;     // rows of the unit of scheduling (lagkv_attend_kernel)
 constexpr int kAttendWarps = 4;
 constexpr int kWarpRows = 16;       // rows of a warp's tile: never across a page or a block (both >= 16)
 
@@ -150,8 +150,9 @@ struct AttendGeo {
 struct AttendSeq {
     int len;     // rows below seq_len (0 where the lengths do not describe the cache)
     int tokens;  // drafted tokens (rows len - tokens .. len - 1)
-    int tiles;   // 64-row tiles of each of its units
+    int tiles;   // TILE-row tiles of each of its units
 };
+template <int TILE = kAttendTile>
 __device__ __forceinline__ AttendSeq attend_seq(const AttendParams& P, int b, bool report) {
     AttendSeq s;
     s.len = __ldg(P.seq_len + b);
@@ -166,7 +167,7 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendParams& P, int b, bo
         rows = min(nblk, P.keep) << P.block_shift;
     }
     if (s.tokens == 0) rows = 0;
-    s.tiles = max(1, (rows + kAttendTile - 1) / kAttendTile);  // a unit without rows still writes its zeros
+    s.tiles = max(1, (rows + TILE - 1) / TILE);  // a unit without rows still writes its zeros
     return s;
 }
 
@@ -176,14 +177,14 @@ struct AttendShare {
     long long pos, end, first, per_cta;
     int b;
 };
-template <int NT>
+template <int NT, int TILE = kAttendTile>
 __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int units_per_seq, long long* scan) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     constexpr int NW = NT / 32;
     long long total = 0;
     for (int b0 = 0; b0 < P.B; b0 += NT) {
         const int b = b0 + tid;
-        total += b < P.B ? (long long)attend_seq(P, b, blockIdx.x == 0).tiles * units_per_seq : 0;
+        total += b < P.B ? (long long)attend_seq<TILE>(P, b, blockIdx.x == 0).tiles * units_per_seq : 0;
     }
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
     if (lane == 0) scan[w] = total;
@@ -205,7 +206,7 @@ __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int u
     for (int b0 = 0; b0 < P.B; b0 += NT) {
         __syncthreads();
         const int b = b0 + tid;
-        const long long n = b < P.B ? (long long)attend_seq(P, b, false).tiles * units_per_seq : 0;
+        const long long n = b < P.B ? (long long)attend_seq<TILE>(P, b, false).tiles * units_per_seq : 0;
         long long inc = n;
         for (int o = 1; o < 32; o <<= 1) {
             const long long v = __shfl_up_sync(~0u, inc, o);
@@ -241,19 +242,46 @@ __device__ __forceinline__ long long attend_offset(const AttendParams& P, int b,
 }
 
 // Where a unit's result goes: finished (out, lse) or as a partial (reference, sum, accumulators).
-template <class G>
-__device__ __forceinline__ void attend_write(const AttendParams& P, int b, int h, int t0, int m0, int rows, int tokens,
-                                             int m, int d, const float (&o)[4], float ref, float sum) {
+template <int D, int DT>
+__device__ __forceinline__ void attend_write(const AttendParams& P, int b, int h, int t0, int m0, int tokens, int m, int d,
+                                             const float (&o)[4], float ref, float sum) {
     // four channels d .. d + 3 of query row m
     const int row = m0 + m, t = t0 + row / P.G, g = row % P.G;
     const long long at = (((long long)b * P.T + t) * P.H + h) * P.G + g;
     const bool live = t < tokens && sum != 0.f;  // NaN sums stay: they compare unequal to 0
     const float inv = live ? P.v_scale / sum : 0.f;
     uint2 v;
-    v.x = live ? pack_out<G::DT>(o[0] * inv, o[1] * inv) : 0u;
-    v.y = live ? pack_out<G::DT>(o[2] * inv, o[3] * inv) : 0u;
-    *reinterpret_cast<uint2*>(P.out + at * G::D + d) = v;
+    v.x = live ? pack_out<DT>(o[0] * inv, o[1] * inv) : 0u;
+    v.y = live ? pack_out<DT>(o[2] * inv, o[3] * inv) : 0u;
+    *reinterpret_cast<uint2*>(P.out + at * D + d) = v;
     if (d == 0 && P.lse) P.lse[at] = live ? 0.69314718055994531f * (ref + log2f(sum)) : -INFINITY;
+}
+
+// A shared unit's result from the partials of CTAs c0 .. c1, in that order, by `threads` threads.  A CTA's
+// partials: [2 slots][psize], slot 1 for the unit that starts in its share, slot 0 for the one that it
+// continues; `part` is where the MR rows lie in a slot.
+template <int D, int DT, int MR>
+__device__ __forceinline__ void attend_combine(const AttendParams& P, int b, int h, int t0, int m0, int mrows, int tokens,
+                                               long long c0, long long c1, int psize, int part, int tid, int threads) {
+    for (int i = tid; i < mrows * (D / 4); i += threads) {
+        const int m = i / (D / 4), d = (i % (D / 4)) * 4;
+        float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (long long c = c0; c <= c1; ++c) {
+            const float* pp = P.partials + (2 * c + (c == c0 ? 1 : 0)) * psize + part;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp + MR * D + 2 * m));
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;
+            const float r = fmaxf(top, ml.x);
+            const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml.x - r);
+            total = total * fo + ml.y * fn;
+            o[0] = o[0] * fo + v.x * fn;
+            o[1] = o[1] * fo + v.y * fn;
+            o[2] = o[2] * fo + v.z * fn;
+            o[3] = o[3] * fo + v.w * fn;
+            top = r;
+        }
+        attend_write<D, DT>(P, b, h, t0, m0, tokens, m, d, o, top, total);
+    }
 }
 
 template <int D, int DT, int MT>
@@ -626,7 +654,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
                 o[3] += v.w * f;
             }
             if (c0 == c1) {
-                attend_write<G>(P, sh.b, h, t0, m0, mrows, seq.tokens, m, d, o, top, total);
+                attend_write<D, DT>(P, sh.b, h, t0, m0, seq.tokens, m, d, o, top, total);
             } else {
                 __stcg(reinterpret_cast<float4*>(part + m * D + d), make_float4(o[0], o[1], o[2], o[3]));
                 if (d == 0) __stcg(reinterpret_cast<float2*>(part + G::MR * D + 2 * m), make_float2(top, total));
@@ -644,25 +672,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
             __syncthreads();
             if (*slast) {
                 __threadfence();
-                for (int i = tid; i < mrows * (D / 4); i += G::NT) {
-                    const int m = i / (D / 4), d = (i % (D / 4)) * 4;
-                    float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (long long c = c0; c <= c1; ++c) {
-                        const float* pp = P.partials + (2 * c + (c == c0 ? 1 : 0)) * PSIZE;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp + G::MR * D + 2 * m));
-                        const float4 v = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
-                        const float r = fmaxf(top, ml.x);
-                        if (ml.x == -INFINITY && ml.y == 0.f) continue;
-                        const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml.x - r);
-                        total = total * fo + ml.y * fn;
-                        o[0] = o[0] * fo + v.x * fn;
-                        o[1] = o[1] * fo + v.y * fn;
-                        o[2] = o[2] * fo + v.z * fn;
-                        o[3] = o[3] * fo + v.w * fn;
-                        top = r;
-                    }
-                    attend_write<G>(P, sh.b, h, t0, m0, mrows, seq.tokens, m, d, o, top, total);
-                }
+                attend_combine<D, DT, G::MR>(P, sh.b, h, t0, m0, mrows, seq.tokens, c0, c1, PSIZE, 0, tid, G::NT);
             }
         }
         sh.pos += ntile;

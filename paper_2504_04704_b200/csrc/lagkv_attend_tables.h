@@ -1,6 +1,7 @@
 // Table of the compiled attention kernels (one translation unit per storage format).
 #pragma once
 #include "lagkv_attend_kernels.cuh"
+#include "lagkv_attend_wide_kernel.cuh"
 
 namespace lagkv {
 
@@ -9,6 +10,8 @@ typedef void (*attend_kernel_t)(const AttendParams);
 struct AttendEntry {
     int D, dtype;
     int rows;     // query rows of a unit
+    bool wide;    // tensor memory kernel: whole sequences only, no block choice
+    size_t partial_words;  // floats of one partial result
     int threads, ctas_per_sm;
     size_t smem;
     attend_kernel_t fn;
@@ -20,11 +23,16 @@ int attend_fp16_kernels(const AttendEntry** table);
 int attend_fp8_kernels(const AttendEntry** table);
 
 #define LAGKV_ATTEND_ENTRY(D, DT, MT) \
-    { D, DT, AttendGeo<D, DT, MT>::MR, AttendGeo<D, DT, MT>::NT, AttendGeo<D, DT, MT>::CTAS, \
+    { D, DT, AttendGeo<D, DT, MT>::MR, false, size_t(AttendGeo<D, DT, MT>::MR) * (D + 2), AttendGeo<D, DT, MT>::NT, \
+      AttendGeo<D, DT, MT>::CTAS, \
       size_t(AttendGeo<D, DT, MT>::SMEM), &lagkv_attend_kernel<D, DT, MT> }
+#define LAGKV_WIDE_ENTRY(D, DT, MT) \
+    { D, DT, MT * kWideTile, true, size_t(WideGeo<D, DT, MT>::PSIZE), kWideThreads, 1, \
+      size_t(WideGeo<D, DT, MT>::SMEM), &lagkv_attend_wide_kernel<D, DT, MT> }
 #define LAGKV_ATTEND_ENTRIES(DT) \
     LAGKV_ATTEND_ENTRY(64, DT, 1), LAGKV_ATTEND_ENTRY(96, DT, 1), LAGKV_ATTEND_ENTRY(128, DT, 1), \
     LAGKV_ATTEND_ENTRY(256, DT, 1), LAGKV_ATTEND_ENTRY(64, DT, 2), LAGKV_ATTEND_ENTRY(96, DT, 2), \
-    LAGKV_ATTEND_ENTRY(128, DT, 2)
+    LAGKV_ATTEND_ENTRY(128, DT, 2), LAGKV_WIDE_ENTRY(64, DT, 1), LAGKV_WIDE_ENTRY(96, DT, 1), LAGKV_WIDE_ENTRY(128, DT, 1), \
+    LAGKV_WIDE_ENTRY(64, DT, 2), LAGKV_WIDE_ENTRY(96, DT, 2), LAGKV_WIDE_ENTRY(128, DT, 2)
 
 }  // namespace lagkv
