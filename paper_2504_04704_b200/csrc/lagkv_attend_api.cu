@@ -3,6 +3,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <cuda.h>
 
 #include "lagkv_attend_tables.h"
 #include "lagkv_block_kernels.cuh"
@@ -129,26 +130,71 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     const long long units = attend_units(plan, *e, query_rows, tokens);
     int rc = workspace_ok(workspace, bytes, kHead + 4096);
     if (rc != LAGKV_OK) return rc;
-    const size_t cb = counter_bytes(bytes), pb = partial_bytes(plan, *e);
+    // a narrow kernel's CTAs count arrivals per unit; a wide one's say who shares a unit
+    const size_t cb = counter_bytes(bytes), pb = partial_bytes(plan, *e) + (e->wide ? up256(size_t(units) * sizeof(int2)) : 0);
+    if (units * (e->rows / 16) > 0x7fffffffll) return LAGKV_EINVAL;
     if (size_t(units) * sizeof(int32_t) > cb || kHead + cb + pb + extra > bytes) return LAGKV_EWORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(workspace);
     P->status = reinterpret_cast<int32_t*>(base);
     P->counters = reinterpret_cast<int32_t*>(base + kHead);
     P->partials = reinterpret_cast<float*>(base + kHead + cb);
+    P->shared = reinterpret_cast<int2*>(base + kHead + cb + partial_bytes(plan, *e));
     P->mtiles = (query_rows + e->rows - 1) / e->rows;
     *entry = e;
     *rest = base + kHead + cb + pb;
     if (!(plan->attend_ready.load(std::memory_order_acquire) >> index & 1)) {
-        if (!raise_smem_limit(reinterpret_cast<const void*>(e->fn), e->smem)) return LAGKV_ECUDA;
+        if (!raise_smem_limit(e->fn, e->smem)) return LAGKV_ECUDA;
         plan->attend_ready.fetch_or(1ull << index, std::memory_order_release);
     }
     return LAGKV_OK;
 }
+typedef CUresult (*encode_tiled_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+encode_tiled_t encode_tiled() {
+    static const encode_tiled_t fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<encode_tiled_t>(p);
+    }();
+    return fn;
+}
+// Tensor map of one cache tensor for the wide kernel: (channels, rows, heads, sequences or pages), boxes of
+// 64 channels in 128-byte swizzled rows (fp8: whole rows as they are) and of a tile's rows, or a page's if fewer.
+int cache_map(const lagkv_config& c, const AttendParams& P, const uint8_t* base, CUtensorMap* map) {
+    const bool fp8 = c.dtype == LAGKV_DTYPE_FP8_E4M3, paged = P.block_table != nullptr;
+    const cuuint64_t rows = paged ? 1ull << P.page_shift : (cuuint64_t)P.S_cap;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.D, rows, (cuuint64_t)c.H_kv, paged ? (cuuint64_t)P.num_pages : (cuuint64_t)c.B};
+    const cuuint64_t strides[3] = {(cuuint64_t)P.ss, (cuuint64_t)P.sh, (cuuint64_t)(paged ? P.page_stride : P.sb)};
+    const cuuint32_t box[4] = {fp8 ? (cuuint32_t)c.D : 64u, (cuuint32_t)(paged && rows < kWideTile ? rows : kWideTile), 1u, 1u};
+    const cuuint32_t ones[4] = {1u, 1u, 1u, 1u};
+    const CUtensorMapDataType type = fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const encode_tiled_t encode = encode_tiled();
+    if (encode == nullptr) return LAGKV_ECUDA;
+    const CUresult r = encode(map, type, 4, const_cast<uint8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? LAGKV_OK : LAGKV_EUNSUPPORTED;  // strides of 2^40 bytes and more
+}
+
 int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cudaStream_t stream) {
-    void* args[] = {&P};
-    if (cudaLaunchKernel(reinterpret_cast<const void*>(e.fn), dim3((unsigned)(plan->sm_count * e.ctas_per_sm)),
-                         dim3(e.threads), args, e.smem, stream) != cudaSuccess)
+    CUtensorMap map_k, map_v;
+    if (e.wide) {
+        int rc = cache_map(plan->cfg, P, P.K, &map_k);
+        if (rc == LAGKV_OK) rc = cache_map(plan->cfg, P, P.V, &map_v);
+        if (rc != LAGKV_OK) return rc;
+    }
+    void* args[] = {&P, &map_k, &map_v};
+    if (cudaLaunchKernel(e.fn, dim3((unsigned)(plan->sm_count * e.ctas_per_sm)), dim3(e.threads), args, e.smem, stream) !=
+        cudaSuccess)
         return LAGKV_ECUDA;
+    if (e.join != nullptr) {
+        const long long ctas = (long long)P.B * P.H * P.mtiles * (e.rows / kJoinRows);
+        if (cudaLaunchKernel(e.join, dim3((unsigned)ctas), dim3(kJoinThreads), args, 0, stream) != cudaSuccess) return LAGKV_ECUDA;
+    }
     return check_launch();
 }
 
@@ -310,7 +356,8 @@ size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, i
             int index;
             const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows, chosen, &index);
             if (e == nullptr) return 0;
-            if (partial_bytes(plan, *e) > partials) partials = partial_bytes(plan, *e);
+            const size_t need = partial_bytes(plan, *e) + (e->wide ? up256(size_t(attend_units(plan, *e, T * G, 1)) * sizeof(int2)) : 0);
+            if (need > partials) partials = need;
         }
     }
     const size_t most = size_t(T) * ((G + 15) / 16);  // units per (sequence, KV head): no unit has fewer than 16 rows

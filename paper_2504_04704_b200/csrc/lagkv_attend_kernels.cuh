@@ -31,6 +31,7 @@ struct AttendParams {
     int32_t* status;
     int32_t* counters;     // [units], zero between calls
     float* partials;       // [grid * 2][MR * (D + 2)]
+    int2* shared;          // wide kernel: first and last CTA of each unit
     long long sb, sh, ss, page_stride;  // bytes
     const int32_t* block_table;
     long long num_pages;
@@ -258,16 +259,16 @@ __device__ __forceinline__ void attend_write(const AttendParams& P, int b, int h
 }
 
 // A shared unit's result from the partials of CTAs c0 .. c1, in that order, by `threads` threads.  A CTA's
-// partials: [2 slots][psize], slot 1 for the unit that starts in its share, slot 0 for the one that it
-// continues; `part` is where the MR rows lie in a slot.
+// partials: [2 slots][MR * (D + 2)], slot 1 for the unit that starts in its share, slot 0 for the one that
+// it continues.
 template <int D, int DT, int MR>
 __device__ __forceinline__ void attend_combine(const AttendParams& P, int b, int h, int t0, int m0, int mrows, int tokens,
-                                               long long c0, long long c1, int psize, int part, int tid, int threads) {
+                                               long long c0, long long c1, int tid, int threads) {
     for (int i = tid; i < mrows * (D / 4); i += threads) {
         const int m = i / (D / 4), d = (i % (D / 4)) * 4;
         float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
         for (long long c = c0; c <= c1; ++c) {
-            const float* pp = P.partials + (2 * c + (c == c0 ? 1 : 0)) * psize + part;
+            const float* pp = P.partials + (2 * c + (c == c0 ? 1 : 0)) * (MR * (D + 2));
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp + MR * D + 2 * m));
             const float4 v = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
             if (ml.x == -INFINITY && ml.y == 0.f) continue;
@@ -672,7 +673,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
             __syncthreads();
             if (*slast) {
                 __threadfence();
-                attend_combine<D, DT, G::MR>(P, sh.b, h, t0, m0, mrows, seq.tokens, c0, c1, PSIZE, 0, tid, G::NT);
+                attend_combine<D, DT, G::MR>(P, sh.b, h, t0, m0, mrows, seq.tokens, c0, c1, tid, G::NT);
             }
         }
         sh.pos += ntile;

@@ -5,8 +5,6 @@
 
 namespace lagkv {
 
-typedef void (*attend_kernel_t)(const AttendParams);
-
 struct AttendEntry {
     int D, dtype;
     int rows;     // query rows of a unit
@@ -14,7 +12,8 @@ struct AttendEntry {
     size_t partial_words;  // floats of one partial result
     int threads, ctas_per_sm;
     size_t smem;
-    attend_kernel_t fn;
+    const void* fn;
+    const void* join;  // wide: launched behind it, for the units that several CTAs share
 };
 
 // each returns the number of entries and sets *table
@@ -25,10 +24,11 @@ int attend_fp8_kernels(const AttendEntry** table);
 #define LAGKV_ATTEND_ENTRY(D, DT, MT) \
     { D, DT, AttendGeo<D, DT, MT>::MR, false, size_t(AttendGeo<D, DT, MT>::MR) * (D + 2), AttendGeo<D, DT, MT>::NT, \
       AttendGeo<D, DT, MT>::CTAS, \
-      size_t(AttendGeo<D, DT, MT>::SMEM), &lagkv_attend_kernel<D, DT, MT> }
+      size_t(AttendGeo<D, DT, MT>::SMEM), reinterpret_cast<const void*>(&lagkv_attend_kernel<D, DT, MT>), nullptr }
 #define LAGKV_WIDE_ENTRY(D, DT, MT) \
-    { D, DT, MT * kWideTile, true, size_t(WideGeo<D, DT, MT>::PSIZE), kWideThreads, 1, \
-      size_t(WideGeo<D, DT, MT>::SMEM), &lagkv_attend_wide_kernel<D, DT, MT> }
+    { D, DT, MT * kWideTile, true, size_t(WideGeo<D, DT, MT>::PSIZE), WideGeo<D, DT, MT>::NT, 1, \
+      size_t(WideGeo<D, DT, MT>::SMEM), reinterpret_cast<const void*>(&lagkv_attend_wide_kernel<D, DT, MT>), \
+      reinterpret_cast<const void*>(&lagkv_attend_join_kernel<D, DT, MT>) }
 #define LAGKV_ATTEND_ENTRIES(DT) \
     LAGKV_ATTEND_ENTRY(64, DT, 1), LAGKV_ATTEND_ENTRY(96, DT, 1), LAGKV_ATTEND_ENTRY(128, DT, 1), \
     LAGKV_ATTEND_ENTRY(256, DT, 1), LAGKV_ATTEND_ENTRY(64, DT, 2), LAGKV_ATTEND_ENTRY(96, DT, 2), \

@@ -7,19 +7,24 @@
 // Two streams keep the tensor cores busy while the other one's softmax runs: with up to 128 query rows the
 // streams take every other tile of rows and are joined at the end, with up to 256 each has its own 128
 // query rows and both read the same tiles.
-// Warps: 0-3 and 4-7 the softmax of stream 0 and 1 (a thread owns a query row), 8-11 fetch K and V tiles
-// into swizzled shared memory (cp.async: rows are found page by page and rows behind the last one are
-// zero-filled, which a tensor map cannot do; fp8 rows are widened to fp16 on the way), 12 issues.
+// Warps: 0-3 and 4-7 the softmax of stream 0 and 1 (a thread owns a query row); 8 issues the products; the
+// others fetch: the first of them by TMA into swizzled shared memory, a box per page and 64 channels (issuing
+// the same tiles as cp.async cost three warps 10000 cycles a step, five times what the products take), all of
+// them to mend V tiles -- rows behind the last one and hidden rows that are not finite become zeros, so that
+// 0 * inf never happens -- and to widen fp8 tiles, which land as they are, to fp16.
+// Partials of shared units (66 KB for 128 query rows) are joined by a kernel of their own: one CTA adding
+// up 18 of them took longer than the attention.
 // Bound: at 128 rows and 16-bit caches by HBM, at 256 by the 16384 exponentials per tile and stream (16 a
 // cycle and SM: as long as the products themselves).
 #pragma once
+#include <cuda.h>
+
 #include "lagkv_attend_kernels.cuh"
 
 namespace lagkv {
 
 constexpr int kWideTile = 128;        // rows of K and V per step
-constexpr int kWideThreads = 13 * 32;
-constexpr int kWideLag = 2;           // tiles whose copies are in flight behind the one being issued
+constexpr int kWideRowFlags = 32;     // loads whose missing rows are remembered: more than the rings hold
 
 template <int D_, int DT_, int MT_>
 struct WideGeo {
@@ -31,12 +36,17 @@ struct WideGeo {
     static constexpr int SLOT = PANELS * PANEL;
     static constexpr int EXCH = 64 * kWideTile * 4;    // MT = 1: 64 channels of one stream's O for the other
     static constexpr int QBYTES = MT == 2 ? 2 * SLOT : SLOT + EXCH;
+    static constexpr int WARPS = DT_ == 2 ? 16 : 12;   // widening takes seven warps to keep up
+    static constexpr int NT = WARPS * 32, FETCH = NT - 9 * 32;
     static constexpr int MISC = 1024;
-    static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES) / SLOT;
-    static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT; // tiles of K or V in the ring
-    static constexpr int SMEM = 1024 + QBYTES + NS * SLOT + MISC;
+    static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
+    static constexpr int RS = DT_ == 2 ? 4 : 0;                  // ... and how many are in flight
+    static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
+    static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
+    static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
+    static constexpr int SMEM = 1024 + QBYTES + NS * SLOT + RS * RAW + MISC;
     static constexpr int PSIZE = MT * kWideTile * (D + 2);
-    static_assert(NS >= 5, "the order of the ring needs five tiles");
+    static_assert(NS >= 3, "a released tile may need the two behind it");
     static_assert(D <= 128 && D % 32 == 0, "tensor memory: 2 x 128 columns of S, 2 x D of O");
 };
 
@@ -160,28 +170,66 @@ __device__ __forceinline__ void wide_next(AttendShare& sh, const WideUnit& w, in
     }
 }
 
+// A walk over the loads of a CTA's share, in order.
+template <class G>
+struct WideCursor {
+    AttendShare sh;
+    WideUnit U;
+    int l;       // load of the unit
+    uint32_t c;  // loads before this one
+    bool more;
+    __device__ __forceinline__ void start(const AttendParams& P, const AttendShare& s) {
+        sh = s;
+        l = 0;
+        c = 0;
+        more = sh.pos < sh.end;
+        if (more) U = wide_unit<G>(P, sh);
+    }
+    __device__ __forceinline__ void next(const AttendParams& P, int units_per_seq) {
+        ++c;
+        if (++l == 2 * U.n) {
+            l = 0;
+            wide_next(sh, U, units_per_seq);
+            more = sh.pos < sh.end;
+            if (more) U = wide_unit<G>(P, sh);
+        }
+    }
+    __device__ __forceinline__ bool is_v() const {
+        return G::MT == 2 ? (l & 1) != 0 : l == 2 * U.n - 1 || (l >= 2 && !(l & 1));
+    }
+    __device__ __forceinline__ int row0() const {  // first row of the tile
+        const int i = G::MT == 2 ? l >> 1 : is_v() ? (l == 2 * U.n - 1 ? U.n - 1 : l / 2 - 1) : (l + 1) >> 1;
+        return (U.tile0 + i) * kWideTile;
+    }
+    // drafted V rows that are not finite are kept out of the tile
+    __device__ __forceinline__ bool careful() const { return U.masked && is_v() && row0() + kWideTile > U.base; }
+};
+
 template <int D, int DT, int MT>
-__global__ void __launch_bounds__(kWideThreads, 1)
-lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
+__global__ void __launch_bounds__(WideGeo<D, DT, MT>::NT, 1)
+lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v) {
     using G = WideGeo<D, DT, MT>;
     using X = Mma<DT>;
     extern __shared__ unsigned char raw[];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t sbase = (smem_u32(raw) + 1023u) & ~1023u;
     unsigned char* smem = raw + (sbase - smem_u32(raw));
-    const uint32_t s_q = sbase, s_ring = sbase + G::QBYTES, s_misc = s_ring + G::NS * G::SLOT;
-    unsigned char* misc = smem + G::QBYTES + G::NS * G::SLOT;
+    const uint32_t s_q = sbase, s_ring = sbase + G::QBYTES, s_raw = s_ring + G::NS * G::SLOT, s_misc = s_raw + G::RS * G::RAW;
+    unsigned char* misc = smem + (s_misc - sbase);
     float* exch = reinterpret_cast<float*>(smem + G::SLOT);  // MT = 1
-    // misc: barriers, the rows of each V tile that are not finite, scheduling scratch
-    const uint32_t b_full = s_misc, b_empty = s_misc + 8 * 8, b_s = s_misc + 16 * 8, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16;
-    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 256);  // [8][4]
-    long long* scan = reinterpret_cast<long long*>(misc + 512);    // [13 + 2]
-    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 640);
-    int* slast = reinterpret_cast<int*>(misc + 644);
+    // misc: barriers, the rows of each V tile that are not finite, the missing 16-row groups of K tiles,
+    // scheduling scratch
+    const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_raw = b_empty + 8 * 8, b_s = b_raw + 4 * 8, b_p = b_s + 16, b_o = b_p + 16,
+                   b_q = b_o + 16, b_mend = b_q + 8;
+    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 256);                     // [8][4]
+    volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 384);       // [kWideRowFlags]
+    long long* scan = reinterpret_cast<long long*>(misc + 512);                       // [16 + 2]
+    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 704);
 
     if (tid == 0) {
         for (int i = 0; i < G::NS; ++i) {
-            mbar_init(b_full + 8 * i, 4);
+            mbar_init(b_full + 8 * i, 1);
             mbar_init(b_empty + 8 * i, 1);
         }
         for (int s = 0; s < 2; ++s) {
@@ -189,16 +237,18 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
             mbar_init(b_p + 8 * s, 4);
             mbar_init(b_o + 8 * s, 1);
         }
+        for (int i = 0; i < G::RS; ++i) mbar_init(b_raw + 8 * i, 1);
         mbar_init(b_q, 8);
+        mbar_init(b_mend, 1);
         fence_mbar_init();
     }
-    if (w == 12) {
+    if (w == 8) {
         __syncwarp();
         tm_alloc(smem_u32(tm_slot));
         tm_fence_before();
     }
     const int upb = P.H * P.mtiles;
-    AttendShare sh = attend_share<kWideThreads, kWideTile>(P, upb, scan);
+    AttendShare sh = attend_share<G::NT, kWideTile>(P, upb, scan);
     __syncthreads();
     tm_fence_after();
     const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(tm_slot);
@@ -206,124 +256,159 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
     constexpr int kO = 256;
     bool ok = true;
 
-    if (w >= 8 && w < 12) {
+    if (w > 8) {
         // ------------------------------------------------------------------ K and V tiles
-        const int ptid = tid - 256;
-        uint32_t c = 0;  // loads so far
-        auto signal = [&](uint32_t k) {
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_full + 8 * (k % G::NS));
+        const int ptid = tid - 9 * 32;
+        const bool issuer = w == 9;
+        uint32_t mended = 0;
+        // after a wait that ran out the walk goes on to its end without waiting or copying, so that the barrier
+        // among these warps still matches
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            if (ok && !mbar_wait_bounded(bar, parity)) {
+                if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+                ok = false;
+            }
+            return ok;
         };
-        for (; ok && sh.pos < sh.end;) {
-            const WideUnit U = wide_unit<G>(P, sh);
-            for (int l = 0; ok && l < 2 * U.n; ++l, ++c) {
-                // which tile is load l
-                int i;
-                bool is_v;
-                if (MT == 2) {
-                    i = l >> 1;
-                    is_v = l & 1;
-                } else {
-                    is_v = l == 2 * U.n - 1 || (l >= 2 && !(l & 1));
-                    i = is_v ? (l == 2 * U.n - 1 ? U.n - 1 : l / 2 - 1) : (l + 1) >> 1;
-                }
-                const int slot = int(c % G::NS), r0 = (U.tile0 + i) * kWideTile;
-                if (c >= uint32_t(G::NS) && !mbar_wait_bounded(b_empty + 8 * slot, (c / G::NS + 1) & 1)) {
-                    if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
-                    ok = false;
-                    break;
-                }
-                const uint8_t* T = is_v ? P.V : P.K;
-                // lanes 0-7: offsets of the tile's eight groups of 16 rows
-                long long off = -1;
-                if (lane < 8 && r0 + 16 * lane < U.lim) off = attend_offset(P, sh.b, U.h, r0 + 16 * lane);
-                const uint32_t dst = s_ring + slot * G::SLOT;
-                const bool careful = is_v && U.masked && r0 + kWideTile > U.base;
-                if (careful) {
-                    if (ptid < 4) odd_rows[slot * 4 + ptid] = 0u;
-                    asm volatile("bar.sync 2, 128;" ::: "memory");
-                }
-                if constexpr (DT != 2) {
-                    if (!careful) {
-#pragma unroll
-                        for (int j = 0; j < kWideTile * G::CPR / 128; ++j) {
-                            const int id = j * 128 + ptid, r = id / G::CPR, ch = id % G::CPR;
-                            const long long o = __shfl_sync(~0u, off, r >> 4);
-                            const bool there = o >= 0 && r0 + r < U.lim;
-                            cp_async16(dst + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
-                                       T + (there ? o + (long long)(r & 15) * P.ss + ch * 16 : 0), there);
-                        }
-                    }
-                }
-                if (DT == 2 || careful) {
-                    // through registers: fp8 rows widen to fp16; of a drafted V tile the rows that are not
-                    // finite are noted and enter as zeros
-                    constexpr int N = kWideTile * G::CPR / 128;
-                    uint4 v[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const int id = j * 128 + ptid, r = id / G::CPR, ch = id % G::CPR;
-                        const long long o = __shfl_sync(~0u, off, r >> 4);
-                        const bool there = o >= 0 && r0 + r < U.lim;
-                        v[j] = there ? __ldg(reinterpret_cast<const uint4*>(T + o + (long long)(r & 15) * P.ss + ch * 16)) : make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    if (careful) {
-#pragma unroll
-                        for (int j = 0; j < N; ++j) {
-                            const int r = (j * 128 + ptid) / G::CPR;
-                            const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-                            bool odd = false;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if (DT == 0) odd |= (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
-                                if (DT == 1) odd |= (x[k] & 0x7c00u) == 0x7c00u || (x[k] & 0x7c000000u) == 0x7c000000u;
-                                if (DT == 2)
-                                    for (int e = 0; e < 4; ++e) odd |= ((x[k] >> (8 * e)) & 0x7f) == 0x7f;
-                            }
-                            if (odd && r0 + r >= U.base) atomicOr(&odd_rows[slot * 4 + (r >> 5)], 1u << (r & 31));
-                        }
-                        asm volatile("bar.sync 2, 128;" ::: "memory");
-                    }
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const int id = j * 128 + ptid, r = id / G::CPR, ch = id % G::CPR;
-                        uint4 x = v[j];
-                        if (careful && (odd_rows[slot * 4 + (r >> 5)] >> (r & 31) & 1)) x = make_uint4(0u, 0u, 0u, 0u);
-                        unsigned char* to = smem + (dst - sbase) + r * 128;
-                        if constexpr (DT != 2) {
-                            *reinterpret_cast<uint4*>(to + (ch >> 3) * G::PANEL + (((ch & 7) ^ (r & 7)) << 4)) = x;
-                        } else {
-                            uint32_t a[2], b[2], e[2], f[2];
-                            Elem<2>::expand(x.x, a);
-                            Elem<2>::expand(x.y, b);
-                            Elem<2>::expand(x.z, e);
-                            Elem<2>::expand(x.w, f);
-                            const int c0 = ch * 2;
-                            to += (c0 >> 3) * G::PANEL;
-                            *reinterpret_cast<uint4*>(to + (((c0 & 7) ^ (r & 7)) << 4)) = make_uint4(a[0], a[1], b[0], b[1]);
-                            *reinterpret_cast<uint4*>(to + ((((c0 + 1) & 7) ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], f[0], f[1]);
-                        }
-                    }
-                }
-                if constexpr (DT == 2) {
-                    signal(c);
-                } else {
-                    cp_async_commit();
-                    if (c >= uint32_t(kWideLag)) {
-                        cp_async_wait<kWideLag>();
-                        signal(c - kWideLag);
-                    }
+        auto wait_slot = [&](uint32_t c) { return c < uint32_t(G::NS) || wait(b_empty + 8 * (c % G::NS), (c / G::NS + 1) & 1); };
+        auto meet = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(G::FETCH) : "memory"); };
+        // The tile as boxes of the tensor map, a lane each: 64 channels (fp8: whole rows) of the rows of a
+        // page.  Boxes behind the last row and pages outside the pool are left out; returns the missing groups
+        // of 16 rows below the last one.
+        const int box_rows = P.block_table == nullptr ? kWideTile : min(kWideTile, 1 << P.page_shift);
+        auto issue = [&](const WideCursor<G>& x, uint32_t dst, uint32_t bar) -> uint32_t {
+            constexpr int BP = DT == 2 ? 1 : G::PANELS;
+            const int box = lane / BP, panel = lane % BP, row = x.row0() + box * box_rows;
+            bool there = box < kWideTile / box_rows && row < x.U.lim;
+            const bool wanted = there;
+            int c1 = row, c3 = x.sh.b;
+            if (there && P.block_table != nullptr) {
+                c3 = __ldg(P.block_table + (long long)x.sh.b * P.max_blocks + (row >> P.page_shift));
+                c1 = row & ((1 << P.page_shift) - 1);
+                if (c3 < 0 || c3 >= P.num_pages) {
+                    there = false;
+                    record_status(P.status, ST_EINVAL, x.sh.b);
                 }
             }
-            wide_next(sh, U, upb);
-        }
+            const int boxes = __popc(__ballot_sync(~0u, there));
+            const unsigned missing = __ballot_sync(~0u, wanted && !there && panel == 0);
+            uint32_t flags = 0;  // a bit per group of 16 rows
+            for (unsigned m = missing; m; m &= m - 1) {
+                const int first = (__ffs(int(m)) - 1) / BP * box_rows / 16;
+                flags |= ((1u << box_rows / 16) - 1) << first;
+            }
+            const uint32_t box_bytes = uint32_t(box_rows) * (DT == 2 ? G::ROWB : 128);
+            if (lane == 0 && !x.is_v()) gone[x.c % kWideRowFlags] = flags;
+            if (lane == 0) mbar_arrive_expect_tx(bar, boxes * box_bytes);
+            __syncwarp();
+            if (there)
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                        dst + panel * G::PANEL + box * box_bytes),
+                    "l"(x.is_v() ? &map_v : &map_k), "r"(panel * 64), "r"(c1), "r"(x.U.h), "r"(c3), "r"(bar)
+                    : "memory");
+            return flags;
+        };
+        auto not_finite = [](const uint4& v) {
+            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (DT == 0) odd |= (x[k] & 0x7f80u) == 0x7f80u || (x[k] & 0x7f800000u) == 0x7f800000u;
+                if (DT == 1) odd |= (x[k] & 0x7c00u) == 0x7c00u || (x[k] & 0x7c000000u) == 0x7c000000u;
+                if (DT == 2)
+                    for (int e = 0; e < 4; ++e) odd |= ((x[k] >> (8 * e)) & 0x7f) == 0x7f;
+            }
+            return odd;
+        };
+        // Notes the drafted rows of a V tile that are not finite; `piece(id)` gives 16 bytes of row id / CPR.
+        auto note_odd = [&](const WideCursor<G>& x, int slot, auto&& piece) {
+            if (ptid < 4) odd_rows[slot * 4 + ptid] = 0u;
+            meet();
+            for (int id = ptid; id < G::CHUNKS; id += G::FETCH) {
+                const int r = id / G::CPR, row = x.row0() + r;
+                if (row >= x.U.base && row < x.U.lim && not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + (r >> 5)], 1u << (r & 31));
+            }
+            meet();
+        };
+        // the groups of 16 rows of a tile whose pages are not in the pool, for warps that did not issue it
+        auto missing_groups = [&](const WideCursor<G>& x) -> uint32_t {
+            if (P.block_table == nullptr) return 0u;
+            const int row = x.row0() + 16 * (lane & 7);
+            bool miss = false;
+            if (row < x.U.lim) {
+                const int page = __ldg(P.block_table + (long long)x.sh.b * P.max_blocks + (row >> P.page_shift));
+                miss = page < 0 || page >= P.num_pages;
+            }
+            return __ballot_sync(~0u, miss) & 255u;
+        };
+        // rows of a V tile that enter as zeros
+        auto zero_row = [&](const WideCursor<G>& x, int slot, int r, uint32_t groups, bool careful) {
+            return x.row0() + r >= x.U.lim || (groups >> (r >> 4) & 1) || (careful && (odd_rows[slot * 4 + (r >> 5)] >> (r & 31) & 1));
+        };
+        WideCursor<G> at;
+        at.start(P, sh);
         if constexpr (DT != 2) {
-            cp_async_wait<0>();
-            if (ok)
-                for (uint32_t k = c > uint32_t(kWideLag) ? c - kWideLag : 0; k < c; ++k) signal(k);
+            for (; at.more; at.next(P, upb)) {
+                const int slot = int(at.c % G::NS);
+                const uint32_t dst = s_ring + slot * G::SLOT;
+                const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
+                const bool careful = at.careful(), mend = at.is_v() && (careful || groups || at.row0() + kWideTile > at.U.lim);
+                if (issuer && wait_slot(at.c)) issue(at, dst, mend ? b_mend : b_full + 8 * slot);
+                if (!mend) continue;
+                wait(b_mend, mended++ & 1);  // look at the tile where it has landed
+                unsigned char* tile = smem + (dst - sbase);
+                auto piece = [&](int id) {
+                    const int r = id / G::CPR, ch = id % G::CPR;
+                    return reinterpret_cast<uint4*>(tile + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+                };
+                if (careful) note_odd(at, slot, [&](int id) { return *piece(id); });
+                for (int id = ptid; id < G::CHUNKS; id += G::FETCH)
+                    if (zero_row(at, slot, id / G::CPR, groups, careful)) *piece(id) = make_uint4(0u, 0u, 0u, 0u);
+                fence_proxy_async();
+                meet();
+                if (ptid == 0 && ok) mbar_arrive(b_full + 8 * slot);
+            }
+        } else {
+            // RS tiles as they are stored, all fetching warps widen one after the other into the ring
+            WideCursor<G> in = at;
+            auto fetch = [&]() {
+                if (!in.more) return;
+                if (issuer && ok) issue(in, s_raw + (in.c % G::RS) * G::RAW, b_raw + 8 * (in.c % G::RS));
+                in.next(P, upb);
+            };
+            for (int k = 0; k < G::RS; ++k) fetch();
+            for (; at.more; at.next(P, upb)) {
+                const int slot = int(at.c % G::NS);
+                const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
+                const bool careful = at.careful(), mend = at.is_v() && (careful || groups || at.row0() + kWideTile > at.U.lim);
+                wait(b_raw + 8 * (at.c % G::RS), (at.c / G::RS) & 1);
+                wait_slot(at.c);
+                const unsigned char* from = smem + (s_raw - sbase) + (at.c % G::RS) * G::RAW;
+                unsigned char* to = smem + (s_ring - sbase) + slot * G::SLOT;
+                if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
+#pragma unroll 2
+                for (int id = ptid; id < G::CHUNKS; id += G::FETCH) {
+                    const int r = id / G::CPR, ch = id % G::CPR;
+                    uint4 x = *reinterpret_cast<const uint4*>(from + id * 16);
+                    if (mend && zero_row(at, slot, r, groups, careful)) x = make_uint4(0u, 0u, 0u, 0u);
+                    uint32_t a[2], b[2], e[2], f[2];
+                    Elem<2>::expand(x.x, a);
+                    Elem<2>::expand(x.y, b);
+                    Elem<2>::expand(x.z, e);
+                    Elem<2>::expand(x.w, f);
+                    unsigned char* row = to + (ch >> 2) * G::PANEL + r * 128;
+                    const int c0 = (ch & 3) * 2;
+                    *reinterpret_cast<uint4*>(row + ((c0 ^ (r & 7)) << 4)) = make_uint4(a[0], a[1], b[0], b[1]);
+                    *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], f[0], f[1]);
+                }
+                fence_proxy_async();
+                meet();  // the stored tile has been read by all: its place may be filled again
+                if (ptid == 0 && ok) mbar_arrive(b_full + 8 * slot);
+                fetch();
+            }
         }
-    } else if (w == 12) {
+    } else if (w == 8) {
         // ------------------------------------------------------------------ the products
         constexpr uint32_t id_qk = mma_idesc(DT == 0, false, kWideTile), id_pv = mma_idesc(DT == 0, true, D);
         uint32_t c0 = 0;                       // first load of the unit
@@ -486,10 +571,13 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
                 const int i = MT == 2 ? k : 2 * k + s, r0 = (U.tile0 + i) * kWideTile;
                 wait(b_s + 8 * s, ns++ & 1);
                 const bool draft = U.masked && r0 + kWideTile > U.base;
-                const bool hidden = draft || r0 + kWideTile > U.lim;
+                const uint32_t missing = gone[(c0 + load_of_k<MT>(i)) % kWideRowFlags];  // 16-row groups without a page
+                const bool hidden = draft || missing || r0 + kWideTile > U.lim;
                 // which of 32 rows from r on this query row sees
                 auto seen32 = [&](int r) -> uint32_t {
                     uint32_t see = r >= U.lim ? 0u : U.lim - r >= 32 ? ~0u : (1u << (U.lim - r)) - 1;
+                    if (missing >> ((r - r0) >> 4) & 1) see &= 0xffff0000u;
+                    if (missing >> ((r - r0) >> 4) & 2) see &= 0x0000ffffu;
                     if (draft && r + 32 > U.base) {
                         const int j = r - U.base;  // drafted rows j ..
                         const uint32_t word = j >= 64 ? 0u : j >= 0 ? uint32_t(bits >> j) : (j > -32 ? uint32_t(bits << -j) | ((1u << -j) - 1) : ~0u);
@@ -497,101 +585,146 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
                     }
                     return see;
                 };
-                // the largest logit first: scores are read twice, registers hold 64 of them
-                float top = -INFINITY;
+                // Two passes over the scores, the largest logit and then the probabilities, in short loops: an
+                // unrolled single pass that holds a tile's probabilities spills and misses in the instruction
+                // cache.  The reference moves only when a probability would pass 2^6 of what it was set for.
                 uint32_t a[32], b[32];
-                tm_ld32(a, t_s);
+                bool again = hidden;
+                if (!hidden) {
+                    float top[2] = {-INFINITY, -INFINITY};
+                    auto largest = [&](const uint32_t (&x)[32]) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t (&x)[32] = (q & 1) ? b : a;
-                    tm_wait_ld(x);
-                    if (q < 3) tm_ld32((q & 1) ? a : b, t_s + 32 * (q + 1));
-                    if (hidden) {
-                        const uint32_t see = seen32(r0 + 32 * q);
+                        for (int e = 0; e < 32; e += 4) {
+                            top[0] = fmaxf(top[0], fmaxf(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
+                            top[1] = fmaxf(top[1], fmaxf(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])));
+                        }
+                    };
+                    tm_ld32(a, t_s);
+#pragma unroll 1
+                    for (int q = 0; q < 128; q += 64) {
+                        tm_wait_ld(a);
+                        tm_ld32(b, t_s + q + 32);
+                        largest(a);
+                        tm_wait_ld(b);
+                        tm_ld32(a, t_s + (q ^ 64));  // the next one, at the end the first one again
+                        largest(b);
+                    }
+                    // no reference yet, or one that is too low (a NaN logit leaves it where it is)
+                    again = __any_sync(~0u, ref == -INFINITY || fmaxf(top[0], top[1]) * scl - X::kRefShift > ref + 6.f);
+                    if (!again) {
+                        const f32x2 scl2 = pack2(scl, scl), at2 = pack2(-ref, -ref);
+                        f32x2 part[2] = {0ull, 0ull};
+                        auto weigh = [&](const uint32_t (&x)[32], uint32_t to) {
+                            uint32_t p[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (see >> e & 1) top = fmaxf(top, __uint_as_float(x[e]));
+                            for (int e = 0; e < 32; e += 2) {
+                                float p0, p1;
+                                unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), scl2, at2), p0, p1);
+                                p0 = ex2(p0);
+                                p1 = ex2(p1);
+                                part[e / 2 & 1] = add2(part[e / 2 & 1], pack2(p0, p1));
+                                p[e / 2] = X::pack(p0, p1);
+                            }
+                            tm_st16(to, p);
+                        };
+#pragma unroll 1
+                        for (int q = 0; q < 128; q += 64) {
+                            tm_wait_ld(a);
+                            tm_ld32(b, t_s + q + 32);
+                            weigh(a, t_s + q / 2);
+                            tm_wait_ld(b);
+                            if (q == 0) tm_ld32(a, t_s + 64);
+                            weigh(b, t_s + q / 2 + 16);
+                        }
+                        float s0, s1;
+                        unpack2(add2(part[0], part[1]), s0, s1);
+                        sum += s0 + s1;
                     } else {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
+                        tm_wait_ld(a);
                     }
                 }
-                top = top * scl - X::kRefShift;
-                // the reference moves only when a probability would pass 2^6 of what it was scaled for
-                const bool first = ref == -INFINITY, grew = top > ref + 6.f || (first && top > -INFINITY);
-                if (__any_sync(~0u, grew && !first)) {
-                    const float r = grew ? top : ref, g = grew && !first ? ex2(ref - r) : 1.f;
-                    sum *= g;
-                    ref = r;
-#pragma unroll
-                    for (int d = 0; d < D; d += 32) {
-                        tm_ld32(a, t_o + d);
+                if (again) {
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        tm_ld32(a, t_s + 32 * q);
+                        const uint32_t see = hidden ? seen32(r0 + 32 * q) : ~0u;
                         tm_wait_ld(a);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * g);
-                        tm_st32(t_o + d, a);
+                        for (int e = 0; e < 32; ++e) top = fmaxf(top, see >> e & 1 ? __uint_as_float(a[e]) : -INFINITY);
                     }
-                } else if (grew) {
-                    ref = top;
-                }
-                const float at = ref == -INFINITY ? 0.f : ref;
-                if (draft) {
-                    // drafted rows that are not finite went into the tile as zeros: add them for those who see them
-                    const uint32_t l = c0 + load_of_v<MT>(i, U.n);
-                    wait(b_full + 8 * (l % G::NS), (l / G::NS) & 1);
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t odd = ok ? odd_rows[l % G::NS * 4 + q] : 0u;
-                        for (; odd; odd &= odd - 1) {
-                            const int e = __ffs(int(odd)) - 1, r = r0 + 32 * q + e;
-                            const float z = __uint_as_float(tm_read1(t_s + 32 * q + e));
-                            const bool see = seen32(r0 + 32 * q) >> e & 1;
-                            const float p = see ? ex2(z * scl - at) : 0.f;
-                            const uint8_t* v = P.V + attend_offset(P, sh.b, U.h, r & ~15) + (long long)(r & 15) * P.ss;
+                    top = top * scl - X::kRefShift;
+                    const bool first = ref == -INFINITY, grew = top > ref + 6.f || (first && top > -INFINITY);
+                    if (__any_sync(~0u, grew && !first)) {
+                        const float g = grew && !first ? ex2(ref - top) : 1.f;
+                        sum *= g;
 #pragma unroll 1
-                            for (int d = 0; d < D; d += 32) {
-                                tm_ld32(a, t_o + d);
-                                tm_wait_ld(a);
+                        for (int d = 0; d < D; d += 32) {
+                            tm_ld32(a, t_o + d);
+                            tm_wait_ld(a);
 #pragma unroll
-                                for (int x = 0; x < 32; ++x) {
-                                    float y;
-                                    if (DT == 2) {
-                                        uint32_t pr[2];
-                                        Elem<2>::expand(__ldg(v + d + x), pr);
-                                        y = Elem<1>::lo(pr[0]);
-                                    } else {
-                                        y = q_to_float(__ldg(reinterpret_cast<const uint16_t*>(v) + d + x), DT == 1);
+                            for (int e = 0; e < 32; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * g);
+                            tm_st32(t_o + d, a);
+                        }
+                    }
+                    if (grew) ref = top;
+                    const float at = ref == -INFINITY ? 0.f : ref;
+                    if (draft) {
+                        // drafted rows that are not finite went into the tile as zeros: add them for those who see them
+                        const uint32_t l = c0 + load_of_v<MT>(i, U.n);
+                        wait(b_full + 8 * (l % G::NS), (l / G::NS) & 1);
+                        tm_wait_st();
+#pragma unroll 1
+                        for (int q = 0; q < 4; ++q) {
+#pragma unroll 1
+                            for (uint32_t odd = ok ? odd_rows[l % G::NS * 4 + q] : 0u; odd; odd &= odd - 1) {
+                                const int e = __ffs(int(odd)) - 1, r = r0 + 32 * q + e;
+                                const float z = __uint_as_float(tm_read1(t_s + 32 * q + e));
+                                const bool see = seen32(r0 + 32 * q) >> e & 1;
+                                const float p = see ? ex2(z * scl - at) : 0.f;
+                                const uint8_t* v = P.V + attend_offset(P, sh.b, U.h, r & ~15) + (long long)(r & 15) * P.ss;
+#pragma unroll 1
+                                for (int d = 0; d < D; d += 32) {
+                                    tm_ld32(a, t_o + d);
+                                    tm_wait_ld(a);
+#pragma unroll
+                                    for (int x = 0; x < 32; ++x) {
+                                        float y;
+                                        if (DT == 2) {
+                                            uint32_t pr[2];
+                                            Elem<2>::expand(__ldg(v + d + x), pr);
+                                            y = Elem<1>::lo(pr[0]);
+                                        } else {
+                                            y = q_to_float(__ldg(reinterpret_cast<const uint16_t*>(v) + d + x), DT == 1);
+                                        }
+                                        if (see) a[x] = __float_as_uint(__uint_as_float(a[x]) + p * y);
                                     }
-                                    if (see) a[x] = __float_as_uint(__uint_as_float(a[x]) + p * y);
+                                    tm_st32(t_o + d, a);
+                                    tm_wait_st();
                                 }
-                                tm_st32(t_o + d, a);
-                                tm_wait_st();
                             }
                         }
                     }
-                }
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
-                tm_ld32(a, t_s);
+                    float part[2] = {0.f, 0.f};
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        tm_ld32(a, t_s + 32 * q);
+                        const uint32_t see = hidden ? seen32(r0 + 32 * q) : ~0u;
+                        tm_wait_ld(a);
+                        uint32_t p[16];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t (&x)[32] = (q & 1) ? b : a;
-                    tm_wait_ld(x);
-                    if (q < 3) tm_ld32((q & 1) ? a : b, t_s + 32 * (q + 1));
-                    const uint32_t see = hidden ? seen32(r0 + 32 * q) : ~0u;
-                    uint32_t p[16];
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float p0 = ex2(fmaf(__uint_as_float(x[e]), scl, -at)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), scl, -at));
-                        if (hidden) {
+                        for (int e = 0; e < 32; e += 2) {
+                            float p0 = ex2(fmaf(__uint_as_float(a[e]), scl, -at)), p1 = ex2(fmaf(__uint_as_float(a[e + 1]), scl, -at));
                             p0 = see >> e & 1 ? p0 : 0.f;
                             p1 = see >> (e + 1) & 1 ? p1 : 0.f;
+                            part[0] += p0;
+                            part[1] += p1;
+                            p[e / 2] = X::pack(p0, p1);
                         }
-                        part[e & 2] += p0;
-                        part[(e & 2) + 1] += p1;
-                        p[e / 2] = X::pack(p0, p1);
+                        tm_st16(t_s + 16 * q, p);
                     }
-                    tm_st16(t_s + 16 * q, p);
+                    sum += part[0] + part[1];
                 }
-                sum += (part[0] + part[1]) + (part[2] + part[3]);
                 tm_wait_st();
                 tm_fence_before();
                 __syncwarp();
@@ -658,37 +791,66 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P) {
                 }
                 if (MT == 1) named_bar_sync(1, 256);
             }
-            if (shared) {
-                if (writes) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
-                __threadfence();
-                named_bar_sync(1, 256);
-                const long long unit = (long long)sh.b * upb + U.u;
-                if (tid == 0) {
-                    *slast = 0;
-                    if (ok) {
-                        const int n = atomicAdd(P.counters + unit, 1);
-                        *slast = n == int(last_cta - first_cta);
-                        if (*slast) P.counters[unit] = 0;
-                    }
-                }
-                named_bar_sync(1, 256);
-                if (*slast) {
-                    __threadfence();
-                    for (int x = 0; x < MT; ++x) {
-                        const int rows = min(kWideTile, U.mrows - x * kWideTile);
-                        attend_combine<D, DT, kWideTile>(P, sh.b, U.h, 0, U.m0 + x * kWideTile, rows, U.seq.tokens, first_cta, last_cta, G::PSIZE,
-                                                         x * kWideTile * (D + 2), tid, 256);
-                    }
-                }
-                named_bar_sync(1, 256);
-            }
+            if (shared && writes) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
+            // who shares the unit, for the kernel that joins the partials: said once, by the CTA that starts it
+            if (tid == 0 && first_cta == (long long)blockIdx.x)
+                P.shared[(long long)sh.b * upb + U.u] = ok ? make_int2(int(first_cta), int(last_cta)) : make_int2(0, 0);
             c0 += 2 * U.n;
             wide_next(sh, U, upb);
         }
     }
     tm_fence_before();
     __syncthreads();
-    if (w == 12) tm_free(tm);
+    if (w == 8) tm_free(tm);
+}
+
+// Joins the partials of shared units in the order of their rows: a CTA per 16 query rows of a unit.
+constexpr int kJoinRows = 16, kJoinThreads = 256;
+template <int D, int DT, int MT>
+__global__ void __launch_bounds__(kJoinThreads)
+lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
+    constexpr int CHUNKS = MT * kWideTile / kJoinRows;
+    const int upb = P.H * P.mtiles, chunk = blockIdx.x % CHUNKS;
+    const long long unit = blockIdx.x / CHUNKS;
+    const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, m0 = u % P.mtiles * (MT * kWideTile);
+    const int r0 = chunk * kJoinRows, rows = min(kJoinRows, P.T * P.G - m0 - r0);
+    if (rows <= 0) return;
+    const int2 who = P.shared[unit];
+    if (who.x == who.y) return;
+    const AttendSeq seq = attend_seq<kWideTile>(P, b, false);
+    const int half = r0 / kWideTile, in_half = r0 % kWideTile;
+    constexpr int PSIZE = WideGeo<D, DT, MT>::PSIZE;
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kJoinThreads) {
+        const int m = in_half + i / (D / 4), d = (i % (D / 4)) * 4;
+        float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        constexpr int BATCH = 8;  // partials in flight
+        for (int c = who.x; c <= who.y; c += BATCH) {
+            float2 ml[BATCH];
+            float4 v[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (c + k <= who.y) {
+                    const float* pp = P.partials + (2ll * (c + k) + (c + k == who.x ? 1 : 0)) * PSIZE + half * kWideTile * (D + 2);
+                    ml[k] = __ldcg(reinterpret_cast<const float2*>(pp + kWideTile * D + 2 * m));
+                    v[k] = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (c + k <= who.y && !(ml[k].x == -INFINITY && ml[k].y == 0.f)) {
+                    const float r = fmaxf(top, ml[k].x);
+                    const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml[k].x - r);
+                    total = total * fo + ml[k].y * fn;
+                    o[0] = o[0] * fo + v[k].x * fn;
+                    o[1] = o[1] * fo + v[k].y * fn;
+                    o[2] = o[2] * fo + v[k].z * fn;
+                    o[3] = o[3] * fo + v[k].w * fn;
+                    top = r;
+                }
+            }
+        }
+        attend_write<D, DT>(P, b, h, 0, m0 + r0, seq.tokens, i / (D / 4), d, o, top, total);
+    }
 }
 
 }  // namespace lagkv

@@ -423,3 +423,38 @@ def test_refusals_touch_nothing(binding):
     for i, bad in ((1, None), (2, args[1]), (3, 0), (4, None), (6, 0), (6, 65), (7, None), (8, None)):
         assert lib.lagkv_tree_commit(*(args[:i] + [bad] + args[i + 1:])) == E, i
     assert lib.lagkv_tree_commit(*(args[:10] + [128, None])) == binding.LAGKV_EWORKSPACE
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP8], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("T,G,page", [(12, 4, 16), (40, 4, 64), (20, 4, 128)])
+def test_missing_pages_under_wide_trees(binding, dtype, T, G, page):
+    """A page outside the pool, among the rows that everybody sees, with more query rows than one narrow unit."""
+    B, H, D, S = 2, 1, 128, 640
+    c = case(binding, B, H, G, D, S, T, dtype, seed=4, lens=[640, 513])
+    nb = S // page
+    perm = torch.randperm(B * nb, generator=torch.Generator().manual_seed(2)).view(B, nb).to(torch.int32).to(DEV)
+    pools = [U.to_pages(c[x], page, perm, B * nb, 0.0) for x in "KV"]
+    gone = [1, (S // 2) // page]
+    table = perm.clone()
+    table[0, gone[0]], table[1, gone[1]] = -1, B * nb
+    got = c["plan"].attend_tree_paged(c["Q"], *pools, table, c["seq"], c["ws"], draft_len=c["draft"], tree_mask=c["mask"], want_lse=True,
+                                      k_scale=c["ks"], v_scale=c["vs"])
+    assert c["plan"].read_status(c["ws"])[0] == binding.LAGKV_EINVAL
+    for b in range(B):
+        keep = torch.tensor([r // page != gone[b] for r in range(S)], device=DEV)
+        K, V = (U.bits(c[x])[b:b + 1][:, :, keep].view(dtype) for x in "KV")
+        want = U.tree_reference(c["Q"][b:b + 1], K, V, [int(c["seq"][b]) - page], [T], c["mask"][b:b + 1], None, c["ks"], c["vs"])
+        U.assert_attention({k: v[b:b + 1] for k, v in got.items()}, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP8], ids=["bf16", "fp16", "fp8"])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_wide_trees_over_many_lengths(binding, dtype, D):
+    """Lengths around the 128-row tiles, empty slots, units of one and two groups of query rows, ragged drafts."""
+    for T, G in ((33, 1), (32, 4), (33, 4), (64, 4), (64, 7)):
+        lens = [0, T, T + 1, 127 + T, 128, 129, 255, 256, 257, 640, 700]
+        lens = [max(n, T) if n else 0 for n in lens]
+        drafts = [0 if n == 0 else T - (i % 3) for i, n in enumerate(lens)]
+        c = case(binding, len(lens), 2, G, D, 700, T, dtype, seed=T, lens=lens, drafts=drafts)
+        poison(c)
+        U.assert_attention(run(c), reference(c))
