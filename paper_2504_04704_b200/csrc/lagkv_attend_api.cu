@@ -132,7 +132,7 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     if (rc != LAGKV_OK) return rc;
     // a narrow kernel's CTAs count arrivals per unit; a wide one's say who shares a unit
     const size_t cb = counter_bytes(bytes), pb = partial_bytes(plan, *e) + (e->wide ? up256(size_t(units) * sizeof(int2)) : 0);
-    if (units * (e->rows / 16) > 0x7fffffffll) return LAGKV_EINVAL;
+    if (units * e->rows > 0x7fffffffll) return LAGKV_EINVAL;
     if (size_t(units) * sizeof(int32_t) > cb || kHead + cb + pb + extra > bytes) return LAGKV_EWORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(workspace);
     P->status = reinterpret_cast<int32_t*>(base);

@@ -242,19 +242,21 @@ __device__ __forceinline__ long long attend_offset(const AttendParams& P, int b,
     return (long long)page * P.page_stride + (long long)h * P.sh + (long long)(row0 & ((1 << P.page_shift) - 1)) * P.ss;
 }
 
-// Where a unit's result goes: finished (out, lse) or as a partial (reference, sum, accumulators).
-template <int D, int DT>
+// The finished result of N (4 or 8) channels d .. of query row m of a unit.
+template <int D, int DT, int N>
 __device__ __forceinline__ void attend_write(const AttendParams& P, int b, int h, int t0, int m0, int tokens, int m, int d,
-                                             const float (&o)[4], float ref, float sum) {
-    // four channels d .. d + 3 of query row m
+                                             const float (&o)[N], float ref, float sum) {
     const int row = m0 + m, t = t0 + row / P.G, g = row % P.G;
     const long long at = (((long long)b * P.T + t) * P.H + h) * P.G + g;
     const bool live = t < tokens && sum != 0.f;  // NaN sums stay: they compare unequal to 0
     const float inv = live ? P.v_scale / sum : 0.f;
-    uint2 v;
-    v.x = live ? pack_out<DT>(o[0] * inv, o[1] * inv) : 0u;
-    v.y = live ? pack_out<DT>(o[2] * inv, o[3] * inv) : 0u;
-    *reinterpret_cast<uint2*>(P.out + at * D + d) = v;
+    uint32_t v[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = live ? pack_out<DT>(o[2 * i] * inv, o[2 * i + 1] * inv) : 0u;
+    if constexpr (N == 8)
+        *reinterpret_cast<uint4*>(P.out + at * D + d) = make_uint4(v[0], v[1], v[2], v[3]);
+    else
+        *reinterpret_cast<uint2*>(P.out + at * D + d) = make_uint2(v[0], v[1]);
     if (d == 0 && P.lse) P.lse[at] = live ? 0.69314718055994531f * (ref + log2f(sum)) : -INFINITY;
 }
 

@@ -7,11 +7,11 @@
 // Two streams keep the tensor cores busy while the other one's softmax runs: with up to 128 query rows the
 // streams take every other tile of rows and are joined at the end, with up to 256 each has its own 128
 // query rows and both read the same tiles.
-// Warps: 0-3 and 4-7 the softmax of stream 0 and 1 (a thread owns a query row); 8 issues the products; the
-// others fetch: the first of them by TMA into swizzled shared memory, a box per page and 64 channels (issuing
-// the same tiles as cp.async cost three warps 10000 cycles a step, five times what the products take), all of
-// them to mend V tiles -- rows behind the last one and hidden rows that are not finite become zeros, so that
-// 0 * inf never happens -- and to widen fp8 tiles, which land as they are, to fp16.
+// Warps: 0-3 and 4-7 the softmax of stream 0 and 1 (a thread owns a query row); 8 issues the products; 9
+// fetches tiles by TMA into swizzled shared memory, a box per page and 64 channels (the same tiles as cp.async
+// cost three warps 10000 cycles a step, five times what the products take); the others help: they load the
+// next unit's queries, mend V tiles -- rows behind the last one and hidden rows that are not finite become
+// zeros, so that 0 * inf never happens -- and widen fp8 tiles, which land as they are, to fp16.
 // Partials of shared units (66 KB for 128 query rows) are joined by a kernel of their own: one CTA adding
 // up 18 of them took longer than the attention.
 // Bound: at 128 rows and 16-bit caches by HBM, at 256 by the 16384 exponentials per tile and stream (16 a
@@ -34,10 +34,10 @@ struct WideGeo {
     static constexpr int PANELS = (D + 63) / 64;       // 64 channels of 16 bits: 128-byte rows, swizzled
     static constexpr int PANEL = kWideTile * 128;
     static constexpr int SLOT = PANELS * PANEL;
-    static constexpr int EXCH = 64 * kWideTile * 4;    // MT = 1: 64 channels of one stream's O for the other
+    static constexpr int EXCH = 64 * kWideTile * 4;    // MT = 1: 32 channels of each stream's O for the other
     static constexpr int QBYTES = MT == 2 ? 2 * SLOT : SLOT + EXCH;
     static constexpr int WARPS = DT_ == 2 ? 16 : 12;   // widening takes seven warps to keep up
-    static constexpr int NT = WARPS * 32, FETCH = NT - 9 * 32;
+    static constexpr int NT = WARPS * 32, HELP = NT - 10 * 32;  // threads that load queries, mend and widen
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
     static constexpr int RS = DT_ == 2 ? 4 : 0;                  // ... and how many are in flight
@@ -60,22 +60,35 @@ __device__ __forceinline__ void tm_free(uint32_t base) {
 }
 __device__ __forceinline__ void tm_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tm_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tm_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// High word of the shared memory operands: rows in groups of eight (1024 bytes), swizzled by 128 bytes.
+constexpr uint32_t kDescHi = 1024u >> 4 | 1u << 14 | 2u << 29;
+// Issued by the lane whose `lead` is set, in code that the whole warp runs: operands that are the same in all
+// lanes stay in uniform registers, moving them there one by one cost more than the products.
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 q, %6, 0;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\t"
+        "mov.b64 b, {%2, %5};\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHi), "r"(lead)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc) {
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {  // adds to d
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(1)
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\tsetp.ne.b32 q, %6, 0;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(1), "n"(kDescHi), "r"(lead)
         : "memory");
+}
+__device__ __forceinline__ void tm_commit(uint32_t lead, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+        "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
 }
 __device__ __forceinline__ void tm_ld32(uint32_t (&r)[32], uint32_t a) {
     asm volatile(
@@ -123,11 +136,9 @@ __device__ __forceinline__ void tm_wait_ld(uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared memory operand: 128-byte rows in groups of eight (1024 bytes), swizzled by 128 bytes.  `lead`: bytes
-// between panels of 64 channels (read when the panels run along the operand's outer dimension, as in V).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
-    return uint64_t((addr & 0x3ffff) >> 4) | uint64_t(lead >> 4) << 16 | uint64_t(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Low word of a shared memory operand.  `lead`: bytes between panels of 64 channels (read when the panels run
+// along the operand's outer dimension, as in V).
+__device__ __forceinline__ uint32_t smem_desc_lo(uint32_t addr, uint32_t lead) { return (addr & 0x3ffff) >> 4 | lead >> 4 << 16; }
 // Instruction word of kind::f16: fp32 accumulators, M = 128.
 __device__ __forceinline__ constexpr uint32_t mma_idesc(bool bf16, bool b_rows_are_k, int n) {
     return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_rows_are_k ? 1u << 16 : 0u) | uint32_t(n / 8) << 17 | uint32_t(128 / 16) << 24;
@@ -170,6 +181,62 @@ __device__ __forceinline__ void wide_next(AttendShare& sh, const WideUnit& w, in
     }
 }
 
+// fp8 caches: the power of two that brings a row of bf16 queries to [2^8, 2^9), and its largest magnitude.
+__device__ __forceinline__ float query_factor(float top) {
+    const int e = (__float_as_int(top) >> 23) & 255;  // 0: zero or subnormal, 255: not finite
+    return e > 0 && e < 255 ? __int_as_float(min(262 - e, 254) << 23) : 1.f;
+}
+__device__ __forceinline__ float largest_of(const uint4& v) {
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(Elem<0>::lo(x[k])), fabsf(Elem<0>::hi(x[k]))));
+    return top;
+}
+
+// The queries of a unit into swizzled shared memory (`to`), 32 rows at a time by warp `warp` of `warps`: a lane
+// finds its row's place once, all lanes copy.
+template <class G>
+__device__ __forceinline__ void load_queries(const AttendParams& P, const WideUnit& U, int b, unsigned char* to, int warp, int warps) {
+    constexpr int D = G::D, CH = D / 8;  // 16-byte pieces of a row
+    const int lane = threadIdx.x & 31;
+    const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)(U.h * P.G) * P.q_sh;
+    auto place = [&](int r, int ch) {
+        return reinterpret_cast<uint4*>(to + (r >> 7) * G::SLOT + (ch >> 3) * G::PANEL + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4));
+    };
+#pragma unroll 1
+    for (int r0 = warp * 32; r0 < G::MT * kWideTile; r0 += warps * 32) {
+        const int row = U.m0 + r0 + lane;
+        const long long off = r0 + lane < U.mrows ? (long long)(row / P.G) * P.q_st + (long long)(row % P.G) * P.q_sh : -1;
+        if constexpr (G::DT != 2) {
+#pragma unroll 4
+            for (int k = 0; k < CH; ++k) {
+                const int id = k * 32 + lane, r = r0 + id / CH, ch = id % CH;
+                const long long o = __shfl_sync(~0u, off, id / CH);
+                cp_async16(smem_u32(place(r, ch)), o >= 0 ? q0 + o + ch * 8 : P.Q, o >= 0);
+            }
+        } else {  // a lane takes its row whole and scales it
+            uint4 v[CH];
+            float top = 0.f;
+#pragma unroll
+            for (int ch = 0; ch < CH; ++ch) v[ch] = off >= 0 ? __ldg(reinterpret_cast<const uint4*>(q0 + off) + ch) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int ch = 0; ch < CH; ++ch) top = fmaxf(top, largest_of(v[ch]));
+            const float f = query_factor(top);
+#pragma unroll
+            for (int ch = 0; ch < CH; ++ch) {
+                uint32_t y[4] = {v[ch].x, v[ch].y, v[ch].z, v[ch].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = MmaHalf::pack(Elem<0>::lo(y[k]) * f, Elem<0>::hi(y[k]) * f);
+                *place(r0 + lane, ch) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+        }
+    }
+    cp_async_commit();
+    cp_async_wait<0>();
+    fence_proxy_async();
+}
+
 // A walk over the loads of a CTA's share, in order.
 template <class G>
 struct WideCursor {
@@ -201,6 +268,8 @@ struct WideCursor {
         const int i = G::MT == 2 ? l >> 1 : is_v() ? (l == 2 * U.n - 1 ? U.n - 1 : l / 2 - 1) : (l + 1) >> 1;
         return (U.tile0 + i) * kWideTile;
     }
+    // a V tile with rows that enter as zeros, or that may
+    __device__ __forceinline__ bool mend(uint32_t missing) const { return missing || careful() || row0() + kWideTile > U.lim; }
     // drafted V rows that are not finite are kept out of the tile
     __device__ __forceinline__ bool careful() const { return U.masked && is_v() && row0() + kWideTile > U.base; }
 };
@@ -212,19 +281,20 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     using G = WideGeo<D, DT, MT>;
     using X = Mma<DT>;
     extern __shared__ unsigned char raw[];
-    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, w = __shfl_sync(~0u, tid >> 5, 0);  // the same in all lanes, visibly
     const uint32_t sbase = (smem_u32(raw) + 1023u) & ~1023u;
     unsigned char* smem = raw + (sbase - smem_u32(raw));
     const uint32_t s_q = sbase, s_ring = sbase + G::QBYTES, s_raw = s_ring + G::NS * G::SLOT, s_misc = s_raw + G::RS * G::RAW;
     unsigned char* misc = smem + (s_misc - sbase);
     float* exch = reinterpret_cast<float*>(smem + G::SLOT);  // MT = 1
-    // misc: barriers, the rows of each V tile that are not finite, the missing 16-row groups of K tiles,
-    // scheduling scratch
-    const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_raw = b_empty + 8 * 8, b_s = b_raw + 4 * 8, b_p = b_s + 16, b_o = b_p + 16,
-                   b_q = b_o + 16, b_mend = b_q + 8;
-    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 256);                     // [8][4]
-    volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 384);       // [kWideRowFlags]
-    long long* scan = reinterpret_cast<long long*>(misc + 512);                       // [16 + 2]
+    // misc: barriers (tile ready, place free, landed but not ready; scores, probabilities twice, O; queries in
+    // place, their place free), the rows of each V tile that are not finite, the missing 16-row groups of K
+    // tiles, scheduling scratch
+    const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_land = b_empty + 8 * 8, b_raw_free = b_land + 4 * 8, b_s = b_land + 8 * 8,
+                   b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_q = b_o + 16, b_q_free = b_q + 8;
+    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 288);                     // [8][4]
+    volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 416);       // [kWideRowFlags]
+    long long* scan = reinterpret_cast<long long*>(misc + 544);                       // [16 + 2]
     uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 704);
 
     if (tid == 0) {
@@ -235,11 +305,13 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         for (int s = 0; s < 2; ++s) {
             mbar_init(b_s + 8 * s, 1);
             mbar_init(b_p + 8 * s, 4);
+            mbar_init(b_p2 + 8 * s, 4);
             mbar_init(b_o + 8 * s, 1);
         }
-        for (int i = 0; i < G::RS; ++i) mbar_init(b_raw + 8 * i, 1);
-        mbar_init(b_q, 8);
-        mbar_init(b_mend, 1);
+        for (int i = 0; i < (DT == 2 ? G::RS : G::NS); ++i) mbar_init(b_land + 8 * i, 1);
+        for (int i = 0; i < G::RS; ++i) mbar_init(b_raw_free + 8 * i, 1);
+        mbar_init(b_q, G::HELP / 32);
+        mbar_init(b_q_free, 1);
         fence_mbar_init();
     }
     if (w == 8) {
@@ -249,66 +321,83 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     }
     const int upb = P.H * P.mtiles;
     AttendShare sh = attend_share<G::NT, kWideTile>(P, upb, scan);
+    if (sh.pos < sh.end) load_queries<G>(P, wide_unit<G>(P, sh), sh.b, smem, w, G::WARPS);  // the first unit's, by all
     __syncthreads();
     tm_fence_after();
-    const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(tm_slot);
+    const uint32_t tm = __shfl_sync(~0u, *reinterpret_cast<volatile uint32_t*>(tm_slot), 0);
     // tensor memory columns: S (and P over it) of stream 0, 1 at 0, 128; O at 256, 256 + D
     constexpr int kO = 256;
     bool ok = true;
 
-    if (w > 8) {
+    if (w == 9) {
         // ------------------------------------------------------------------ K and V tiles
-        const int ptid = tid - 9 * 32;
-        const bool issuer = w == 9;
-        uint32_t mended = 0;
-        // after a wait that ran out the walk goes on to its end without waiting or copying, so that the barrier
-        // among these warps still matches
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (ok && !mbar_wait_bounded(bar, parity)) {
-                if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
-                ok = false;
-            }
-            return ok;
-        };
-        auto wait_slot = [&](uint32_t c) { return c < uint32_t(G::NS) || wait(b_empty + 8 * (c % G::NS), (c / G::NS + 1) & 1); };
-        auto meet = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(G::FETCH) : "memory"); };
         // The tile as boxes of the tensor map, a lane each: 64 channels (fp8: whole rows) of the rows of a
-        // page.  Boxes behind the last row and pages outside the pool are left out; returns the missing groups
-        // of 16 rows below the last one.
+        // page.  Boxes behind the last row and pages outside the pool are left out.
+        constexpr int BP = DT == 2 ? 1 : G::PANELS;
         const int box_rows = P.block_table == nullptr ? kWideTile : min(kWideTile, 1 << P.page_shift);
-        auto issue = [&](const WideCursor<G>& x, uint32_t dst, uint32_t bar) -> uint32_t {
-            constexpr int BP = DT == 2 ? 1 : G::PANELS;
-            const int box = lane / BP, panel = lane % BP, row = x.row0() + box * box_rows;
-            bool there = box < kWideTile / box_rows && row < x.U.lim;
+        const int box = lane / BP, panel = lane % BP;
+        const uint32_t box_bytes = uint32_t(box_rows) * (DT == 2 ? G::ROWB : 128);
+        WideCursor<G> at;
+        at.start(P, sh);
+        for (; at.more; at.next(P, upb)) {
+            const int row = at.row0() + box * box_rows;
+            bool there = box < kWideTile / box_rows && row < at.U.lim;
             const bool wanted = there;
-            int c1 = row, c3 = x.sh.b;
+            int c1 = row, c3 = at.sh.b;
             if (there && P.block_table != nullptr) {
-                c3 = __ldg(P.block_table + (long long)x.sh.b * P.max_blocks + (row >> P.page_shift));
+                c3 = __ldg(P.block_table + (long long)at.sh.b * P.max_blocks + (row >> P.page_shift));
                 c1 = row & ((1 << P.page_shift) - 1);
                 if (c3 < 0 || c3 >= P.num_pages) {
                     there = false;
-                    record_status(P.status, ST_EINVAL, x.sh.b);
+                    record_status(P.status, ST_EINVAL, at.sh.b);
                 }
             }
             const int boxes = __popc(__ballot_sync(~0u, there));
             const unsigned missing = __ballot_sync(~0u, wanted && !there && panel == 0);
-            uint32_t flags = 0;  // a bit per group of 16 rows
-            for (unsigned m = missing; m; m &= m - 1) {
-                const int first = (__ffs(int(m)) - 1) / BP * box_rows / 16;
-                flags |= ((1u << box_rows / 16) - 1) << first;
+            uint32_t flags = 0;  // a bit per group of 16 rows whose page is not in the pool
+            for (unsigned m = missing; m; m &= m - 1) flags |= ((1u << box_rows / 16) - 1) << (__ffs(int(m)) - 1) / BP * box_rows / 16;
+            const bool is_v = at.is_v();
+            uint32_t dst, bar;
+            bool free;
+            if (DT == 2) {
+                const uint32_t place = at.c % (G::RS ? G::RS : 1);
+                free = int(at.c) < G::RS || mbar_wait_bounded(b_raw_free + 8 * place, (at.c / (G::RS ? G::RS : 1) + 1) & 1);
+                dst = s_raw + place * G::RAW;
+                bar = b_land + 8 * place;
+            } else {
+                const uint32_t slot = at.c % G::NS;
+                free = at.c < uint32_t(G::NS) || mbar_wait_bounded(b_empty + 8 * slot, (at.c / G::NS + 1) & 1);
+                dst = s_ring + slot * G::SLOT;
+                bar = (is_v && at.mend(flags) ? b_land : b_full) + 8 * slot;
             }
-            const uint32_t box_bytes = uint32_t(box_rows) * (DT == 2 ? G::ROWB : 128);
-            if (lane == 0 && !x.is_v()) gone[x.c % kWideRowFlags] = flags;
-            if (lane == 0) mbar_arrive_expect_tx(bar, boxes * box_bytes);
+            if (!free) {
+                if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+                break;
+            }
+            if (lane == 0) {
+                if (!is_v) gone[at.c % kWideRowFlags] = flags;
+                mbar_arrive_expect_tx(bar, boxes * box_bytes);
+            }
             __syncwarp();
             if (there)
                 asm volatile(
                     "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
                         dst + panel * G::PANEL + box * box_bytes),
-                    "l"(x.is_v() ? &map_v : &map_k), "r"(panel * 64), "r"(c1), "r"(x.U.h), "r"(c3), "r"(bar)
+                    "l"(is_v ? &map_v : &map_k), "r"(panel * 64), "r"(c1), "r"(at.U.h), "r"(c3), "r"(bar)
                     : "memory");
-            return flags;
+        }
+    } else if (w > 9) {
+        // ------------------------------------------------------------------ help
+        const int ptid = tid - 10 * 32;
+        // after a wait that ran out the walk goes on to its end without waiting, so that the barrier among these
+        // warps still matches
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            if (ok && !mbar_wait_bounded(bar, parity)) {
+                if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+                ok = false;
+            }
         };
+        auto meet = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(G::HELP) : "memory"); };
         auto not_finite = [](const uint4& v) {
             const uint32_t x[4] = {v.x, v.y, v.z, v.w};
             bool odd = false;
@@ -325,13 +414,13 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         auto note_odd = [&](const WideCursor<G>& x, int slot, auto&& piece) {
             if (ptid < 4) odd_rows[slot * 4 + ptid] = 0u;
             meet();
-            for (int id = ptid; id < G::CHUNKS; id += G::FETCH) {
-                const int r = id / G::CPR, row = x.row0() + r;
-                if (row >= x.U.base && row < x.U.lim && not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + (r >> 5)], 1u << (r & 31));
-            }
+            const int first = max(0, x.U.base - x.row0()) * G::CPR, last = min(kWideTile, x.U.lim - x.row0()) * G::CPR;
+#pragma unroll 4
+            for (int id = first + ptid; id < last; id += G::HELP)
+                if (not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
             meet();
         };
-        // the groups of 16 rows of a tile whose pages are not in the pool, for warps that did not issue it
+        // the groups of 16 rows of a V tile whose pages are not in the pool
         auto missing_groups = [&](const WideCursor<G>& x) -> uint32_t {
             if (P.block_table == nullptr) return 0u;
             const int row = x.row0() + 16 * (lane & 7);
@@ -342,53 +431,48 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             return __ballot_sync(~0u, miss) & 255u;
         };
-        // rows of a V tile that enter as zeros
         auto zero_row = [&](const WideCursor<G>& x, int slot, int r, uint32_t groups, bool careful) {
             return x.row0() + r >= x.U.lim || (groups >> (r >> 4) & 1) || (careful && (odd_rows[slot * 4 + (r >> 5)] >> (r & 31) & 1));
         };
+        // where the rows that may have to be zeroed begin
+        auto first_zero = [&](const WideCursor<G>& x, int slot, uint32_t groups, bool careful) {
+            if (groups) return 0;
+            const bool odd = careful && (odd_rows[slot * 4] | odd_rows[slot * 4 + 1] | odd_rows[slot * 4 + 2] | odd_rows[slot * 4 + 3]);
+            return max(0, (odd ? min(x.U.base, x.U.lim) : x.U.lim) - x.row0());
+        };
+        uint32_t landed = 0, units = 0;  // parities of the places where tiles land; units behind
         WideCursor<G> at;
         at.start(P, sh);
-        if constexpr (DT != 2) {
-            for (; at.more; at.next(P, upb)) {
-                const int slot = int(at.c % G::NS);
-                const uint32_t dst = s_ring + slot * G::SLOT;
-                const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
-                const bool careful = at.careful(), mend = at.is_v() && (careful || groups || at.row0() + kWideTile > at.U.lim);
-                if (issuer && wait_slot(at.c)) issue(at, dst, mend ? b_mend : b_full + 8 * slot);
-                if (!mend) continue;
-                wait(b_mend, mended++ & 1);  // look at the tile where it has landed
-                unsigned char* tile = smem + (dst - sbase);
+        for (; at.more; at.next(P, upb)) {
+            if (at.l == 0 && at.c > 0) {  // the next unit's queries, once the products with those before are done
+                wait(b_q_free, units++ & 1);
+                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, G::HELP / 32);
+                __syncwarp();
+                if (lane == 0 && ok) mbar_arrive(b_q);
+            }
+            if (DT != 2 && !at.is_v()) continue;
+            const int slot = int(at.c % G::NS);
+            const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
+            const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
+            if (DT != 2 && !mend) continue;
+            const int place = DT == 2 ? int(at.c % (G::RS ? G::RS : 1)) : slot;
+            wait(b_land + 8 * place, landed >> place & 1);
+            landed ^= 1u << place;
+            unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
+            if constexpr (DT != 2) {
                 auto piece = [&](int id) {
                     const int r = id / G::CPR, ch = id % G::CPR;
                     return reinterpret_cast<uint4*>(tile + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
                 };
                 if (careful) note_odd(at, slot, [&](int id) { return *piece(id); });
-                for (int id = ptid; id < G::CHUNKS; id += G::FETCH)
+                for (int id = first_zero(at, slot, groups, careful) * G::CPR + ptid; id < G::CHUNKS; id += G::HELP)
                     if (zero_row(at, slot, id / G::CPR, groups, careful)) *piece(id) = make_uint4(0u, 0u, 0u, 0u);
-                fence_proxy_async();
-                meet();
-                if (ptid == 0 && ok) mbar_arrive(b_full + 8 * slot);
-            }
-        } else {
-            // RS tiles as they are stored, all fetching warps widen one after the other into the ring
-            WideCursor<G> in = at;
-            auto fetch = [&]() {
-                if (!in.more) return;
-                if (issuer && ok) issue(in, s_raw + (in.c % G::RS) * G::RAW, b_raw + 8 * (in.c % G::RS));
-                in.next(P, upb);
-            };
-            for (int k = 0; k < G::RS; ++k) fetch();
-            for (; at.more; at.next(P, upb)) {
-                const int slot = int(at.c % G::NS);
-                const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
-                const bool careful = at.careful(), mend = at.is_v() && (careful || groups || at.row0() + kWideTile > at.U.lim);
-                wait(b_raw + 8 * (at.c % G::RS), (at.c / G::RS) & 1);
-                wait_slot(at.c);
-                const unsigned char* from = smem + (s_raw - sbase) + (at.c % G::RS) * G::RAW;
-                unsigned char* to = smem + (s_ring - sbase) + slot * G::SLOT;
+            } else {
+                if (at.c >= uint32_t(G::NS)) wait(b_empty + 8 * slot, (at.c / G::NS + 1) & 1);
+                const unsigned char* from = smem + (s_raw - sbase) + place * G::RAW;
                 if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
 #pragma unroll 2
-                for (int id = ptid; id < G::CHUNKS; id += G::FETCH) {
+                for (int id = ptid; id < G::CHUNKS; id += G::HELP) {
                     const int r = id / G::CPR, ch = id % G::CPR;
                     uint4 x = *reinterpret_cast<const uint4*>(from + id * 16);
                     if (mend && zero_row(at, slot, r, groups, careful)) x = make_uint4(0u, 0u, 0u, 0u);
@@ -397,108 +481,93 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                     Elem<2>::expand(x.y, b);
                     Elem<2>::expand(x.z, e);
                     Elem<2>::expand(x.w, f);
-                    unsigned char* row = to + (ch >> 2) * G::PANEL + r * 128;
+                    unsigned char* row = tile + (ch >> 2) * G::PANEL + r * 128;
                     const int c0 = (ch & 3) * 2;
                     *reinterpret_cast<uint4*>(row + ((c0 ^ (r & 7)) << 4)) = make_uint4(a[0], a[1], b[0], b[1]);
                     *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], f[0], f[1]);
                 }
-                fence_proxy_async();
-                meet();  // the stored tile has been read by all: its place may be filled again
-                if (ptid == 0 && ok) mbar_arrive(b_full + 8 * slot);
-                fetch();
+            }
+            fence_proxy_async();
+            meet();
+            if (ptid == 0 && ok) {
+                mbar_arrive(b_full + 8 * slot);
+                if (DT == 2) mbar_arrive(b_raw_free + 8 * place);
             }
         }
     } else if (w == 8) {
         // ------------------------------------------------------------------ the products
         constexpr uint32_t id_qk = mma_idesc(DT == 0, false, kWideTile), id_pv = mma_idesc(DT == 0, true, D);
-        uint32_t c0 = 0;                       // first load of the unit
-        uint32_t np[2] = {0, 0}, nq = 0;       // probabilities and units waited for
+        const uint32_t lead = elect_one();
+        uint32_t slot = G::NS - 1, phase = 1;   // the load taken last (loads are taken in their order)
+        uint32_t np = 0, nq = 0;                // parities of the streams' probabilities (a bit each), of units
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (ok && !mbar_wait_bounded(bar, parity)) {
+            if (!mbar_wait_bounded(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
                 ok = false;
             }
-            tm_fence_after();
             return ok;
         };
-        auto wait_load = [&](uint32_t l) { return wait(b_full + 8 * ((c0 + l) % G::NS), ((c0 + l) / G::NS) & 1); };
-        auto slot_of = [&](uint32_t l) { return s_ring + ((c0 + l) % G::NS) * G::SLOT; };
-        auto qk = [&](int s, uint32_t l) {
-            if (lane == 0) {
-                const uint32_t q = s_q + (MT == 2 ? s * G::SLOT : 0), k = slot_of(l);
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t o = (ks >> 2) * G::PANEL + (ks & 3) * 32;
-                    mma_ss(tm + s * 128, smem_desc(q + o, 16), smem_desc(k + o, 16), id_qk, ks != 0);
-                }
-                tm_commit(b_s + 8 * s);
+        auto next_load = [&]() {
+            if (++slot == uint32_t(G::NS)) {
+                slot = 0;
+                phase ^= 1;
             }
-            __syncwarp();
+            return wait(b_full + 8 * slot, phase);
         };
-        auto pv = [&](int s, uint32_t l) {
-            if (lane == 0) {
-                const uint32_t v = slot_of(l);
-#pragma unroll
-                for (int ks = 0; ks < kWideTile / 16; ++ks)
-                    mma_ts(tm + kO + s * D, tm + s * 128 + ks * 8, smem_desc(v + ks * 2048, G::PANEL), id_pv);
-            }
-            __syncwarp();
-        };
-        auto release = [&](uint32_t l) {
-            if (lane == 0) tm_commit(b_empty + 8 * ((c0 + l) % G::NS));
-            __syncwarp();
-        };
-        auto done = [&](int s) {
-            if (lane == 0) tm_commit(b_o + 8 * s);
-            __syncwarp();
-        };
-        for (; ok && sh.pos < sh.end;) {
+        const long long begin = sh.pos;
+        while (ok && sh.pos < sh.end) {
             const WideUnit U = wide_unit<G>(P, sh);
-            const int n = U.n;
-            if (!wait(b_q, nq++ & 1)) break;
-            if (MT == 2) {
-                if (!wait_load(0)) break;
-                qk(0, 0);
-                qk(1, 0);
-                release(0);
-                for (int i = 0; i < n; ++i) {
-                    if (!wait_load(2 * i + 1)) break;
-                    for (int s = 0; s < 2; ++s) {
-                        if (!wait(b_p + 8 * s, np[s]++ & 1)) break;
-                        pv(s, 2 * i + 1);
-                        if (s == 1) release(2 * i + 1);
-                        if (i + 1 < n) {
-                            if (s == 0 && !wait_load(2 * i + 2)) break;
-                            qk(s, 2 * i + 2);
-                            if (s == 1) release(2 * i + 2);
-                        } else {
-                            done(s);
-                        }
-                    }
-                    if (!ok) break;
-                }
-            } else {
-                for (int i = 0; i < min(n, 2); ++i) {
-                    if (!wait_load(load_of_k<1>(i))) break;
-                    qk(i, load_of_k<1>(i));
-                    release(load_of_k<1>(i));
-                }
-                for (int i = 0; ok && i < n; ++i) {
-                    const int s = i & 1;
-                    if (!wait_load(load_of_v<1>(i, n))) break;
-                    if (!wait(b_p + 8 * s, np[s]++ & 1)) break;
-                    pv(s, load_of_v<1>(i, n));
-                    release(load_of_v<1>(i, n));
-                    if (i + 2 < n) {
-                        if (!wait_load(load_of_k<1>(i + 2))) break;
-                        qk(s, load_of_k<1>(i + 2));
-                        release(load_of_k<1>(i + 2));
-                    } else {
-                        done(s);
-                    }
-                }
+            const int n = __shfl_sync(~0u, U.n, 0);
+            if (sh.pos != begin) {  // the first unit's queries are there
+                if (!wait(b_q, nq)) break;
+                nq ^= 1;
             }
-            c0 += 2 * n;
+            // Step i: O += P V of step i and the scores of step i + LEAD, whose place the former has freed.
+            constexpr int LEAD = MT == 2 ? 1 : 2;
+#pragma unroll 1
+            for (int i = -LEAD; i < n; ++i) {
+                const bool has_v = i >= 0, has_k = i + LEAD < n;
+                uint32_t v_slot = 0;
+                if (has_v) {
+                    if (!next_load()) break;
+                    v_slot = slot;
+                }
+                if (has_k && !next_load()) break;
+#pragma unroll 1
+                for (int k = 0; k < MT; ++k) {
+                    const int s = MT == 2 ? k : i & 1;
+                    if (has_v) {
+                        const uint32_t v = smem_desc_lo(s_ring + v_slot * G::SLOT, G::PANEL), parity = np >> s & 1;
+                        np ^= 1u << s;
+                        // the first 64 rows as soon as their probabilities are there, the others behind them
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (!wait((half ? b_p2 : b_p) + 8 * s, parity)) break;
+                            tm_fence_after();
+#pragma unroll
+                            for (int ks = half * 4; ks < half * 4 + 4; ++ks)
+                                mma_ts(lead, tm + kO + s * D, tm + s * 128 + ks * 8, v + ks * (2048 >> 4), id_pv);
+                        }
+                        if (!ok) break;
+                    }
+                    if (has_k) {
+                        // addresses count in 16 bytes in the low word and never carry out of it
+                        const uint32_t q = smem_desc_lo(s_q + (MT == 2 ? s * G::SLOT : 0), 16), kd = smem_desc_lo(s_ring + slot * G::SLOT, 16);
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            const uint32_t o = ((ks >> 2) * G::PANEL + (ks & 3) * 32) >> 4;
+                            mma_ss(lead, tm + s * 128, q + o, kd + o, id_qk, ks != 0);
+                        }
+                        tm_commit(lead, b_s + 8 * s);
+                    } else if (has_v) {
+                        tm_commit(lead, b_o + 8 * s);
+                    }
+                }
+                if (!ok) break;
+                if (has_v) tm_commit(lead, b_empty + 8 * v_slot);
+                if (has_k) tm_commit(lead, b_empty + 8 * slot);
+                if (i + LEAD == n - 1) tm_commit(lead, b_q_free);  // the unit's last scores
+            }
             wide_next(sh, U, upb);
         }
     } else {
@@ -521,32 +590,13 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             const int mu = (MT == 2 ? s * kWideTile : 0) + m;      // this thread's query row in the unit
             const int row = U.m0 + mu, t = row / P.G;
             const bool there = mu < U.mrows;
-            // query row -> swizzled shared memory (with MT = 1 the two groups take half of the chunks each)
             float f = 1.f;
-            {
+            if (DT == 2 && there) {  // the factor that the row was stored with
                 const uint16_t* q = P.Q + (long long)sh.b * P.q_sb + (long long)t * P.q_st + (long long)(U.h * P.G + row % P.G) * P.q_sh;
-                if (DT == 2) {
-                    float top = 0.f;
-                    if (there)
-                        for (int d = 0; d < D; d += 8) {
-                            const uint4 v = __ldg(reinterpret_cast<const uint4*>(q + d));
-                            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) top = fmaxf(top, fmaxf(fabsf(Elem<0>::lo(x[k])), fabsf(Elem<0>::hi(x[k]))));
-                        }
-                    const int e = (__float_as_int(top) >> 23) & 255;
-                    if (e > 0 && e < 255) f = __int_as_float(min(262 - e, 254) << 23);
-                }
-                for (int ch = MT == 2 ? 0 : s; ch < D / 8; ch += MT == 2 ? 1 : 2) {
-                    uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(q + ch * 8)) : make_uint4(0u, 0u, 0u, 0u);
-                    if (DT == 2) {
-                        uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] = MmaHalf::pack(Elem<0>::lo(x[k]) * f, Elem<0>::hi(x[k]) * f);
-                        v = make_uint4(x[0], x[1], x[2], x[3]);
-                    }
-                    *reinterpret_cast<uint4*>(smem + (MT == 2 ? s * G::SLOT : 0) + (ch >> 3) * G::PANEL + m * 128 + (((ch & 7) ^ (m & 7)) << 4)) = v;
-                }
+                float top = 0.f;
+#pragma unroll 8
+                for (int d = 0; d < D; d += 8) top = fmaxf(top, largest_of(__ldg(reinterpret_cast<const uint4*>(q + d))));
+                f = query_factor(top);
             }
             const float scl = P.scale_log2 / f;
             unsigned long long bits = 0;
@@ -561,11 +611,6 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 for (int d = 0; d < D; d += 32) tm_st32(t_o + d, z);
                 tm_wait_st();
             }
-            fence_proxy_async();
-            tm_fence_before();
-            __syncwarp();
-            if (lane == 0 && ok) mbar_arrive(b_q);
-
             float ref = -INFINITY, sum = 0.f;
             for (int k = 0; k < mine; ++k) {
                 const int i = MT == 2 ? k : 2 * k + s, r0 = (U.tile0 + i) * kWideTile;
@@ -585,18 +630,18 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                     }
                     return see;
                 };
-                // Two passes over the scores, the largest logit and then the probabilities, in short loops: an
-                // unrolled single pass that holds a tile's probabilities spills and misses in the instruction
-                // cache.  The reference moves only when a probability would pass 2^6 of what it was set for.
-                uint32_t a[32], b[32];
-                bool again = hidden;
+                // Two passes over the scores, the largest logit and then the probabilities (one pass that holds a
+                // tile's probabilities until the largest is known spills and misses in the instruction cache).
+                // The reference moves only when a probability would pass 2^6 of what it was set for.
+                uint32_t a[32], b[32], c[32];
+                float top;
                 if (!hidden) {
-                    float top[2] = {-INFINITY, -INFINITY};
+                    float t2[2] = {-INFINITY, -INFINITY};
                     auto largest = [&](const uint32_t (&x)[32]) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
-                            top[0] = fmaxf(top[0], fmaxf(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
-                            top[1] = fmaxf(top[1], fmaxf(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])));
+                            t2[0] = fmaxf(t2[0], fmaxf(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
+                            t2[1] = fmaxf(t2[1], fmaxf(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])));
                         }
                     };
                     tm_ld32(a, t_s);
@@ -606,129 +651,134 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                         tm_ld32(b, t_s + q + 32);
                         largest(a);
                         tm_wait_ld(b);
-                        tm_ld32(a, t_s + (q ^ 64));  // the next one, at the end the first one again
+                        if (q == 0) tm_ld32(a, t_s + 64);
                         largest(b);
                     }
-                    // no reference yet, or one that is too low (a NaN logit leaves it where it is)
-                    again = __any_sync(~0u, ref == -INFINITY || fmaxf(top[0], top[1]) * scl - X::kRefShift > ref + 6.f);
-                    if (!again) {
-                        const f32x2 scl2 = pack2(scl, scl), at2 = pack2(-ref, -ref);
-                        f32x2 part[2] = {0ull, 0ull};
-                        auto weigh = [&](const uint32_t (&x)[32], uint32_t to) {
-                            uint32_t p[16];
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                float p0, p1;
-                                unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), scl2, at2), p0, p1);
-                                p0 = ex2(p0);
-                                p1 = ex2(p1);
-                                part[e / 2 & 1] = add2(part[e / 2 & 1], pack2(p0, p1));
-                                p[e / 2] = X::pack(p0, p1);
-                            }
-                            tm_st16(to, p);
-                        };
+                    top = fmaxf(t2[0], t2[1]);
+                } else {
+                    // logits that this query row does not see become -infinity in place
+                    top = -INFINITY;
 #pragma unroll 1
-                        for (int q = 0; q < 128; q += 64) {
-                            tm_wait_ld(a);
-                            tm_ld32(b, t_s + q + 32);
-                            weigh(a, t_s + q / 2);
-                            tm_wait_ld(b);
-                            if (q == 0) tm_ld32(a, t_s + 64);
-                            weigh(b, t_s + q / 2 + 16);
-                        }
-                        float s0, s1;
-                        unpack2(add2(part[0], part[1]), s0, s1);
-                        sum += s0 + s1;
-                    } else {
+                    for (int q = 0; q < 4; ++q) {
+                        tm_ld32(a, t_s + 32 * q);
+                        const uint32_t see = seen32(r0 + 32 * q);
                         tm_wait_ld(a);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            if (!(see >> e & 1)) a[e] = 0xff800000u;
+                            top = fmaxf(top, __uint_as_float(a[e]));
+                        }
+                        tm_st32(t_s + 32 * q, a);
+                    }
+                    tm_wait_st();
+                }
+                top = top * scl - X::kRefShift;
+                const bool first = ref == -INFINITY, grew = top > ref + 6.f || (first && top > -INFINITY);
+                if (__any_sync(~0u, grew && !first)) {
+                    const float g = grew && !first ? ex2(ref - top) : 1.f;
+                    sum *= g;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        tm_ld32(a, t_o + d);
+                        tm_wait_ld(a);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * g);
+                        tm_st32(t_o + d, a);
+                    }
+                    tm_wait_st();
+                }
+                if (grew) ref = top;
+                const float at = ref == -INFINITY ? 0.f : ref;
+                if (draft) {
+                    // drafted rows that are not finite went into the tile as zeros: add them for those who see them
+                    const uint32_t l = c0 + load_of_v<MT>(i, U.n);
+                    wait(b_full + 8 * (l % G::NS), (l / G::NS) & 1);
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+#pragma unroll 1
+                        for (uint32_t odd = ok ? odd_rows[l % G::NS * 4 + q] : 0u; odd; odd &= odd - 1) {
+                            const int e = __ffs(int(odd)) - 1, r = r0 + 32 * q + e;
+                            const float z = __uint_as_float(tm_read1(t_s + 32 * q + e));
+                            const bool see = seen32(r0 + 32 * q) >> e & 1;
+                            const float p = see ? ex2(z * scl - at) : 0.f;
+                            const uint8_t* v = P.V + attend_offset(P, sh.b, U.h, r & ~15) + (long long)(r & 15) * P.ss;
+#pragma unroll 1
+                            for (int d = 0; d < D; d += 32) {
+                                tm_ld32(a, t_o + d);
+                                tm_wait_ld(a);
+#pragma unroll
+                                for (int x = 0; x < 32; ++x) {
+                                    float y;
+                                    if (DT == 2) {
+                                        uint32_t pr[2];
+                                        Elem<2>::expand(__ldg(v + d + x), pr);
+                                        y = Elem<1>::lo(pr[0]);
+                                    } else {
+                                        y = q_to_float(__ldg(reinterpret_cast<const uint16_t*>(v) + d + x), DT == 1);
+                                    }
+                                    if (see) a[x] = __float_as_uint(__uint_as_float(a[x]) + p * y);
+                                }
+                                tm_st32(t_o + d, a);
+                                tm_wait_st();
+                            }
+                        }
                     }
                 }
-                if (again) {
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
-                        tm_ld32(a, t_s + 32 * q);
-                        const uint32_t see = hidden ? seen32(r0 + 32 * q) : ~0u;
-                        tm_wait_ld(a);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, see >> e & 1 ? __uint_as_float(a[e]) : -INFINITY);
-                    }
-                    top = top * scl - X::kRefShift;
-                    const bool first = ref == -INFINITY, grew = top > ref + 6.f || (first && top > -INFINITY);
-                    if (__any_sync(~0u, grew && !first)) {
-                        const float g = grew && !first ? ex2(ref - top) : 1.f;
-                        sum *= g;
-#pragma unroll 1
-                        for (int d = 0; d < D; d += 32) {
-                            tm_ld32(a, t_o + d);
-                            tm_wait_ld(a);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * g);
-                            tm_st32(t_o + d, a);
-                        }
-                    }
-                    if (grew) ref = top;
-                    const float at = ref == -INFINITY ? 0.f : ref;
-                    if (draft) {
-                        // drafted rows that are not finite went into the tile as zeros: add them for those who see them
-                        const uint32_t l = c0 + load_of_v<MT>(i, U.n);
-                        wait(b_full + 8 * (l % G::NS), (l / G::NS) & 1);
-                        tm_wait_st();
-#pragma unroll 1
-                        for (int q = 0; q < 4; ++q) {
-#pragma unroll 1
-                            for (uint32_t odd = ok ? odd_rows[l % G::NS * 4 + q] : 0u; odd; odd &= odd - 1) {
-                                const int e = __ffs(int(odd)) - 1, r = r0 + 32 * q + e;
-                                const float z = __uint_as_float(tm_read1(t_s + 32 * q + e));
-                                const bool see = seen32(r0 + 32 * q) >> e & 1;
-                                const float p = see ? ex2(z * scl - at) : 0.f;
-                                const uint8_t* v = P.V + attend_offset(P, sh.b, U.h, r & ~15) + (long long)(r & 15) * P.ss;
-#pragma unroll 1
-                                for (int d = 0; d < D; d += 32) {
-                                    tm_ld32(a, t_o + d);
-                                    tm_wait_ld(a);
-#pragma unroll
-                                    for (int x = 0; x < 32; ++x) {
-                                        float y;
-                                        if (DT == 2) {
-                                            uint32_t pr[2];
-                                            Elem<2>::expand(__ldg(v + d + x), pr);
-                                            y = Elem<1>::lo(pr[0]);
-                                        } else {
-                                            y = q_to_float(__ldg(reinterpret_cast<const uint16_t*>(v) + d + x), DT == 1);
-                                        }
-                                        if (see) a[x] = __float_as_uint(__uint_as_float(a[x]) + p * y);
-                                    }
-                                    tm_st32(t_o + d, a);
-                                    tm_wait_st();
-                                }
-                            }
-                        }
-                    }
-                    float part[2] = {0.f, 0.f};
-#pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
-                        tm_ld32(a, t_s + 32 * q);
-                        const uint32_t see = hidden ? seen32(r0 + 32 * q) : ~0u;
-                        tm_wait_ld(a);
+                // tells the issuing warp that 64 more columns of probabilities are in place
+                auto hand_over = [&](uint32_t bar) {
+                    tm_wait_st();
+                    tm_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && ok) mbar_arrive(bar + 8 * s);
+                };
+                {
+                    const f32x2 scl2 = pack2(scl, scl), at2 = pack2(-at, -at);
+                    f32x2 part[2] = {0ull, 0ull};
+                    // Exponentials of 32 columns beside the sums and 16-bit forms of the 32 before them, written
+                    // in turns: the special function unit takes eight cycles for what the others do in two.
+                    auto raise = [&](uint32_t (&x)[32], int e) {
+                        float p0, p1;
+                        unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), scl2, at2), p0, p1);
+                        x[e] = __float_as_uint(ex2(p0));
+                        x[e + 1] = __float_as_uint(ex2(p1));
+                    };
+                    auto finish = [&](const uint32_t (&x)[32], uint32_t (&p)[16], int e) {
+                        const float p0 = __uint_as_float(x[e]), p1 = __uint_as_float(x[e + 1]);
+                        part[e / 2 & 1] = add2(part[e / 2 & 1], pack2(p0, p1));
+                        p[e / 2] = X::pack(p0, p1);
+                    };
+                    auto both = [&](uint32_t (&x)[32], const uint32_t (&before)[32], uint32_t to) {
                         uint32_t p[16];
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
-                            float p0 = ex2(fmaf(__uint_as_float(a[e]), scl, -at)), p1 = ex2(fmaf(__uint_as_float(a[e + 1]), scl, -at));
-                            p0 = see >> e & 1 ? p0 : 0.f;
-                            p1 = see >> (e + 1) & 1 ? p1 : 0.f;
-                            part[0] += p0;
-                            part[1] += p1;
-                            p[e / 2] = X::pack(p0, p1);
+                            raise(x, e);
+                            finish(before, p, e);
                         }
-                        tm_st16(t_s + 16 * q, p);
-                    }
-                    sum += part[0] + part[1];
+                        tm_st16(to, p);
+                    };
+                    tm_ld32(a, t_s);
+                    tm_wait_ld(a);
+                    tm_ld32(b, t_s + 32);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) raise(a, e);
+                    tm_wait_ld(b);
+                    tm_ld32(c, t_s + 64);
+                    both(b, a, t_s);
+                    tm_wait_ld(c);
+                    tm_ld32(a, t_s + 96);
+                    both(c, b, t_s + 16);
+                    hand_over(b_p);
+                    tm_wait_ld(a);
+                    both(a, c, t_s + 32);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) finish(a, p, e);
+                    tm_st16(t_s + 48, p);
+                    hand_over(b_p2);
+                    float s0, s1;
+                    unpack2(add2(part[0], part[1]), s0, s1);
+                    sum += s0 + s1;
                 }
-                tm_wait_st();
-                tm_fence_before();
-                __syncwarp();
-                if (lane == 0 && ok) mbar_arrive(b_p + 8 * s);
             }
             if (mine > 0) wait(b_o + 8 * s, no++ & 1);
 
@@ -737,8 +787,8 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             const long long first_cta = g0 / sh.per_cta, last_cta = (g0 + U.seq.tiles - 1) / sh.per_cta;
             const bool shared = first_cta != last_cta;
             float* part = P.partials + (2ll * blockIdx.x + (first_cta == (long long)blockIdx.x ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0);
-            float mref = ref, msum = sum, f_own = 1.f, f_other = 1.f;
-            if (MT == 1) {  // join the streams: stream 1 hands its O over, 64 channels at a time
+            float mref = ref, msum = sum, f_own = 1.f;
+            if (MT == 1) {  // both streams' references and sums; each finishes every other group of 32 channels
                 float2* ml = reinterpret_cast<float2*>(exch);
                 ml[s * kWideTile + m] = make_float2(ref, sum);
                 named_bar_sync(1, 256);
@@ -746,52 +796,50 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 named_bar_sync(1, 256);
                 mref = fmaxf(ref, o.x);
                 f_own = ref == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : ex2(ref - mref);
-                f_other = o.x == -INFINITY ? (o.y == 0.f ? 0.f : 1.f) : ex2(o.x - mref);
-                msum = s == 0 ? sum * f_own + o.y * f_other : 0.f;
+                const float f_other = o.x == -INFINITY ? (o.y == 0.f ? 0.f : 1.f) : ex2(o.x - mref);
+                const float own = sum * f_own, other = o.y * f_other;
+                msum = s == 0 ? own + other : other + own;
             }
-            const bool writes = there && ok && (MT == 2 || s == 0);
-#pragma unroll
-            for (int d0 = 0; d0 < D; d0 += 64) {
-                constexpr int kHalf = 64;
-                const int nd = D - d0 < kHalf ? D - d0 : kHalf;
-                if (MT == 1 && s == 1) {
-#pragma unroll
-                    for (int d = 0; d < nd; d += 32) {
-                        uint32_t a[32];
-                        tm_ld32(a, t_o + d0 + d);
+            const bool writes = there && ok;
+#pragma unroll 1
+            for (int d0 = 0; d0 < D; d0 += MT == 1 ? 64 : 32) {
+                uint32_t a[32];
+                if (MT == 1) {
+                    // hands over its part of the other's channels
+                    const int give = d0 + 32 * (s ^ 1);
+                    if (give < D) {
+                        tm_ld32(a, t_o + give);
                         tm_wait_ld(a);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) exch[(d + e) * kWideTile + m] = __uint_as_float(a[e]) * f_own;
+                        for (int e = 0; e < 32; ++e) exch[(s * 32 + e) * kWideTile + m] = __uint_as_float(a[e]) * f_own;
                     }
+                    named_bar_sync(1, 256);
                 }
-                if (MT == 1) named_bar_sync(1, 256);
-                if (MT == 2 || s == 0) {
+                const int d = d0 + (MT == 1 ? 32 * s : 0);
+                if (d < D) {
+                    tm_ld32(a, t_o + d);
+                    tm_wait_ld(a);
+                    if (MT == 1) {
 #pragma unroll
-                    for (int d = 0; d < nd; d += 32) {
-                        uint32_t a[32];
-                        tm_ld32(a, t_o + d0 + d);
-                        tm_wait_ld(a);
+                        for (int e = 0; e < 32; ++e)
+                            a[e] = __float_as_uint(__uint_as_float(a[e]) * f_own + exch[((s ^ 1) * 32 + e) * kWideTile + m]);
+                    }
+                    if (writes && shared) {  // channel by channel: a warp writes 32 rows side by side
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            float o[4];
+                        for (int e = 0; e < 32; ++e) __stcg(part + (d + e) * kWideTile + m, __uint_as_float(a[e]));
+                    } else if (writes) {
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                o[x] = __uint_as_float(a[e + x]) * f_own;
-                                if (MT == 1) o[x] += exch[(d + e + x) * kWideTile + m];
-                            }
-                            if (writes) {
-                                if (shared) {
-                                    __stcg(reinterpret_cast<float4*>(part + m * D + d0 + d + e), make_float4(o[0], o[1], o[2], o[3]));
-                                } else {
-                                    attend_write<D, DT>(P, sh.b, U.h, 0, U.m0, U.seq.tokens, mu, d0 + d + e, o, mref, msum);
-                                }
-                            }
+                        for (int e = 0; e < 32; e += 8) {
+                            float o[8];
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) o[x] = __uint_as_float(a[e + x]);
+                            attend_write<D, DT>(P, sh.b, U.h, 0, U.m0, U.seq.tokens, mu, d + e, o, mref, msum);
                         }
                     }
                 }
                 if (MT == 1) named_bar_sync(1, 256);
             }
-            if (shared && writes) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
+            if (shared && writes && (MT == 2 || s == 0)) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
             // who shares the unit, for the kernel that joins the partials: said once, by the CTA that starts it
             if (tid == 0 && first_cta == (long long)blockIdx.x)
                 P.shared[(long long)sh.b * upb + U.u] = ok ? make_int2(int(first_cta), int(last_cta)) : make_int2(0, 0);
@@ -804,52 +852,52 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     if (w == 8) tm_free(tm);
 }
 
-// Joins the partials of shared units in the order of their rows: a CTA per 16 query rows of a unit.
-constexpr int kJoinRows = 16, kJoinThreads = 256;
+// Joins the partials of shared units in the order of their rows: a CTA per 32 query rows of a unit, a lane
+// per row, a warp per eighth of the channels.
+constexpr int kJoinRows = 32, kJoinThreads = 256;
 template <int D, int DT, int MT>
 __global__ void __launch_bounds__(kJoinThreads)
 lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
-    constexpr int CHUNKS = MT * kWideTile / kJoinRows;
+    constexpr int CHUNKS = MT * kWideTile / kJoinRows, N = D / 8, PSIZE = WideGeo<D, DT, MT>::PSIZE;
     const int upb = P.H * P.mtiles, chunk = blockIdx.x % CHUNKS;
     const long long unit = blockIdx.x / CHUNKS;
-    const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, m0 = u % P.mtiles * (MT * kWideTile);
-    const int r0 = chunk * kJoinRows, rows = min(kJoinRows, P.T * P.G - m0 - r0);
-    if (rows <= 0) return;
     const int2 who = P.shared[unit];
     if (who.x == who.y) return;
+    const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, m0 = u % P.mtiles * (MT * kWideTile);
+    const int mu = chunk * kJoinRows + (threadIdx.x & 31), d0 = (threadIdx.x >> 5) * N;
+    if (m0 + mu >= P.T * P.G) return;
     const AttendSeq seq = attend_seq<kWideTile>(P, b, false);
-    const int half = r0 / kWideTile, in_half = r0 % kWideTile;
-    constexpr int PSIZE = WideGeo<D, DT, MT>::PSIZE;
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kJoinThreads) {
-        const int m = in_half + i / (D / 4), d = (i % (D / 4)) * 4;
-        float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int BATCH = 8;  // partials in flight
-        for (int c = who.x; c <= who.y; c += BATCH) {
-            float2 ml[BATCH];
-            float4 v[BATCH];
+    const float* base = P.partials + mu / kWideTile * (kWideTile * (D + 2));
+    const int m = mu % kWideTile;
+    float top = -INFINITY, total = 0.f, o[N];
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (c + k <= who.y) {
-                    const float* pp = P.partials + (2ll * (c + k) + (c + k == who.x ? 1 : 0)) * PSIZE + half * kWideTile * (D + 2);
-                    ml[k] = __ldcg(reinterpret_cast<const float2*>(pp + kWideTile * D + 2 * m));
-                    v[k] = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
-                }
-            }
+    for (int d = 0; d < N; ++d) o[d] = 0.f;
+    constexpr int BATCH = 4;  // partials in flight
+    for (int c = who.x; c <= who.y; c += BATCH) {
+        float2 ml[BATCH];
+        float v[BATCH][N];
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (c + k <= who.y && !(ml[k].x == -INFINITY && ml[k].y == 0.f)) {
-                    const float r = fmaxf(top, ml[k].x);
-                    const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml[k].x - r);
-                    total = total * fo + ml[k].y * fn;
-                    o[0] = o[0] * fo + v[k].x * fn;
-                    o[1] = o[1] * fo + v[k].y * fn;
-                    o[2] = o[2] * fo + v[k].z * fn;
-                    o[3] = o[3] * fo + v[k].w * fn;
-                    top = r;
-                }
-            }
+        for (int k = 0; k < BATCH; ++k) {
+            const float* pp = base + (2ll * min(c + k, who.y) + (c + k == who.x ? 1 : 0)) * PSIZE;
+            ml[k] = __ldcg(reinterpret_cast<const float2*>(pp + kWideTile * D + 2 * m));
+#pragma unroll
+            for (int d = 0; d < N; ++d) v[k][d] = __ldcg(pp + (d0 + d) * kWideTile + m);
         }
-        attend_write<D, DT>(P, b, h, 0, m0 + r0, seq.tokens, i / (D / 4), d, o, top, total);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (c + k > who.y || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;
+            const float r = fmaxf(top, ml[k].x);
+            const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml[k].x - r);
+            total = total * fo + ml[k].y * fn;
+#pragma unroll
+            for (int d = 0; d < N; ++d) o[d] = o[d] * fo + v[k][d] * fn;
+            top = r;
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < N; d += 4) {
+        const float x[4] = {o[d], o[d + 1], o[d + 2], o[d + 3]};
+        attend_write<D, DT>(P, b, h, 0, m0, seq.tokens, mu, d0 + d, x, top, total);
     }
 }
 

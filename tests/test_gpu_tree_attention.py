@@ -458,3 +458,13 @@ def test_wide_trees_over_many_lengths(binding, dtype, D):
         c = case(binding, len(lens), 2, G, D, 700, T, dtype, seed=T, lens=lens, drafts=drafts)
         poison(c)
         U.assert_attention(run(c), reference(c))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP8], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("T,G", [(16, 4), (40, 4)])
+def test_wide_trees_in_a_batch_of_short_sequences(binding, dtype, T, G):
+    """Several units per CTA, of one tile and of several, in every order."""
+    lens = [(40, 130, 300, 41, 129, 128, 500)[(i * i + i // 3) % 7] for i in range(300)]
+    c = case(binding, 300, 2, G, 64, 500, T, dtype, seed=T, lens=lens)
+    poison(c)
+    U.assert_attention(run(c), reference(c))
