@@ -172,28 +172,51 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendParams& P, int b, bo
     return s;
 }
 
+// a / b for 0 <= a, 0 < b: in 32 bits where they fit, which is what every real batch does
+__device__ __forceinline__ long long div_small(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)(uint32_t(a) / uint32_t(b)) : a / b;
+}
+
 // A CTA's share of the tiles: [pos, end) in the order (sequence, unit, tile); `b` and `first` are the
 // sequence that holds pos and its first tile.
 struct AttendShare {
     long long pos, end, first, per_cta;
     int b;
 };
+// `scan`: [NT / 32 + 2] words of shared memory.  Batches of up to NT sequences take one look at the lengths.
 template <int NT, int TILE = kAttendTile>
 __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int units_per_seq, long long* scan) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     constexpr int NW = NT / 32;
-    long long total = 0;
-    for (int b0 = 0; b0 < P.B; b0 += NT) {
-        const int b = b0 + tid;
-        total += b < P.B ? (long long)attend_seq<TILE>(P, b, blockIdx.x == 0).tiles * units_per_seq : 0;
+    auto tiles_of = [&](int b, bool report) { return b < P.B ? (long long)attend_seq<TILE>(P, b, report).tiles * units_per_seq : 0ll; };
+    // inclusive sum over the CTA up to this thread; `all`: over the CTA
+    auto sum_up = [&](long long n, long long* all) {
+        long long inc = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(~0u, inc, o);
+            if (lane >= o) inc += v;
+        }
+        if (lane == 31) scan[w] = inc;
+        __syncthreads();
+        *all = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            if (i == w) inc += *all;  // the warps before
+            *all += scan[i];
+        }
+        return inc;
+    };
+    long long n = tiles_of(tid, blockIdx.x == 0), all, total;
+    long long inc = sum_up(n, &all);
+    total = all;
+    for (int b0 = NT; b0 < P.B; b0 += NT) {
+        __syncthreads();
+        sum_up(tiles_of(b0 + tid, blockIdx.x == 0), &all);
+        total += all;
     }
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-    if (lane == 0) scan[w] = total;
-    __syncthreads();
-    total = 0;
-    for (int i = 0; i < NW; ++i) total += scan[i];
     AttendShare s;
-    s.per_cta = (total + gridDim.x - 1) / gridDim.x;
+    s.per_cta = div_small(total + gridDim.x - 1, gridDim.x);
     s.pos = s.per_cta * blockIdx.x;
     s.end = s.pos + s.per_cta < total ? s.pos + s.per_cta : total;
     s.b = 0;
@@ -204,27 +227,24 @@ __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int u
     }
     long long* found = scan + NW;
     long long base = 0;
-    for (int b0 = 0; b0 < P.B; b0 += NT) {
-        __syncthreads();
-        const int b = b0 + tid;
-        const long long n = b < P.B ? (long long)attend_seq<TILE>(P, b, false).tiles * units_per_seq : 0;
-        long long inc = n;
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(~0u, inc, o);
-            if (lane >= o) inc += v;
+    for (int b0 = 0;;) {
+        if (n > 0 && s.pos >= base + inc - n && s.pos < base + inc) {
+            found[0] = b0 + tid;
+            found[1] = base + inc - n;
         }
-        if (lane == 31) scan[w] = inc;
         __syncthreads();
-        long long before = base;
-        for (int i = 0; i < w; ++i) before += scan[i];
-        if (n > 0 && s.pos >= before + inc - n && s.pos < before + inc) {
-            found[0] = b;
-            found[1] = before + inc - n;
+        if (P.B <= NT) break;
+        // more sequences than threads: the groups one after the other until one holds pos
+        if (b0 == 0) {  // `all` is the last group's: the first one's again
+            inc = sum_up(n, &all);
+            __syncthreads();
         }
-        for (int i = 0; i < NW; ++i) base += scan[i];
+        base += all;
         if (base > s.pos) break;
+        b0 += NT;
+        n = tiles_of(b0 + tid, false);
+        inc = sum_up(n, &all);
     }
-    __syncthreads();
     s.b = int(found[0]);
     s.first = found[1];
     return s;
@@ -307,7 +327,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
 
     while (sh.pos < sh.end) {
         const AttendSeq seq = attend_seq(P, sh.b, false);
-        const int u = int((sh.pos - sh.first) / seq.tiles), tile0 = int((sh.pos - sh.first) % seq.tiles);
+        const int u = int(div_small(sh.pos - sh.first, seq.tiles)), tile0 = int(sh.pos - sh.first - (long long)u * seq.tiles);
         const int ntile = int(min((long long)(seq.tiles - tile0), sh.end - sh.pos));
         const int mt = u % P.mtiles, h = (u / P.mtiles) % P.H, t0 = blocks ? u / P.mtiles / P.H : 0;
         const int mrows_all = blocks ? P.G : P.T * P.G;
@@ -326,61 +346,8 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
         if (seq.tokens == 0) vrows = 0;
         const int nt16 = (max(vrows, 0) + kWarpRows - 1) / kWarpRows;
 
-        // queries, masks and row scales of the unit
-        __syncthreads();
-        {
-            constexpr int PER = G::NT / G::MR;  // threads per query row
-            const int m = tid / PER, part = tid % PER;
-            const int row = m0 + m, t = t0 + row / P.G, g = row % P.G;
-            const bool there = m < mrows;
-            const uint16_t* q = P.Q + (long long)sh.b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G + g) * P.q_sh;
-            float f = 1.f;
-            if (DT == 2) {  // largest magnitude to [2^8, 2^9)
-                float top = 0.f;
-                if (there)
-                    for (int d = part; d < D; d += PER) top = fmaxf(top, fabsf(Elem<0>::lo(__ldg(q + d))));
-#pragma unroll
-                for (int o = PER / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-                const int e = (__float_as_int(top) >> 23) & 255;
-                // e = 0: zero or subnormal, e = 255: not finite
-                if (e > 0 && e < 255) f = __int_as_float(min(262 - e, 254) << 23);
-            }
-            for (int d = part * 2; d < D; d += PER * 2) {
-                uint32_t v = there ? __ldg(reinterpret_cast<const uint32_t*>(q + d)) : 0u;
-                int at = d;
-                if (DT == 2) {
-                    v = MmaHalf::pack(Elem<0>::lo(v) * f, Elem<0>::hi(v) * f);
-                    // the order of the channels in which a word of four fp8 values meets the fragments
-                    const int c = (d & 15) >> 2, i = (d & 3) >> 1;
-                    at = (d & ~15) + 2 * c + 8 * i;
-                }
-                *reinterpret_cast<uint32_t*>(smem + G::OFF_Q + m * G::QPITCH + at * 2) = v;
-            }
-            if (part == 0) {
-                sscale[m] = P.scale_log2 / f;
-                unsigned long long bits = 0;
-                if (there && masked && t < seq.tokens)
-                    bits = P.mask ? P.mask[(long long)sh.b * P.T + t] : (t == 63 ? ~0ull : (2ull << t) - 1);
-                smask[m] = bits;
-            }
-        }
-        __syncthreads();
-
-        // ---- this warp's tiles w, w + NW, ...
-        float acc[MT][D / 8][4], ref[MT][2], sum[MT][2], scl[MT][2];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][n][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                ref[i][e] = -INFINITY;
-                sum[i][e] = 0.f;
-                scl[i][e] = sscale[i * 16 + (lane >> 2) + 8 * e];
-            }
-        }
+        // ---- this warp's tiles w, w + NW, ... ; the first are on their way before anything else
+        __syncthreads();  // the ring holds nothing of the unit before
         const int mine = (nt16 - w + G::NW - 1) / G::NW;  // tiles of this warp (<= 0: none)
         // lane l: byte offset (-1: not there) and first row of this warp's tile 32 * (i / 32) + l, looked up
         // 32 tiles at a time so that the chain of table reads is not paid per tile
@@ -422,6 +389,59 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
         };
 #pragma unroll 1
         for (int i = 0; i < G::STAGES - 1; ++i) issue(i);
+        // queries, masks and row scales of the unit
+        {
+            constexpr int PER = G::NT / G::MR;  // threads per query row
+            const int m = tid / PER, part = tid % PER;
+            const int row = m0 + m, t = t0 + row / P.G, g = row % P.G;
+            const bool there = m < mrows;
+            const uint16_t* q = P.Q + (long long)sh.b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G + g) * P.q_sh;
+            float f = 1.f;
+            if (DT == 2) {  // largest magnitude to [2^8, 2^9)
+                float top = 0.f;
+                if (there)
+                    for (int d = part; d < D; d += PER) top = fmaxf(top, fabsf(Elem<0>::lo(__ldg(q + d))));
+#pragma unroll
+                for (int o = PER / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+                const int e = (__float_as_int(top) >> 23) & 255;
+                // e = 0: zero or subnormal, e = 255: not finite
+                if (e > 0 && e < 255) f = __int_as_float(min(262 - e, 254) << 23);
+            }
+            for (int d = part * 2; d < D; d += PER * 2) {
+                uint32_t v = there ? __ldg(reinterpret_cast<const uint32_t*>(q + d)) : 0u;
+                int at = d;
+                if (DT == 2) {
+                    v = MmaHalf::pack(Elem<0>::lo(v) * f, Elem<0>::hi(v) * f);
+                    // the order of the channels in which a word of four fp8 values meets the fragments
+                    const int c = (d & 15) >> 2, i = (d & 3) >> 1;
+                    at = (d & ~15) + 2 * c + 8 * i;
+                }
+                *reinterpret_cast<uint32_t*>(smem + G::OFF_Q + m * G::QPITCH + at * 2) = v;
+            }
+            if (part == 0) {
+                sscale[m] = P.scale_log2 / f;
+                unsigned long long bits = 0;
+                if (there && masked && t < seq.tokens)
+                    bits = P.mask ? P.mask[(long long)sh.b * P.T + t] : (t == 63 ? ~0ull : (2ull << t) - 1);
+                smask[m] = bits;
+            }
+        }
+        __syncthreads();
+
+        float acc[MT][D / 8][4], ref[MT][2], sum[MT][2], scl[MT][2];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][n][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                ref[i][e] = -INFINITY;
+                sum[i][e] = 0.f;
+                scl[i][e] = sscale[i * 16 + (lane >> 2) + 8 * e];
+            }
+        }
 #pragma unroll 1
         for (int i = 0; i < mine; ++i) {
             issue(i + G::STAGES - 1);
@@ -635,7 +655,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
 
         // who shares this unit: CTAs c0 .. c1
         const long long g0 = sh.first + (long long)u * seq.tiles;
-        const long long c0 = g0 / sh.per_cta, c1 = (g0 + seq.tiles - 1) / sh.per_cta;
+        const long long c0 = div_small(g0, sh.per_cta), c1 = div_small(g0 + seq.tiles - 1, sh.per_cta);
         constexpr int PSIZE = G::MR * (D + 2);
         float* part = P.partials + (2ll * blockIdx.x + (c0 == (long long)blockIdx.x ? 1 : 0)) * PSIZE;
         for (int i = tid; i < mrows * (D / 4); i += G::NT) {

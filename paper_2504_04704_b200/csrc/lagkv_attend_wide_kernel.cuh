@@ -162,8 +162,8 @@ template <class G>
 __device__ __forceinline__ WideUnit wide_unit(const AttendParams& P, const AttendShare& sh) {
     WideUnit w;
     w.seq = attend_seq<kWideTile>(P, sh.b, false);
-    w.u = int((sh.pos - sh.first) / w.seq.tiles);
-    w.tile0 = int((sh.pos - sh.first) % w.seq.tiles);
+    w.u = int(div_small(sh.pos - sh.first, w.seq.tiles));
+    w.tile0 = int(sh.pos - sh.first - (long long)w.u * w.seq.tiles);
     w.n = int(min((long long)(w.seq.tiles - w.tile0), sh.end - sh.pos));
     w.h = w.u / P.mtiles % P.H;
     w.m0 = w.u % P.mtiles * (G::MT * kWideTile);
@@ -784,7 +784,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
 
             // ---- the unit's result
             const long long g0 = sh.first + (long long)U.u * U.seq.tiles;
-            const long long first_cta = g0 / sh.per_cta, last_cta = (g0 + U.seq.tiles - 1) / sh.per_cta;
+            const long long first_cta = div_small(g0, sh.per_cta), last_cta = div_small(g0 + U.seq.tiles - 1, sh.per_cta);
             const bool shared = first_cta != last_cta;
             float* part = P.partials + (2ll * blockIdx.x + (first_cta == (long long)blockIdx.x ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0);
             float mref = ref, msum = sum, f_own = 1.f;
