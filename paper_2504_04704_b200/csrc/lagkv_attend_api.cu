@@ -140,6 +140,7 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     P->partials = reinterpret_cast<float*>(base + kHead + cb);
     P->shared = reinterpret_cast<int2*>(base + kHead + cb + partial_bytes(plan, *e));
     P->mtiles = (query_rows + e->rows - 1) / e->rows;
+    P->lead = e->wide ? kWideLead : kAttendLead;
     *entry = e;
     *rest = base + kHead + cb + pb;
     if (!(plan->attend_ready.load(std::memory_order_acquire) >> index & 1)) {

@@ -38,12 +38,14 @@ struct AttendParams {
     long long q_sb, q_st, q_sh;         // elements
     int B, H, G, T, S_cap, max_blocks, page_shift;
     int mtiles;            // groups of M rows per (sequence, KV head)
+    int lead;              // what beginning a unit costs, in tiles: counted when the work is shared out
     float scale_log2, v_scale;
     const int32_t* idx;    // blocks: [B, T, H, keep] ascending block numbers, -1 behind the last
     int keep, block_shift;
 };
 
 constexpr int kAttendTile = 64;     // rows of the unit of scheduling (lagkv_attend_kernel)
+constexpr int kAttendLead = 8;      // P.lead: 16 caches of 16384 rows in 80 us, 85 with equal shares of the rows
 constexpr int kAttendWarps = 4;
 constexpr int kWarpRows = 16;       // rows of a warp's tile: never across a page or a block (both >= 16)
 
@@ -177,18 +179,48 @@ __device__ __forceinline__ long long div_small(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? (long long)(uint32_t(a) / uint32_t(b)) : a / b;
 }
 
-// A CTA's share of the tiles: [pos, end) in the order (sequence, unit, tile); `b` and `first` are the
-// sequence that holds pos and its first tile.
+// A CTA's share of the tiles: [pos, end) in the order (sequence, unit, tile), where each unit begins with
+// P.lead tiles of no rows, so that a CTA which drains one unit and begins another gets fewer rows; `b` and
+// `first` are the sequence that holds pos and its first tile.
 struct AttendShare {
     long long pos, end, first, per_cta;
     int b;
 };
+// The part of a share that lies in one unit.
+struct AttendPart {
+    int u;               // unit of the sequence
+    int tile0, n;        // tiles with rows (n = 0: none)
+    int step;            // tiles to go on by, those of no rows too
+    long long c0, c1;    // first and last CTA that have rows of the unit
+};
+__device__ __forceinline__ AttendPart attend_part(const AttendParams& P, const AttendShare& sh, int tiles) {
+    AttendPart a;
+    const int all = tiles + P.lead;
+    a.u = int(div_small(sh.pos - sh.first, all));
+    const long long begin = sh.first + (long long)a.u * all;
+    const int v0 = int(sh.pos - begin);
+    a.step = int(min((long long)(all - v0), sh.end - sh.pos));
+    a.tile0 = max(0, v0 - P.lead);
+    a.n = max(0, v0 + a.step - P.lead - a.tile0);
+    a.c0 = div_small(begin + P.lead, sh.per_cta);
+    a.c1 = div_small(begin + all - 1, sh.per_cta);
+    return a;
+}
+__device__ __forceinline__ void attend_advance(const AttendParams& P, AttendShare& sh, int step, int tiles, int units_per_seq) {
+    sh.pos += step;
+    if (sh.pos == sh.first + (long long)units_per_seq * (tiles + P.lead)) {
+        sh.first = sh.pos;
+        ++sh.b;
+    }
+}
 // `scan`: [NT / 32 + 2] words of shared memory.  Batches of up to NT sequences take one look at the lengths.
 template <int NT, int TILE = kAttendTile>
 __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int units_per_seq, long long* scan) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     constexpr int NW = NT / 32;
-    auto tiles_of = [&](int b, bool report) { return b < P.B ? (long long)attend_seq<TILE>(P, b, report).tiles * units_per_seq : 0ll; };
+    auto tiles_of = [&](int b, bool report) {
+        return b < P.B ? (long long)(attend_seq<TILE>(P, b, report).tiles + P.lead) * units_per_seq : 0ll;
+    };
     // inclusive sum over the CTA up to this thread; `all`: over the CTA
     auto sum_up = [&](long long n, long long* all) {
         long long inc = n;
@@ -289,19 +321,29 @@ __device__ __forceinline__ void attend_combine(const AttendParams& P, int b, int
     for (int i = tid; i < mrows * (D / 4); i += threads) {
         const int m = i / (D / 4), d = (i % (D / 4)) * 4;
         float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (long long c = c0; c <= c1; ++c) {
-            const float* pp = P.partials + (2 * c + (c == c0 ? 1 : 0)) * (MR * (D + 2));
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp + MR * D + 2 * m));
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;
-            const float r = fmaxf(top, ml.x);
-            const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml.x - r);
-            total = total * fo + ml.y * fn;
-            o[0] = o[0] * fo + v.x * fn;
-            o[1] = o[1] * fo + v.y * fn;
-            o[2] = o[2] * fo + v.z * fn;
-            o[3] = o[3] * fo + v.w * fn;
-            top = r;
+        constexpr int BATCH = 4;  // partials in flight: one after the other each costs an L2 round trip
+        for (long long c = c0; c <= c1; c += BATCH) {
+            float2 ml[BATCH];
+            float4 v[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const long long from = min(c + k, c1);
+                const float* pp = P.partials + (2 * from + (from == c0 ? 1 : 0)) * (MR * (D + 2));
+                ml[k] = __ldcg(reinterpret_cast<const float2*>(pp + MR * D + 2 * m));
+                v[k] = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (c + k > c1 || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;
+                const float r = fmaxf(top, ml[k].x);
+                const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml[k].x - r);
+                total = total * fo + ml[k].y * fn;
+                o[0] = o[0] * fo + v[k].x * fn;
+                o[1] = o[1] * fo + v[k].y * fn;
+                o[2] = o[2] * fo + v[k].z * fn;
+                o[3] = o[3] * fo + v[k].w * fn;
+                top = r;
+            }
         }
         attend_write<D, DT>(P, b, h, t0, m0, tokens, m, d, o, top, total);
     }
@@ -327,8 +369,12 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
 
     while (sh.pos < sh.end) {
         const AttendSeq seq = attend_seq(P, sh.b, false);
-        const int u = int(div_small(sh.pos - sh.first, seq.tiles)), tile0 = int(sh.pos - sh.first - (long long)u * seq.tiles);
-        const int ntile = int(min((long long)(seq.tiles - tile0), sh.end - sh.pos));
+        const AttendPart part_of = attend_part(P, sh, seq.tiles);
+        const int u = part_of.u, tile0 = part_of.tile0, ntile = part_of.n;
+        if (ntile == 0) {
+            attend_advance(P, sh, part_of.step, seq.tiles, upb);
+            continue;
+        }
         const int mt = u % P.mtiles, h = (u / P.mtiles) % P.H, t0 = blocks ? u / P.mtiles / P.H : 0;
         const int mrows_all = blocks ? P.G : P.T * P.G;
         const int m0 = mt * G::MR, mrows = min(G::MR, mrows_all - m0);
@@ -654,8 +700,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
         __syncthreads();
 
         // who shares this unit: CTAs c0 .. c1
-        const long long g0 = sh.first + (long long)u * seq.tiles;
-        const long long c0 = div_small(g0, sh.per_cta), c1 = div_small(g0 + seq.tiles - 1, sh.per_cta);
+        const long long c0 = part_of.c0, c1 = part_of.c1;
         constexpr int PSIZE = G::MR * (D + 2);
         float* part = P.partials + (2ll * blockIdx.x + (c0 == (long long)blockIdx.x ? 1 : 0)) * PSIZE;
         for (int i = tid; i < mrows * (D / 4); i += G::NT) {
@@ -698,11 +743,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
                 attend_combine<D, DT, G::MR>(P, sh.b, h, t0, m0, mrows, seq.tokens, c0, c1, tid, G::NT);
             }
         }
-        sh.pos += ntile;
-        if (sh.pos == sh.first + (long long)upb * seq.tiles) {
-            sh.first = sh.pos;
-            ++sh.b;
-        }
+        attend_advance(P, sh, part_of.step, seq.tiles, upb);
     }
 }
 

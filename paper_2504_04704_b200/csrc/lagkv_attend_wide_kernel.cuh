@@ -24,6 +24,7 @@
 namespace lagkv {
 
 constexpr int kWideTile = 128;        // rows of K and V per step
+constexpr int kWideLead = 6;          // P.lead: 32 tokens over 16 x 9728 rows in 101 us, 108 with equal shares
 constexpr int kWideRowFlags = 32;     // loads whose missing rows are remembered: more than the rings hold
 
 template <int D_, int DT_, int MT_>
@@ -37,7 +38,9 @@ struct WideGeo {
     static constexpr int EXCH = 64 * kWideTile * 4;    // MT = 1: 32 channels of each stream's O for the other
     static constexpr int QBYTES = MT == 2 ? 2 * SLOT : SLOT + EXCH;
     static constexpr int WARPS = DT_ == 2 ? 16 : 12;   // widening takes seven warps to keep up
-    static constexpr int NT = WARPS * 32, HELP = NT - 10 * 32;  // threads that load queries, mend and widen
+    static constexpr int NT = WARPS * 32;
+    // Warps 10 ..: load queries; mend V tiles (16-bit), or widen in two groups, one for K and one for V tiles
+    static constexpr int HELP_WARPS = WARPS - 10, GROUPS = DT_ == 2 ? 2 : 1, HELP = HELP_WARPS / GROUPS * 32;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
     static constexpr int RS = DT_ == 2 ? 4 : 0;                  // ... and how many are in flight
@@ -155,6 +158,7 @@ __device__ __forceinline__ int load_of_v(int i, int n) { return MT == 2 ? 2 * i 
 struct WideUnit {
     AttendSeq seq;
     int u, h, m0, mrows, tile0, n;  // n: steps of this share
+    int step, first_cta, last_cta;
     int lim, base;                  // rows seen at all, first drafted row
     bool masked;
 };
@@ -162,9 +166,13 @@ template <class G>
 __device__ __forceinline__ WideUnit wide_unit(const AttendParams& P, const AttendShare& sh) {
     WideUnit w;
     w.seq = attend_seq<kWideTile>(P, sh.b, false);
-    w.u = int(div_small(sh.pos - sh.first, w.seq.tiles));
-    w.tile0 = int(sh.pos - sh.first - (long long)w.u * w.seq.tiles);
-    w.n = int(min((long long)(w.seq.tiles - w.tile0), sh.end - sh.pos));
+    const AttendPart a = attend_part(P, sh, w.seq.tiles);
+    w.u = a.u;
+    w.tile0 = a.tile0;
+    w.n = a.n;
+    w.step = a.step;
+    w.first_cta = int(a.c0);
+    w.last_cta = int(a.c1);
     w.h = w.u / P.mtiles % P.H;
     w.m0 = w.u % P.mtiles * (G::MT * kWideTile);
     w.mrows = min(G::MT * kWideTile, P.T * P.G - w.m0);
@@ -173,12 +181,22 @@ __device__ __forceinline__ WideUnit wide_unit(const AttendParams& P, const Atten
     w.masked = P.mask != nullptr || w.seq.tokens > 1;
     return w;
 }
-__device__ __forceinline__ void wide_next(AttendShare& sh, const WideUnit& w, int units_per_seq) {
-    sh.pos += w.n;
-    if (sh.pos == sh.first + (long long)units_per_seq * w.seq.tiles) {
-        sh.first = sh.pos;
-        ++sh.b;
-    }
+// Goes on to the next unit with rows (`w` is the present one, or any when n == 0); false: none.
+template <class G>
+__device__ __forceinline__ bool wide_next(const AttendParams& P, AttendShare& sh, WideUnit& w, int units_per_seq) {
+    do {
+        attend_advance(P, sh, w.step, w.seq.tiles, units_per_seq);
+        if (sh.pos >= sh.end) return false;
+        w = wide_unit<G>(P, sh);
+    } while (w.n == 0);
+    return true;
+}
+// The first unit with rows.
+template <class G>
+__device__ __forceinline__ bool wide_first(const AttendParams& P, AttendShare& sh, WideUnit& w, int units_per_seq) {
+    if (sh.pos >= sh.end) return false;
+    w = wide_unit<G>(P, sh);
+    return w.n > 0 || wide_next<G>(P, sh, w, units_per_seq);
 }
 
 // fp8 caches: the power of two that brings a row of bf16 queries to [2^8, 2^9), and its largest magnitude.
@@ -245,20 +263,18 @@ struct WideCursor {
     int l;       // load of the unit
     uint32_t c;  // loads before this one
     bool more;
-    __device__ __forceinline__ void start(const AttendParams& P, const AttendShare& s) {
+    __device__ __forceinline__ void start(const AttendShare& s, const WideUnit& u, bool any) {
         sh = s;
+        U = u;
         l = 0;
         c = 0;
-        more = sh.pos < sh.end;
-        if (more) U = wide_unit<G>(P, sh);
+        more = any;
     }
     __device__ __forceinline__ void next(const AttendParams& P, int units_per_seq) {
         ++c;
         if (++l == 2 * U.n) {
             l = 0;
-            wide_next(sh, U, units_per_seq);
-            more = sh.pos < sh.end;
-            if (more) U = wide_unit<G>(P, sh);
+            more = wide_next<G>(P, sh, U, units_per_seq);
         }
     }
     __device__ __forceinline__ bool is_v() const {
@@ -310,7 +326,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         }
         for (int i = 0; i < (DT == 2 ? G::RS : G::NS); ++i) mbar_init(b_land + 8 * i, 1);
         for (int i = 0; i < G::RS; ++i) mbar_init(b_raw_free + 8 * i, 1);
-        mbar_init(b_q, G::HELP / 32);
+        mbar_init(b_q, G::HELP_WARPS);
         mbar_init(b_q_free, 1);
         fence_mbar_init();
     }
@@ -321,7 +337,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     }
     const int upb = P.H * P.mtiles;
     AttendShare sh = attend_share<G::NT, kWideTile>(P, upb, scan);
-    if (sh.pos < sh.end) load_queries<G>(P, wide_unit<G>(P, sh), sh.b, smem, w, G::WARPS);  // the first unit's, by all
+    WideUnit U;
+    bool any = wide_first<G>(P, sh, U, upb);
+    if (any) load_queries<G>(P, U, sh.b, smem, w, G::WARPS);  // the first unit's, by all
     __syncthreads();
     tm_fence_after();
     const uint32_t tm = __shfl_sync(~0u, *reinterpret_cast<volatile uint32_t*>(tm_slot), 0);
@@ -338,7 +356,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         const int box = lane / BP, panel = lane % BP;
         const uint32_t box_bytes = uint32_t(box_rows) * (DT == 2 ? G::ROWB : 128);
         WideCursor<G> at;
-        at.start(P, sh);
+        at.start(sh, U, any);
         for (; at.more; at.next(P, upb)) {
             const int row = at.row0() + box * box_rows;
             bool there = box < kWideTile / box_rows && row < at.U.lim;
@@ -388,7 +406,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         }
     } else if (w > 9) {
         // ------------------------------------------------------------------ help
-        const int ptid = tid - 10 * 32;
+        const int group = (w - 10) / (G::HELP / 32), ptid = tid - 10 * 32 - group * G::HELP;  // group 0 the V tiles, 1 the K tiles
         // after a wait that ran out the walk goes on to its end without waiting, so that the barrier among these
         // warps still matches
         auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -397,7 +415,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 ok = false;
             }
         };
-        auto meet = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(G::HELP) : "memory"); };
+        auto meet = [&]() { named_bar_sync(2 + group, G::HELP); };
         auto not_finite = [](const uint4& v) {
             const uint32_t x[4] = {v.x, v.y, v.z, v.w};
             bool odd = false;
@@ -442,20 +460,23 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         };
         uint32_t landed = 0, units = 0;  // parities of the places where tiles land; units behind
         WideCursor<G> at;
-        at.start(P, sh);
+        at.start(sh, U, any);
         for (; at.more; at.next(P, upb)) {
             if (at.l == 0 && at.c > 0) {  // the next unit's queries, once the products with those before are done
                 wait(b_q_free, units++ & 1);
-                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, G::HELP / 32);
+                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, G::HELP_WARPS);
                 __syncwarp();
                 if (lane == 0 && ok) mbar_arrive(b_q);
             }
-            if (DT != 2 && !at.is_v()) continue;
+            const int place = DT == 2 ? int(at.c % (G::RS ? G::RS : 1)) : int(at.c % G::NS);
+            if (at.is_v() != (group == 0)) {
+                if (DT == 2) landed ^= 1u << place;  // the other group's
+                continue;
+            }
             const int slot = int(at.c % G::NS);
             const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
             const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
             if (DT != 2 && !mend) continue;
-            const int place = DT == 2 ? int(at.c % (G::RS ? G::RS : 1)) : slot;
             wait(b_land + 8 * place, landed >> place & 1);
             landed ^= 1u << place;
             unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
@@ -471,7 +492,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 if (at.c >= uint32_t(G::NS)) wait(b_empty + 8 * slot, (at.c / G::NS + 1) & 1);
                 const unsigned char* from = smem + (s_raw - sbase) + place * G::RAW;
                 if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
-#pragma unroll 2
+#pragma unroll 4
                 for (int id = ptid; id < G::CHUNKS; id += G::HELP) {
                     const int r = id / G::CPR, ch = id % G::CPR;
                     uint4 x = *reinterpret_cast<const uint4*>(from + id * 16);
@@ -514,11 +535,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             return wait(b_full + 8 * slot, phase);
         };
-        const long long begin = sh.pos;
-        while (ok && sh.pos < sh.end) {
-            const WideUnit U = wide_unit<G>(P, sh);
+        for (bool first = true; ok && any; first = false) {
             const int n = __shfl_sync(~0u, U.n, 0);
-            if (sh.pos != begin) {  // the first unit's queries are there
+            if (!first) {  // the first unit's queries are there
                 if (!wait(b_q, nq)) break;
                 nq ^= 1;
             }
@@ -568,7 +587,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 if (has_k) tm_commit(lead, b_empty + 8 * slot);
                 if (i + LEAD == n - 1) tm_commit(lead, b_q_free);  // the unit's last scores
             }
-            wide_next(sh, U, upb);
+            any = wide_next<G>(P, sh, U, upb);
         }
     } else {
         // ------------------------------------------------------------------ softmax of a stream
@@ -584,8 +603,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             tm_fence_after();
         };
-        for (; sh.pos < sh.end;) {
-            const WideUnit U = wide_unit<G>(P, sh);
+        while (any) {
             const int mine = (MT == 2 ? U.n : (U.n - s + 1) / 2);  // steps of this stream
             const int mu = (MT == 2 ? s * kWideTile : 0) + m;      // this thread's query row in the unit
             const int row = U.m0 + mu, t = row / P.G;
@@ -783,10 +801,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             if (mine > 0) wait(b_o + 8 * s, no++ & 1);
 
             // ---- the unit's result
-            const long long g0 = sh.first + (long long)U.u * U.seq.tiles;
-            const long long first_cta = div_small(g0, sh.per_cta), last_cta = div_small(g0 + U.seq.tiles - 1, sh.per_cta);
+            const int first_cta = U.first_cta, last_cta = U.last_cta;
             const bool shared = first_cta != last_cta;
-            float* part = P.partials + (2ll * blockIdx.x + (first_cta == (long long)blockIdx.x ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0);
+            float* part = P.partials + (2ll * blockIdx.x + (first_cta == int(blockIdx.x) ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0);
             float mref = ref, msum = sum, f_own = 1.f;
             if (MT == 1) {  // both streams' references and sums; each finishes every other group of 32 channels
                 float2* ml = reinterpret_cast<float2*>(exch);
@@ -841,10 +858,10 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             if (shared && writes && (MT == 2 || s == 0)) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
             // who shares the unit, for the kernel that joins the partials: said once, by the CTA that starts it
-            if (tid == 0 && first_cta == (long long)blockIdx.x)
-                P.shared[(long long)sh.b * upb + U.u] = ok ? make_int2(int(first_cta), int(last_cta)) : make_int2(0, 0);
+            if (tid == 0 && first_cta == int(blockIdx.x))
+                P.shared[(long long)sh.b * upb + U.u] = ok ? make_int2(first_cta, last_cta) : make_int2(0, 0);
             c0 += 2 * U.n;
-            wide_next(sh, U, upb);
+            any = wide_next<G>(P, sh, U, upb);
         }
     }
     tm_fence_before();
