@@ -48,10 +48,27 @@ long long attend_units(const lagkv_plan_s* plan, const AttendEntry& e, int query
 bool query_shape_ok(const lagkv_config& c, int T, int H_q) {
     return T >= 1 && T <= 64 && H_q >= c.H_kv && H_q % c.H_kv == 0 && H_q / c.H_kv <= 64;
 }
+// The choice of blocks: [chosen | 64-bit scores | 32-bit scores | how far these can be off]
+struct ChoiceLayout {
+    size_t keys, approx, error, total;
+    ChoiceLayout(const lagkv_config& c, int T, int64_t blocks, int keep) {
+        const size_t units = size_t(c.B) * T * c.H_kv;
+        keys = up256(units * size_t(keep) * sizeof(int32_t));
+        approx = keys + up256(units * size_t(blocks) * sizeof(unsigned long long));
+        error = approx + up256(units * size_t(blocks) * sizeof(float));
+        total = error + up256(units * (size_t(blocks) / kScoreChunk + 1) * sizeof(float));
+    }
+};
 size_t choice_bytes(const lagkv_config& c, int T, int64_t blocks, int keep) {
-    if (blocks == 0) return 0;
-    const size_t units = size_t(c.B) * T * c.H_kv;
-    return up256(units * size_t(keep) * sizeof(int32_t)) + up256(units * size_t(blocks) * sizeof(double));
+    return blocks == 0 ? 0 : ChoiceLayout(c, T, blocks, keep).total;
+}
+
+template <int DT>
+const void* score_kernel(int D) {
+    return D == 64    ? reinterpret_cast<const void*>(&lagkv_block_score_kernel<DT, 64>)
+           : D == 96  ? reinterpret_cast<const void*>(&lagkv_block_score_kernel<DT, 96>)
+           : D == 128 ? reinterpret_cast<const void*>(&lagkv_block_score_kernel<DT, 128>)
+                      : reinterpret_cast<const void*>(&lagkv_block_score_kernel<DT, 256>);
 }
 
 int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, void* out, float* lse, AttendParams* P) {
@@ -194,7 +211,8 @@ int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cuda
         return LAGKV_ECUDA;
     if (e.join != nullptr) {
         const long long ctas = (long long)P.B * P.H * P.mtiles * (e.rows / kJoinRows);
-        if (cudaLaunchKernel(e.join, dim3((unsigned)ctas), dim3(kJoinThreads), args, 0, stream) != cudaSuccess) return LAGKV_ECUDA;
+        const int rc = launch_behind(e.join, unsigned(ctas), kJoinThreads, args, 0, stream);
+        if (rc != LAGKV_OK) return rc;
     }
     return check_launch();
 }
@@ -307,38 +325,50 @@ int attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block
     P.seq_len = seq_len;
     P.keep = choice->keep;
     const long long units = (long long)P.B * P.T * P.H;
-    const int chunks = int((choice->blocks + kScoreBlocks - 1) / kScoreBlocks);
-    if (units * chunks > 0x7fffffffll) return LAGKV_EINVAL;
+    // blocks per CTA of the score kernel: few for one user's latency, more where CTAs abound
+    ScoreShape S;
+    S.blocks = choice->blocks;
+    const long long small = units * ((choice->blocks + kScoreChunk - 1) / kScoreChunk) / (8ll * plan->sm_count);
+    S.chunk = kScoreChunk * int(small < 1 ? 1 : small > 8 ? 8 : small);
+    S.chunks = int((choice->blocks + S.chunk - 1) / S.chunk);
+    if (units * S.chunks > 0x7fffffffll) return LAGKV_EINVAL;
     DeviceGuard guard(c.device);
     const AttendEntry* e;
     unsigned char* rest;
     rc = attend_prepare(plan, P.G, P.T, true, choice_bytes(c, P.T, choice->blocks, choice->keep), workspace, bytes, &P, &e, &rest);
     if (rc != LAGKV_OK) return rc;
+    const ChoiceLayout lay(c, P.T, choice->blocks, choice->keep);
     int32_t* idx = idx_out ? idx_out : reinterpret_cast<int32_t*>(rest);
-    unsigned long long* keys = reinterpret_cast<unsigned long long*>(rest + up256(size_t(units) * P.keep * sizeof(int32_t)));
+    unsigned long long* keys = reinterpret_cast<unsigned long long*>(rest + lay.keys);
+    S.approx = reinterpret_cast<float*>(rest + lay.approx);
+    S.error = reinterpret_cast<float*>(rest + lay.error);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const uint8_t* bd = static_cast<const uint8_t*>(bounds);
-    const size_t score_smem = size_t(kScoreHeads) * (c.D + 2) * sizeof(double);
-    const dim3 sgrid((unsigned)(units * chunks));
-    if (c.dtype == LAGKV_DTYPE_BF16)
-        lagkv_block_score_kernel<0><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
-    else if (c.dtype == LAGKV_DTYPE_FP16)
-        lagkv_block_score_kernel<1><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
-    else
-        lagkv_block_score_kernel<2><<<sgrid, kScoreThreads, score_smem, stream>>>(P, bd, choice->blocks, chunks, c.D, keys);
-    const size_t select_smem = size_t(choice->blocks) * sizeof(unsigned long long);
+    const bool bf16 = c.dtype == LAGKV_DTYPE_BF16, fp16 = c.dtype == LAGKV_DTYPE_FP16;
+    const void* score = bf16 ? score_kernel<0>(c.D) : fp16 ? score_kernel<1>(c.D) : score_kernel<2>(c.D);
+    const void* select = bf16   ? reinterpret_cast<const void*>(&lagkv_block_select_kernel<0>)
+                         : fp16 ? reinterpret_cast<const void*>(&lagkv_block_select_kernel<1>)
+                                : reinterpret_cast<const void*>(&lagkv_block_select_kernel<2>);
+    const size_t select_smem = size_t(choice->blocks) * 8;  // a score and a number each
     constexpr unsigned long long kSelectReady = 1ull << 63;
     if (!(plan->attend_ready.load(std::memory_order_acquire) & kSelectReady)) {
-        if (!raise_smem_limit(reinterpret_cast<const void*>(&lagkv_block_select_kernel), size_t(kMaxBlocks) * sizeof(unsigned long long)))
-            return LAGKV_ECUDA;
+        if (!raise_smem_limit(select, size_t(kMaxBlocks) * 8)) return LAGKV_ECUDA;
         plan->attend_ready.fetch_or(kSelectReady, std::memory_order_release);
     }
-    lagkv_block_select_kernel<<<dim3((unsigned)units), kSelectThreads, select_smem, stream>>>(
-        P, keys, choice->blocks, choice->sink_blocks, choice->recent_blocks, idx);
-    rc = check_launch();
-    if (rc != LAGKV_OK) return rc;
+    {
+        void* args[] = {&P, &bd, &S};
+        if (cudaLaunchKernel(score, dim3((unsigned)(units * S.chunks)), dim3(kScoreThreads), args, 0, stream) != cudaSuccess) return LAGKV_ECUDA;
+    }
+    {
+        int D = c.D, sink = choice->sink_blocks, recent = choice->recent_blocks;
+        void* args[] = {&P, &bd, &S, &D, &keys, &sink, &recent, &idx};
+        rc = launch_behind(select, unsigned(units), kSelectThreads, args, select_smem, stream);
+        if (rc != LAGKV_OK) return rc;
+    }
     P.idx = idx;
-    return attend_launch(plan, *e, P, stream);
+    void* args[] = {&P};
+    rc = launch_behind(e->fn, unsigned(plan->sm_count * e->ctas_per_sm), unsigned(e->threads), args, e->smem, stream);
+    return rc == LAGKV_OK ? check_launch() : rc;
 }
 
 }  // namespace

@@ -366,6 +366,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
     const bool blocks = P.idx != nullptr;
     const int upb = (blocks ? P.T : 1) * P.H * P.mtiles;  // units of a sequence
     AttendShare sh = attend_share<G::NT>(P, upb, sscan);
+    if (blocks) asm volatile("griddepcontrol.wait;" ::: "memory");  // the choice
 
     while (sh.pos < sh.end) {
         const AttendSeq seq = attend_seq(P, sh.b, false);

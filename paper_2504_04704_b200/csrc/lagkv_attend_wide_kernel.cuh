@@ -297,6 +297,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     using G = WideGeo<D, DT, MT>;
     using X = Mma<DT>;
     extern __shared__ unsigned char raw[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, w = __shfl_sync(~0u, tid >> 5, 0);  // the same in all lanes, visibly
     const uint32_t sbase = (smem_u32(raw) + 1023u) & ~1023u;
     unsigned char* smem = raw + (sbase - smem_u32(raw));
@@ -878,6 +879,7 @@ lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
     constexpr int CHUNKS = MT * kWideTile / kJoinRows, N = D / 8, PSIZE = WideGeo<D, DT, MT>::PSIZE;
     const int upb = P.H * P.mtiles, chunk = blockIdx.x % CHUNKS;
     const long long unit = blockIdx.x / CHUNKS;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials
     const int2 who = P.shared[unit];
     if (who.x == who.y) return;
     const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, m0 = u % P.mtiles * (MT * kWideTile);

@@ -4,7 +4,10 @@
 // minimum and maximum of its K rows, in the storage format (no rounding).  For a query q every logit of
 // the block is at most  sum_c max(q_c * min_c, q_c * max_c);  a block's score is the largest such bound
 // over the query heads of the KV head.  Scores that decide which blocks are read may differ in their last
-// bits only, so they are summed in 64 bits: the choice does not depend on the order of the sums.
+// bits only, so the choice is that of scores summed in 64 bits.  Nearly all blocks are far from the border,
+// though: scores are first summed in 32 bits, with a bound E on how far off they can be, and only blocks
+// within 2 E of the border are summed again in 64 (all in 64 bits took 49 us for eight caches of 2048 blocks,
+// where the bounds are read in 10).
 #pragma once
 #include "lagkv_attend_kernels.cuh"
 
@@ -12,8 +15,8 @@ namespace lagkv {
 
 constexpr int kBoundsThreads = 256;
 constexpr int kScoreThreads = 128;
-constexpr int kScoreBlocks = kScoreThreads / 4;  // blocks per CTA: four lanes each
-constexpr int kScoreHeads = 8;                   // query heads whose sums a thread holds at a time
+constexpr int kScoreHeads = 4;                   // query heads whose sums a lane holds at a time
+constexpr int kScoreChunk = 32;                  // blocks that a CTA takes in one go
 constexpr int kSelectThreads = 256;
 constexpr int kSelectBins = 2048;
 
@@ -116,222 +119,406 @@ __device__ __forceinline__ unsigned long long double_key(double f) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(f);
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
-
-// Four lanes per block, each a quarter of its 16-byte chunks; the queries wait in shared memory in 64
-// bits.  Products of 16-bit values are exact, sums are off by less than 2^-45 of the largest term.
+// pair `p` of channels of a row of bounds, as two floats
 template <int DT>
+__device__ __forceinline__ f32x2 bound_pair(const uint8_t* row, int p) {
+    if constexpr (DT == 2) {
+        uint32_t w[2];
+        Elem<2>::expand(__ldg(reinterpret_cast<const uint16_t*>(row) + p), w);
+        return widen2<Elem<2>>(w[0]);
+    } else {
+        return widen2<Elem<DT>>(__ldg(reinterpret_cast<const uint32_t*>(row) + p));
+    }
+}
+// pair `p` of channels of a query
+template <int DT>
+__device__ __forceinline__ f32x2 query_pair(const uint16_t* q, int p) {
+    return widen2<Elem<DT == 1 ? 1 : 0>>(__ldg(reinterpret_cast<const uint32_t*>(q) + p));
+}
+__device__ __forceinline__ float max_of_warp(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
+    return v;
+}
+
+// What one launch of the score kernel looks like.
+struct ScoreShape {
+    long long blocks;     // blocks per (sequence, KV head) of the bounds
+    int chunks, chunk;    // CTAs per unit, blocks per CTA
+    float* approx;        // [units][blocks]
+    float* error;         // [units][chunks]
+};
+
+// A warp takes NB blocks at a time, a lane a few pairs of channels of each; with q = q+ + q- (its positive and
+// negative parts) a block's bound is sum q+ max + q- min, two packed multiply-adds per pair.  The 32 (or
+// 16) sums of a warp are joined in one transposed reduction.  Products of 16-bit values are exact; each of the
+// 2 D additions is off by at most 2^-24 of sum |q_c| m_c <= |q| |m|, m_c = max(|min_c|, |max_c|).
+template <int DT, int D>
 __global__ void __launch_bounds__(kScoreThreads)
-lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, long long blocks, int chunks, int D,
-                         unsigned long long* __restrict__ keys) {
-    using E = Elem<DT>;
-    constexpr int EPC = 16 / E::EB;  // channels per 16-byte chunk
-    extern __shared__ double sq[];   // [kScoreHeads][D + 2]
-    const int tid = threadIdx.x, ql = tid & 3;
-    const long long unit = blockIdx.x / chunks;  // (b * T + t) * H + h
-    const int h = int(unit % P.H), t = int(unit / P.H % P.T), b = int(unit / P.H / P.T);
+lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, const ScoreShape S) {
+    constexpr int ROWB = D * Elem<DT>::EB, PAIRS = D / 2, K = (PAIRS + 31) / 32, NB = K > 2 ? 4 : 8, NV = NB * kScoreHeads;
+    __shared__ float red[kScoreThreads / 32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const long long unit = blockIdx.x / S.chunks;  // (b * T + t) * H + h
+    const int h = int(unit % P.H), t = int(unit / P.H % P.T), b = int(unit / P.H / P.T), chunk = int(blockIdx.x % S.chunks);
     const AttendSeq seq = attend_seq(P, b, false);
     if (seq.tokens == 0) return;
     const int lim = seq.len - (P.T - 1 - t), nb = (lim + (1 << P.block_shift) - 1) >> P.block_shift;
-    const int j0 = int(blockIdx.x % chunks) * kScoreBlocks;
+    const int j0 = chunk * S.chunk, j1 = min(nb, j0 + S.chunk);
     if (j0 >= nb || nb <= P.keep) return;  // nothing to choose
-    const int j = j0 + (tid >> 2), cpr = D / EPC;
-    const uint8_t* lo = bounds + (((long long)b * P.H + h) * blocks + min(j, nb - 1)) * 2 * cpr * 16;
-    double best = -INFINITY;
-    for (int g0 = 0; g0 < P.G; g0 += kScoreHeads) {
-        const int gn = min(kScoreHeads, P.G - g0);
-        __syncthreads();
-        for (int i = tid; i < kScoreHeads * D; i += kScoreThreads) {
-            const int g = i / D, d = i % D;
-            float v = 0.f;
-            if (g < gn)
-                v = q_to_float(__ldg(P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G + g0 + g) * P.q_sh + d), DT == 1);
-            sq[g * (D + 2) + d] = double(v);
-        }
-        __syncthreads();
-        double acc[kScoreHeads];
+    const uint8_t* rows = bounds + ((long long)b * P.H + h) * S.blocks * 2 * ROWB;
+    const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G) * P.q_sh;
+    const f32x2 zero = 0ull;
+    float q2 = 0.f, m2 = 0.f;  // largest squared norms
+    for (int j = j0 + w * NB; j < j1; j += kScoreThreads / 32 * NB) {
+        f32x2 lo[NB][K], hi[NB][K];
 #pragma unroll
-        for (int g = 0; g < kScoreHeads; ++g) acc[g] = 0.0;
-        for (int c = ql; c < cpr; c += 4) {
-            const uint4 vl = __ldg(reinterpret_cast<const uint4*>(lo) + c), vh = __ldg(reinterpret_cast<const uint4*>(lo) + cpr + c);
-            const uint32_t wl[4] = {vl.x, vl.y, vl.z, vl.w}, wh[4] = {vh.x, vh.y, vh.z, vh.w};
+        for (int i = 0; i < NB; ++i) {
+            const uint8_t* row = rows + (long long)min(j + i, nb - 1) * 2 * ROWB;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t pl[E::PW], ph[E::PW];
-                E::expand(wl[i], pl);
-                E::expand(wh[i], ph);
-#pragma unroll
-                for (int k = 0; k < E::PW; ++k)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const double mn = e ? E::hi(pl[k]) : E::lo(pl[k]), mx = e ? E::hi(ph[k]) : E::lo(ph[k]);
-                        const double* q = sq + c * EPC + (i * E::PW + k) * 2 + e;
-#pragma unroll
-                        for (int g = 0; g < kScoreHeads; ++g) {
-                            if (g < gn) {
-                                const double x = q[g * (D + 2)];
-                                acc[g] = fma(x, x >= 0.0 ? mx : mn, acc[g]);
-                            }
-                        }
-                    }
+            for (int k = 0; k < K; ++k) {
+                const bool in = PAIRS % 32 == 0 || lane + 32 * k < PAIRS;
+                lo[i][k] = in ? bound_pair<DT>(row, lane + 32 * k) : zero;
+                hi[i][k] = in ? bound_pair<DT>(row + ROWB, lane + 32 * k) : zero;
             }
         }
+        float best = -INFINITY;
+        for (int g0 = 0; g0 < P.G; g0 += kScoreHeads) {
+            float v[NV];
 #pragma unroll
-        for (int g = 0; g < kScoreHeads; ++g) {
-            if (g < gn) {
-                acc[g] += __shfl_xor_sync(~0u, acc[g], 1);
-                acc[g] += __shfl_xor_sync(~0u, acc[g], 2);
-                best = fmax(best, acc[g]);
+            for (int g = 0; g < kScoreHeads; ++g) {
+                const uint16_t* q = q0 + (long long)min(g0 + g, P.G - 1) * P.q_sh;  // heads behind the last repeat it
+                f32x2 pos[K], neg[K], n2 = zero;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const bool in = PAIRS % 32 == 0 || lane + 32 * k < PAIRS;
+                    const f32x2 x = in ? query_pair<DT>(q, lane + 32 * k) : zero;
+                    float a, c;
+                    unpack2(x, a, c);
+                    pos[k] = pack2(fmaxf(a, 0.f), fmaxf(c, 0.f));
+                    neg[k] = pack2(fminf(a, 0.f), fminf(c, 0.f));
+                    n2 = fma2(x, x, n2);
+                }
+                if (j == j0 + w * NB) {  // once per warp
+                    float a, c;
+                    unpack2(n2, a, c);
+                    a += c;
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
+                    q2 = fmaxf(q2, a == a ? a : INFINITY);
+                }
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    f32x2 sum = zero;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) sum = fma2(pos[k], hi[i][k], fma2(neg[k], lo[i][k], sum));
+                    float a, c;
+                    unpack2(sum, a, c);
+                    v[i * kScoreHeads + g] = a + c;
+                }
             }
+            transposed_reduce<NV, 32>(v, lane);  // lane l holds (block, head) l * NV / 32
+            constexpr int STEP = 32 / NV;
+            float s = v[0];
+            bool nan = s != s;
+            s = fmaxf(s, __shfl_xor_sync(~0u, s, STEP));
+            s = fmaxf(s, __shfl_xor_sync(~0u, s, 2 * STEP));
+            const unsigned any = __ballot_sync(~0u, nan);
+            if (any >> (lane & ~(4 * STEP - 1)) & ((1ull << (4 * STEP)) - 1)) s = NAN;  // decided in 64 bits
+            best = s != s || best != best ? NAN : fmaxf(best, s);
         }
+        constexpr int LANES = 32 / NB;  // lanes that hold a block's score
+        const int at = j + lane / LANES;
+        if (lane % LANES == 0 && at < j1) S.approx[unit * S.blocks + at] = best;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            float n = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float a, c, d, e;
+                unpack2(lo[i][k], a, c);
+                unpack2(hi[i][k], d, e);
+                const float x = fmaxf(fabsf(a), fabsf(d)), y = fmaxf(fabsf(c), fabsf(e));
+                n = fmaf(x, x, fmaf(y, y, n));
+            }
+            lo[i][0] = pack2(n, 0.f);
+        }
+        float n[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            float z;
+            unpack2(lo[i][0], n[i], z);
+        }
+        transposed_reduce<NB, 32>(n, lane);
+        m2 = fmaxf(m2, n[0] == n[0] ? n[0] : INFINITY);
     }
-    if (ql == 0 && j < nb) keys[unit * blocks + j] = double_key(best);
+    // 1.01: the roundings of the norms themselves
+    const float e = 1.01f * (2 * D + 8) * 0x1p-24f * sqrtf(q2) * sqrtf(max_of_warp(m2)) + 1e-37f;
+    if (lane == 0) red[w] = e == e ? e : INFINITY;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float top = 0.f;
+        for (int i = 0; i < kScoreThreads / 32; ++i) top = fmaxf(top, red[i]);
+        S.error[unit * S.chunks + chunk] = top;
+    }
 }
 
 // ------------------------------------------------------------------------------------ choice
-// One CTA per (sequence, token, KV head): the first `sink` and last `recent` blocks and the best of the
-// others, `keep` in all, lower block first among equals, written in ascending order with -1 behind.  The
-// border is found by histograms over the range of the keys, each pass narrowing it to one of 2048 bins.
-__global__ void __launch_bounds__(kSelectThreads)
-lagkv_block_select_kernel(const AttendParams P, const unsigned long long* __restrict__ keys, long long blocks, int sink,
-                          int recent, int32_t* __restrict__ idx) {
-    extern __shared__ unsigned long long sk[];  // the unit's keys
-    __shared__ int hist[kSelectBins];
-    __shared__ unsigned long long red[2][kSelectThreads / 32];
-    __shared__ int wsum[2][kSelectThreads / 32];
-    __shared__ int found[3];
+// Narrows [lo, hi] (the smallest and the largest of the keys asked about) to the key with `need` - 1 larger ones,
+// by histograms over 2048 bins: returns it and leaves in `need` how many of the keys equal to it are wanted;
+// all = every key equal to it (or, early, of its bin: then the returned key is the bin's lowest).
+template <class Key, class Get>
+__device__ __forceinline__ Key find_border(Key lo, Key hi, int n, int& need, bool& all, int* hist, int* wsum, int* found, Get&& get) {
+    constexpr int NW = kSelectThreads / 32, PER = kSelectBins / kSelectThreads;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    constexpr int NW = kSelectThreads / 32;
-    const long long unit = blockIdx.x;
-    const int t = int(unit / P.H % P.T), b = int(unit / P.H / P.T);
-    const AttendSeq seq = attend_seq(P, b, unit % ((long long)P.H * P.T) == 0 && tid == 0);
-    const int lim = seq.tokens == 0 ? 0 : seq.len - (P.T - 1 - t);
-    const int nb = (lim + (1 << P.block_shift) - 1) >> P.block_shift;
-    int32_t* out = idx + unit * P.keep;
-    if (nb <= P.keep) {
-        for (int i = tid; i < P.keep; i += kSelectThreads) out[i] = i < nb ? i : -1;
-        return;
-    }
-    // candidates: blocks [sink, nb - recent); nb > keep >= sink + recent
-    const int c0 = sink, c1 = nb - recent;
-    int need = P.keep - sink - recent;
-    unsigned long long lo = ~0ull, hi = 0;
-    for (int j = tid; j < nb; j += kSelectThreads) {
-        const unsigned long long k = __ldg(keys + unit * blocks + j);
-        sk[j] = k;
-        if (j >= c0 && j < c1) {
-            lo = min(lo, k);
-            hi = max(hi, k);
-        }
-    }
-    for (int o = 16; o; o >>= 1) {
-        lo = min(lo, __shfl_xor_sync(~0u, lo, o));
-        hi = max(hi, __shfl_xor_sync(~0u, hi, o));
-    }
-    if (lane == 0) {
-        red[0][w] = lo;
-        red[1][w] = hi;
-    }
-    __syncthreads();
-    for (int i = 0; i < NW; ++i) {
-        lo = min(lo, red[0][i]);
-        hi = max(hi, red[1][i]);
-    }
-    // keys above hi are taken, keys below lo are not, `need` of those in between are still to be found
-    unsigned long long border = 0;  // keys above it are taken, and of those equal to it ...
-    int ties = 0;                   // ... this many, the lowest blocks first (-1: all)
-    const bool none = need == 0;
-    while (!none) {
-        const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 11);
+    for (;;) {
+        const int width = sizeof(Key) == 8 ? 64 - __clzll((long long)(hi - lo)) : 32 - __clz(int(hi - lo)), shift = max(0, width - 11);
+        __syncthreads();
         for (int i = tid; i < kSelectBins; i += kSelectThreads) hist[i] = 0;
         __syncthreads();
-        for (int j = c0 + tid; j < c1; j += kSelectThreads) {
-            const unsigned long long k = sk[j];
+        for (int j = tid; j < n; j += kSelectThreads) {
+            const Key k = get(j);
             if (k >= lo && k <= hi) atomicAdd(&hist[int((k - lo) >> shift)], 1);
         }
         __syncthreads();
-        // thread i holds bins from the top: [kSelectBins - 8 (i + 1), kSelectBins - 8 i)
-        constexpr int PER = kSelectBins / kSelectThreads;
-        const int top = kSelectBins - PER * (tid + 1);
+        const int top = kSelectBins - PER * (tid + 1);  // this thread's bins, counted from the top
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) mine += hist[top + i];
         int inc = mine;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(~0u, inc, o);
             if (lane >= o) inc += v;
         }
-        if (lane == 31) wsum[0][w] = inc;
+        if (lane == 31) wsum[w] = inc;
         __syncthreads();
         int before = inc - mine;
-        for (int i = 0; i < w; ++i) before += wsum[0][i];
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+            if (i < w) before += wsum[i];
         if (before < need && before + mine >= need) {
             int at = before;
             for (int i = PER - 1; i >= 0; --i) {
-                const int n = hist[top + i];
-                if (at + n >= need) {
+                const int c = hist[top + i];
+                if (at + c >= need) {
                     found[0] = top + i;
                     found[1] = need - at;
-                    found[2] = n;
+                    found[2] = c;
                     break;
                 }
-                at += n;
+                at += c;
             }
         }
         __syncthreads();
-        const unsigned long long new_lo = lo + ((unsigned long long)found[0] << shift);
-        const unsigned long long width = shift == 0 ? 0 : (1ull << shift) - 1;
-        const unsigned long long new_hi = hi - new_lo < width ? hi : new_lo + width;
-        need = found[1];
-        const int n = found[2];
+        const Key new_lo = lo + (Key(found[0]) << shift), span = shift == 0 ? Key(0) : (Key(1) << shift) - 1;
+        hi = hi - new_lo < span ? hi : new_lo + span;
         lo = new_lo;
-        hi = new_hi;
-        if (n == need || lo == hi) {  // the whole bin, or equal keys
-            border = lo;
-            ties = n == need ? -1 : need;
-            break;
+        need = found[1];
+        all = found[2] == need;
+        if (lo == hi || (sizeof(Key) == 8 && all)) return lo;
+    }
+}
+
+// The 64-bit score of a block, by one warp.
+template <int DT>
+__device__ __forceinline__ double exact_score(const AttendParams& P, const uint8_t* row, const uint16_t* q0, int D, int rowb, int lane) {
+    double best = -INFINITY;
+    for (int g = 0; g < P.G; ++g) {
+        double sum = 0.0;
+        for (int p = lane; p < D / 2; p += 32) {
+            float q[2], lo[2], hi[2];
+            unpack2(query_pair<DT>(q0 + (long long)g * P.q_sh, p), q[0], q[1]);
+            unpack2(bound_pair<DT>(row, p), lo[0], lo[1]);
+            unpack2(bound_pair<DT>(row + rowb, p), hi[0], hi[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) sum = fma(double(q[e]), double(q[e] >= 0.f ? hi[e] : lo[e]), sum);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        best = fmax(best, sum);
+    }
+    return best;
+}
+
+// One CTA per (sequence, token, KV head): the first `sink` and last `recent` blocks and the best of the
+// others, `keep` in all, lower block first among equals, written in ascending order with -1 behind.
+template <int DT>
+__global__ void __launch_bounds__(kSelectThreads)
+lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, const ScoreShape S, int D,
+                          unsigned long long* __restrict__ keys, int sink, int recent, int32_t* __restrict__ idx) {
+    extern __shared__ float sa[];  // the candidates' scores, then the numbers of those near the border
+    __shared__ int hist[kSelectBins];
+    __shared__ float red[2][kSelectThreads / 32];
+    __shared__ int wsum[2][kSelectThreads / 32];
+    __shared__ int found[4];
+    __shared__ unsigned long long range[2];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    constexpr int NW = kSelectThreads / 32;
+    const long long unit = blockIdx.x;
+    const int h = int(unit % P.H), t = int(unit / P.H % P.T), b = int(unit / P.H / P.T);
+    const AttendSeq seq = attend_seq(P, b, unit % ((long long)P.H * P.T) == 0 && tid == 0);
+    const int lim = seq.tokens == 0 ? 0 : seq.len - (P.T - 1 - t);
+    const int nb = (lim + (1 << P.block_shift) - 1) >> P.block_shift;
+    int32_t* out = idx + unit * P.keep;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the scores
+    if (nb <= P.keep) {
+        for (int i = tid; i < P.keep; i += kSelectThreads) out[i] = i < nb ? i : -1;
+        return;
+    }
+    // candidates: blocks [sink, nb - recent); nb > keep >= sink + recent, so there are more than are wanted
+    const int n = nb - recent - sink;
+    int need = P.keep - sink - recent;
+    if (need > 0) {
+        uint32_t lo = ~0u, hi = 0u;
+        float error = 0.f;
+        for (int j = tid; j < n; j += kSelectThreads) {
+            const float a = __ldcg(S.approx + unit * S.blocks + sink + j);
+            sa[j] = a;
+            const uint32_t k = float_key(a);
+            lo = min(lo, k);
+            hi = max(hi, k);
+        }
+        for (int c = tid; c < (nb + S.chunk - 1) / S.chunk; c += kSelectThreads) error = fmaxf(error, __ldcg(S.error + unit * S.chunks + c));
+        if (tid == 0) {
+            range[0] = ~0ull;
+            range[1] = 0ull;
+            found[3] = 0;
+        }
+        __syncthreads();
+        lo = __reduce_min_sync(~0u, lo);
+        hi = __reduce_max_sync(~0u, hi);
+        error = max_of_warp(error);
+        if (lane == 0) {
+            atomicMin(&range[0], (unsigned long long)lo);
+            atomicMax(&range[1], (unsigned long long)hi);
+            red[0][w] = error;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) error = fmaxf(error, red[0][i]);
+        lo = uint32_t(range[0]);
+        hi = uint32_t(range[1]);
+        bool all;
+        int rank = need;
+        const uint32_t border = find_border<uint32_t>(lo, hi, n, rank, all, hist, wsum[0], found, [&](int j) { return float_key(sa[j]); });
+        // float of the key: the need-th largest 32-bit score; the need-th largest 64-bit one is within E of it
+        const float tau = __uint_as_float(border >> 31 ? border & 0x7fffffffu : ~border);
+        const float above = tau + 2.f * error * 1.0001f, below = tau - 2.f * error * 1.0001f;
+        const float over = fabsf(tau) * 0x1p-22f;  // the two sums above are rounded
+        auto sure = [&](float a) { return a > above + over; };
+        auto out_of_it = [&](float a) { return a < below - over; };
+        int* near = reinterpret_cast<int*>(sa) + n;
+        // blocks near the border, in their order: each thread a run of candidates
+        const int per = (n + kSelectThreads - 1) / kSelectThreads, j0 = min(n, tid * per), j1 = min(n, j0 + per);
+        int ni = 0, na = 0;
+        for (int j = j0; j < j1; ++j) {
+            const float a = sa[j];
+            ni += sure(a);
+            na += !sure(a) && !out_of_it(a);
+        }
+        int ii = ni, ia = na;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(~0u, ii, o), y = __shfl_up_sync(~0u, ia, o);
+            if (lane >= o) {
+                ii += x;
+                ia += y;
+            }
+        }
+        __syncthreads();
+        if (lane == 31) {
+            wsum[0][w] = ii;
+            wsum[1][w] = ia;
+        }
+        __syncthreads();
+        int total_in = 0, total_near = 0, at = ia - na;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            if (i < w) at += wsum[1][i];
+            total_in += wsum[0][i];
+            total_near += wsum[1][i];
+        }
+        int wanted = need - total_in;  // of the blocks near the border; at least one
+        const bool near_all = wanted >= total_near;
+        if (!near_all) {
+            for (int j = j0; j < j1; ++j) {
+                const float a = sa[j];
+                if (!sure(a) && !out_of_it(a)) near[at++] = j;
+            }
+            __syncthreads();
+            const int rowb = D * Elem<DT>::EB;
+            const uint8_t* rows = bounds + (((long long)b * P.H + h) * S.blocks + sink) * 2 * rowb;
+            const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G) * P.q_sh;
+            unsigned long long* mine = keys + unit * S.blocks;
+            if (tid == 0) {
+                range[0] = ~0ull;
+                range[1] = 0ull;
+            }
+            __syncthreads();
+            for (int i = w; i < total_near; i += NW) {
+                const unsigned long long k = double_key(exact_score<DT>(P, rows + (long long)near[i] * 2 * rowb, q0, D, rowb, lane));
+                if (lane == 0) {
+                    mine[i] = k;
+                    atomicMin(&range[0], k);
+                    atomicMax(&range[1], k);
+                }
+            }
+            __syncthreads();
+            const unsigned long long k = find_border<unsigned long long>(range[0], range[1], total_near, wanted, all, hist, wsum[0], found,
+                                                                         [&](int i) { return mine[i]; });
+            // the chosen ones become certain, the others impossible; of keys equal to k the lowest blocks
+            const int pn = (total_near + kSelectThreads - 1) / kSelectThreads, i0 = min(total_near, tid * pn), i1 = min(total_near, i0 + pn);
+            int ne = 0;
+            for (int i = i0; i < i1; ++i) ne += mine[i] == k;
+            int ie = ne;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(~0u, ie, o);
+                if (lane >= o) ie += x;
+            }
+            __syncthreads();
+            if (lane == 31) wsum[0][w] = ie;
+            __syncthreads();
+            int be = ie - ne;
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+                if (i < w) be += wsum[0][i];
+            for (int i = i0; i < i1; ++i) {
+                const bool in = all ? mine[i] >= k : mine[i] > k || (mine[i] == k && be < wanted);
+                be += mine[i] == k;
+                sa[near[i]] = in ? INFINITY : -INFINITY;
+            }
+            __syncthreads();
+        }
+        for (int j = j0; j < j1; ++j) {
+            const float a = sa[j];
+            sa[j] = sure(a) || a == INFINITY || (near_all && !out_of_it(a)) ? 1.f : 0.f;
         }
         __syncthreads();
     }
-    // ordered output: each thread a run of blocks, ranks by a scan
+    // ordered output: each thread a run of blocks
     const int per = (nb + kSelectThreads - 1) / kSelectThreads, j0 = min(nb, tid * per), j1 = min(nb, j0 + per);
-    auto state = [&](int j) {  // 2: taken, 1: taken if among the first `ties` equal ones, 0: not
-        if (j < c0 || j >= c1) return 2;
-        if (none) return 0;
-        const unsigned long long k = sk[j];
-        if (ties < 0) return k >= border ? 2 : 0;
-        return k > border ? 2 : k == border ? 1 : 0;
-    };
-    int nt = 0, ne = 0;
-    for (int j = j0; j < j1; ++j) {
-        const int s = state(j);
-        nt += s == 2;
-        ne += s == 1;
-    }
-    int it = nt, ie = ne;
+    auto taken = [&](int j) { return j < sink || j >= sink + n || (need > 0 && sa[j - sink] != 0.f); };
+    int c = 0;
+    for (int j = j0; j < j1; ++j) c += taken(j);
+    int inc = c;
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int a = __shfl_up_sync(~0u, it, o), e = __shfl_up_sync(~0u, ie, o);
-        if (lane >= o) {
-            it += a;
-            ie += e;
-        }
+        const int v = __shfl_up_sync(~0u, inc, o);
+        if (lane >= o) inc += v;
     }
     __syncthreads();
-    if (lane == 31) {
-        wsum[0][w] = it;
-        wsum[1][w] = ie;
-    }
+    if (lane == 31) wsum[0][w] = inc;
     __syncthreads();
-    int bt = it - nt, be = ie - ne;
-    for (int i = 0; i < w; ++i) {
-        bt += wsum[0][i];
-        be += wsum[1][i];
-    }
-    for (int j = j0; j < j1; ++j) {
-        const int s = state(j);
-        if (s == 2 || (s == 1 && be < ties)) out[bt + min(be, max(ties, 0))] = j;
-        bt += s == 2;
-        be += s == 1;
-    }
+    int at = inc - c;
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+        if (i < w) at += wsum[0][i];
+    for (int j = j0; j < j1; ++j)
+        if (taken(j)) out[at++] = j;
 }
 
 }  // namespace lagkv

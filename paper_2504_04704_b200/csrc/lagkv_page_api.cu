@@ -118,8 +118,9 @@ int lagkv_pages_fork(lagkv_plan_t plan, void* K_pool, void* V_pool, const lagkv_
     DeviceGuard guard(plan->cfg.device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     lagkv_pages_fork_plan_kernel<<<n, kScanThreads, 0, stream>>>(P, seq_len, static_len, src, dst);
-    lagkv_pages_fork_kernel<<<copy_grid(plan), kPageThreads, 0, stream>>>(P, seq_len, static_len, src, dst, n);
-    return check_launch();
+    void* args[] = {&P, &seq_len, &static_len, &src, &dst, &n};
+    rc = launch_behind(reinterpret_cast<const void*>(&lagkv_pages_fork_kernel), unsigned(copy_grid(plan)), kPageThreads, args, 0, stream);
+    return rc == LAGKV_OK ? check_launch() : rc;
 }
 
 int lagkv_pages_compact(lagkv_plan_t plan, void* K_pool, void* V_pool, const lagkv_paged_layout* layout, int64_t num_pages,
@@ -133,8 +134,9 @@ int lagkv_pages_compact(lagkv_plan_t plan, void* K_pool, void* V_pool, const lag
     DeviceGuard guard(plan->cfg.device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     lagkv_pages_compact_plan_kernel<<<1, kScanThreads, 0, stream>>>(P, live_out);
-    lagkv_pages_compact_kernel<<<copy_grid(plan), kPageThreads, 0, stream>>>(P);
-    return check_launch();
+    void* args[] = {&P};
+    rc = launch_behind(reinterpret_cast<const void*>(&lagkv_pages_compact_kernel), unsigned(copy_grid(plan)), kPageThreads, args, 0, stream);
+    return rc == LAGKV_OK ? check_launch() : rc;
 }
 
 }  // extern "C"

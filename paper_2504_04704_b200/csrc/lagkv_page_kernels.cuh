@@ -183,6 +183,7 @@ lagkv_pages_fork_plan_kernel(const PageParams P, const int32_t* __restrict__ seq
                              const int32_t* __restrict__ src, const int32_t* __restrict__ dst) {
     __shared__ int sums[32];
     __shared__ int flag;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int i = blockIdx.x, tid = threadIdx.x, n = gridDim.x;
     int32_t* w = P.work + (long long)i * kPairWords;
     int32_t* owner = P.work + (long long)P.B * kPairWords;
@@ -264,6 +265,7 @@ __device__ __forceinline__ void copy_slice(const PageParams& P, int from, int to
 __global__ void __launch_bounds__(kPageThreads)
 lagkv_pages_fork_kernel(const PageParams P, int32_t* seq_len, int32_t* static_len, const int32_t* __restrict__ src,
                         const int32_t* __restrict__ dst, int n) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int copies = P.work[(long long)P.B * kPairWords + P.B];
     if (copies < 0) return;
     // tables and lengths: the first CTAs, a pair at a time
@@ -321,6 +323,7 @@ lagkv_pages_fork_kernel(const PageParams P, int32_t* seq_len, int32_t* static_le
 __global__ void __launch_bounds__(kScanThreads)
 lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
     __shared__ int sums[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int PER = 8;
     const int tid = threadIdx.x;
     long long live = 0;
@@ -367,6 +370,7 @@ lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
 
 __global__ void __launch_bounds__(kPageThreads)
 lagkv_pages_compact_kernel(const PageParams P) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int live = P.work[0], moves = P.work[1];
     const long long stride = (long long)gridDim.x * kPageThreads, first = blockIdx.x * (long long)kPageThreads + threadIdx.x;
     for (long long i = first; i < (long long)P.B * P.max_blocks; i += stride) {

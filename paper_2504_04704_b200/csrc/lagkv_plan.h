@@ -4,6 +4,7 @@
 #include "lagkv.h"
 
 #include <atomic>
+#include <cstring>
 #include <cuda_runtime.h>
 #include <mutex>
 
@@ -124,4 +125,20 @@ inline int resolve_strides(const lagkv_config& c, int64_t S, Strides* out) {
 
 inline int check_launch() {
     return cudaPeekAtLastError() == cudaSuccess ? LAGKV_OK : LAGKV_ECUDA;
+}
+
+// A launch that may begin while the one before it in the stream is ending: both kernels call griddepcontrol.
+inline int launch_behind(const void* fn, unsigned grid, unsigned threads, void** args, size_t smem, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? LAGKV_OK : LAGKV_ECUDA;
 }
