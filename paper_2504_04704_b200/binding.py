@@ -199,6 +199,15 @@ def _stream(device) -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
+# The operators of a decode step take a few microseconds on the device, so their wrappers count: addresses go to
+# ctypes as plain integers and the stream is asked for without making a Stream object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
 def lagkv_keep_for_target(Ls: int, sink: int, lag: int, target_C: float) -> int:
     return int(load_library().lagkv_keep_for_target(int(Ls), int(sink), int(lag), float(target_C)))
 
@@ -438,50 +447,49 @@ class Plan:
         return ws
 
     def _check_ints(self, t, name: str, shape, dtype=torch.int32):
-        if t is None:
-            return
-        if t.dtype != dtype or not t.is_cuda or t.device.index != self.device or tuple(t.shape) != tuple(shape) or \
-                not t.is_contiguous():
+        if t is not None and (t.dtype != dtype or t.get_device() != self.device or t.shape != shape or not t.is_contiguous()):
             raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor {tuple(shape)} on device {self.device}")
 
     def _check_contiguous_cache(self, t, name: str):
         """A cache ``[B, H, S_cap, D]`` whose strides are the plan's (0 = contiguous)."""
-        self._check_cache(t, name)
-        c = self.cfg
-        if t.dim() != 4 or t.shape[0] != c.B or t.shape[1] != c.H_kv or t.shape[3] != c.D:
+        if t.dtype != self.dtype or t.get_device() != self.device:
+            raise TypeError(f"{name} must be a {self.dtype} CUDA tensor on device {self.device}")
+        c, shape = self.cfg, t.shape
+        if len(shape) != 4 or shape[0] != c.B or shape[1] != c.H_kv or shape[3] != c.D:
             raise TypeError(f"{name} must be [{c.B}, {c.H_kv}, S_cap, {c.D}]")
+        if t.is_contiguous() and not (c.stride_b or c.stride_h or c.stride_s):
+            return
         ss = c.stride_s or c.D
-        sh = c.stride_h or t.shape[2] * ss
+        sh = c.stride_h or shape[2] * ss
         want = (c.stride_b or c.H_kv * sh, sh, ss, 1)
-        if any(n > 1 and have != w for n, have, w in zip(t.shape, t.stride(), want)):
+        if any(n > 1 and have != w for n, have, w in zip(shape, t.stride(), want)):
             raise TypeError(f"{name} has strides {t.stride()}, the plan says {want}")
 
     def _query(self, Q, scale, k_scale, v_scale) -> lagkv_query:
-        c = self.cfg
+        c, shape = self.cfg, Q.shape
         want = torch.float16 if self.dtype == torch.float16 else torch.bfloat16
-        if Q.dtype != want or not Q.is_cuda or Q.device.index != self.device or Q.dim() != 4 or Q.shape[0] != c.B or \
-                Q.shape[3] != c.D or Q.stride(3) != 1:
+        if Q.dtype != want or Q.get_device() != self.device or len(shape) != 4 or shape[0] != c.B or shape[3] != c.D or Q.stride(3) != 1:
             raise TypeError(f"Q must be a {want} CUDA tensor [{c.B}, T, H_q, {c.D}] with channel stride 1")
-        T, H_q = int(Q.shape[1]), int(Q.shape[2])
-        strides = (0, 0, 0) if Q.is_contiguous() else tuple(int(Q.stride(i)) for i in range(3))
-        return lagkv_query(T, H_q, 0.0 if scale is None else float(scale), float(k_scale), float(v_scale), *strides)
+        strides = (0, 0, 0) if Q.is_contiguous() else Q.stride()[:3]
+        return lagkv_query(shape[1], shape[2], 0.0 if scale is None else scale, k_scale, v_scale, *strides)
 
     def _attend_out(self, Q, out, want_lse):
         if out is None:
-            out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            out = torch.empty_like(Q, memory_format=torch.contiguous_format)
         elif out.dtype != Q.dtype or out.shape != Q.shape or not out.is_contiguous() or out.device != Q.device:
             raise TypeError("out must be a contiguous tensor like Q")
-        lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if want_lse else None
+        lse = Q.new_empty(Q.shape[:3], dtype=torch.float32) if want_lse else None
         return out, lse
 
     def _paged_pool(self, K_pool, V_pool, block_table, strides, num_pages):
         """Layout and page count of a pool, checked against the tensors."""
-        self._check_cache(K_pool, "K_pool")
+        for pool in (K_pool, V_pool):
+            if pool is not None and (pool.dtype != self.dtype or pool.get_device() != self.device):
+                raise TypeError(f"the pools must be {self.dtype} CUDA tensors on device {self.device}")
         if V_pool is not None:
-            self._check_cache(V_pool, "V_pool")
             if V_pool.shape != K_pool.shape or V_pool.stride() != K_pool.stride():
                 raise TypeError("K_pool and V_pool must have the same shape and strides")
-        if block_table.device.index != self.device:
+        if block_table.get_device() != self.device:
             raise TypeError(f"block_table must be on device {self.device}")
         if strides is None:
             c = self.cfg
@@ -508,8 +516,8 @@ class Plan:
             raise TypeError("K and V must have the same shape")
         out, lse = self._attend_out(Q, out, want_lse)
         rc = self.lib.lagkv_attend_tree(
-            self.handle, ctypes.byref(q), _ptr(Q), _ptr(K), _ptr(V), int(K.shape[2]), _ptr(seq_len), _ptr(draft_len),
-            _ptr(tree_mask), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, ctypes.byref(q), _addr(Q), _addr(K), _addr(V), int(K.shape[2]), _addr(seq_len), _addr(draft_len),
+            _addr(tree_mask), _addr(out), _addr(lse), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_attend_tree")
         return {"out": out, "lse": lse} if want_lse else {"out": out}
 
@@ -525,9 +533,9 @@ class Plan:
         self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
         out, lse = self._attend_out(Q, out, want_lse)
         rc = self.lib.lagkv_attend_tree_paged(
-            self.handle, ctypes.byref(q), _ptr(Q), _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(seq_len),
-            _ptr(draft_len), _ptr(tree_mask), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
-            _stream(self._dev()))
+            self.handle, ctypes.byref(q), _addr(Q), _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(seq_len),
+            _addr(draft_len), _addr(tree_mask), _addr(out), _addr(lse), _addr(workspace), workspace.numel(),
+            _raw_stream(self.device))
         _check(rc, "lagkv_attend_tree_paged")
         return {"out": out, "lse": lse} if want_lse else {"out": out}
 
@@ -550,8 +558,8 @@ class Plan:
         if V_cache.shape != K_cache.shape:
             raise TypeError("K_cache and V_cache must have the same shape")
         rc = self.lib.lagkv_tree_commit(
-            self.handle, _ptr(K_cache), _ptr(V_cache), int(K_cache.shape[2]), _ptr(seq_len), _ptr(draft_len), T,
-            _ptr(accepted), _ptr(n_accepted), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(K_cache), _addr(V_cache), int(K_cache.shape[2]), _addr(seq_len), _addr(draft_len), T,
+            _addr(accepted), _addr(n_accepted), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_tree_commit")
 
     def tree_commit_paged(self, K_pool, V_pool, block_table, seq_len, accepted, n_accepted, workspace, draft_len=None,
@@ -560,8 +568,8 @@ class Plan:
         T = self._check_commit(seq_len, draft_len, accepted, n_accepted)
         lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, num_pages)
         rc = self.lib.lagkv_tree_commit_paged(
-            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(seq_len), _ptr(draft_len), T,
-            _ptr(accepted), _ptr(n_accepted), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(seq_len), _addr(draft_len), T,
+            _addr(accepted), _addr(n_accepted), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_tree_commit_paged")
 
     # ---- blocks
@@ -572,12 +580,11 @@ class Plan:
                            torch.float8_e4m3fn else self.dtype, device=self._dev()).view(self.dtype)
 
     def _check_bounds(self, bounds):
-        c = self.cfg
-        self._check_cache(bounds, "bounds")
-        if bounds.dim() != 5 or (bounds.shape[0], bounds.shape[1], bounds.shape[3], bounds.shape[4]) != (c.B, c.H_kv, 2, c.D) or \
-                not bounds.is_contiguous():
-            raise TypeError(f"bounds must be contiguous [{c.B}, {c.H_kv}, blocks, 2, {c.D}]")
-        return int(bounds.shape[2])
+        c, shape = self.cfg, bounds.shape
+        if bounds.dtype != self.dtype or bounds.get_device() != self.device or len(shape) != 5 or \
+                shape != (c.B, c.H_kv, shape[2], 2, c.D) or not bounds.is_contiguous():
+            raise TypeError(f"bounds must be a contiguous {self.dtype} CUDA tensor [{c.B}, {c.H_kv}, blocks, 2, {c.D}]")
+        return shape[2]
 
     def block_bounds(self, K, seq_len, bounds, workspace, block_rows=64, from_len=None):
         """``lagkv_block_bounds``: per-channel minimum and maximum of each block of ``block_rows`` K rows below
@@ -586,8 +593,8 @@ class Plan:
         blocks = self._check_bounds(bounds)
         self._check_ints(seq_len, "seq_len", (self.cfg.B,))
         self._check_ints(from_len, "from_len", (self.cfg.B,))
-        rc = self.lib.lagkv_block_bounds(self.handle, _ptr(K), int(K.shape[2]), _ptr(from_len), _ptr(seq_len), int(block_rows),
-                                         _ptr(bounds), blocks, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+        rc = self.lib.lagkv_block_bounds(self.handle, _addr(K), int(K.shape[2]), _addr(from_len), _addr(seq_len), int(block_rows),
+                                         _addr(bounds), blocks, _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_block_bounds")
 
     def block_bounds_paged(self, K_pool, block_table, seq_len, bounds, workspace, block_rows=64, from_len=None, strides=None,
@@ -598,8 +605,8 @@ class Plan:
         self._check_ints(seq_len, "seq_len", (self.cfg.B,))
         self._check_ints(from_len, "from_len", (self.cfg.B,))
         rc = self.lib.lagkv_block_bounds_paged(
-            self.handle, _ptr(K_pool), ctypes.byref(lay), pages, _ptr(from_len), _ptr(seq_len), int(block_rows), _ptr(bounds),
-            blocks, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(K_pool), ctypes.byref(lay), pages, _addr(from_len), _addr(seq_len), int(block_rows), _addr(bounds),
+            blocks, _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_block_bounds_paged")
 
     def _blocks_out(self, Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse, want_idx):
@@ -607,7 +614,7 @@ class Plan:
         self._check_ints(seq_len, "seq_len", (self.cfg.B,))
         choice = lagkv_block_choice(int(block_rows), int(keep), int(sink_blocks), int(recent_blocks), blocks)
         out, lse = self._attend_out(Q, out, want_lse)
-        idx = torch.empty((self.cfg.B, Q.shape[1], self.cfg.H_kv, int(keep)), dtype=torch.int32, device=Q.device) if want_idx else None
+        idx = Q.new_empty((self.cfg.B, Q.shape[1], self.cfg.H_kv, int(keep)), dtype=torch.int32) if want_idx else None
         got = {"out": out}
         if want_lse:
             got["lse"] = lse
@@ -628,8 +635,8 @@ class Plan:
         choice, got, lse, idx = self._blocks_out(Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse,
                                                  want_idx)
         rc = self.lib.lagkv_attend_blocks(
-            self.handle, ctypes.byref(q), ctypes.byref(choice), _ptr(Q), _ptr(K), _ptr(V), int(K.shape[2]), _ptr(seq_len),
-            _ptr(bounds), _ptr(got["out"]), _ptr(lse), _ptr(idx), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, ctypes.byref(q), ctypes.byref(choice), _addr(Q), _addr(K), _addr(V), int(K.shape[2]), _addr(seq_len),
+            _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_attend_blocks")
         return got
 
@@ -642,9 +649,9 @@ class Plan:
         choice, got, lse, idx = self._blocks_out(Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse,
                                                  want_idx)
         rc = self.lib.lagkv_attend_blocks_paged(
-            self.handle, ctypes.byref(q), ctypes.byref(choice), _ptr(Q), _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages,
-            _ptr(seq_len), _ptr(bounds), _ptr(got["out"]), _ptr(lse), _ptr(idx), _ptr(workspace), workspace.numel(),
-            _stream(self._dev()))
+            self.handle, ctypes.byref(q), ctypes.byref(choice), _addr(Q), _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages,
+            _addr(seq_len), _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), _addr(workspace), workspace.numel(),
+            _raw_stream(self.device))
         _check(rc, "lagkv_attend_blocks_paged")
         return got
 
@@ -655,7 +662,7 @@ class Plan:
         if nbytes == 0:
             raise LagKVError(LAGKV_EINVAL, "lagkv_pages_workspace_bytes")
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self._dev())
-        _check(self.lib.lagkv_pages_workspace_init(self.handle, _ptr(ws), ws.numel(), _stream(self._dev())),
+        _check(self.lib.lagkv_pages_workspace_init(self.handle, _addr(ws), ws.numel(), _raw_stream(self.device)),
                "lagkv_pages_workspace_init")
         return ws
 
@@ -672,8 +679,8 @@ class Plan:
         self._check_table(block_table, refs)
         self._check_ints(keep_len, "keep_len", (self.cfg.B,))
         rc = self.lib.lagkv_pages_release(
-            self.handle, _ptr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _ptr(refs),
-            _ptr(keep_len), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _addr(refs),
+            _addr(keep_len), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_pages_release")
 
     def pages_reserve(self, block_table, refs, want_len, workspace, page_size) -> None:
@@ -681,8 +688,8 @@ class Plan:
         self._check_table(block_table, refs)
         self._check_ints(want_len, "want_len", (self.cfg.B,))
         rc = self.lib.lagkv_pages_reserve(
-            self.handle, _ptr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _ptr(refs),
-            _ptr(want_len), _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _addr(refs),
+            _addr(want_len), _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_pages_reserve")
 
     def pages_fork(self, K_pool, V_pool, block_table, refs, seq_len, static_len, src, dst, workspace, strides=None) -> None:
@@ -696,8 +703,8 @@ class Plan:
         self._check_ints(src, "src", (n,))
         self._check_ints(dst, "dst", (n,))
         rc = self.lib.lagkv_pages_fork(
-            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(refs), _ptr(seq_len), _ptr(static_len),
-            _ptr(src), _ptr(dst), n, _ptr(workspace), workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(refs), _addr(seq_len), _addr(static_len),
+            _addr(src), _addr(dst), n, _addr(workspace), workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_pages_fork")
 
     def pages_compact(self, K_pool, V_pool, block_table, refs, workspace, strides=None, live_out=None) -> torch.Tensor:
@@ -707,8 +714,8 @@ class Plan:
         live = torch.empty(1, dtype=torch.int32, device=refs.device) if live_out is None else live_out
         self._check_ints(live, "live_out", (1,))
         rc = self.lib.lagkv_pages_compact(
-            self.handle, _ptr(K_pool), _ptr(V_pool), ctypes.byref(lay), pages, _ptr(refs), _ptr(live), _ptr(workspace),
-            workspace.numel(), _stream(self._dev()))
+            self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(refs), _addr(live), _addr(workspace),
+            workspace.numel(), _raw_stream(self.device))
         _check(rc, "lagkv_pages_compact")
         return live
 
