@@ -15,7 +15,7 @@ namespace lagkv {
 
 constexpr int kBoundsThreads = 256;
 constexpr int kScoreThreads = 128;
-constexpr int kScoreHeads = 4;                   // query heads whose sums a lane holds at a time
+constexpr int kScoreHeads = 8;                   // query heads of one pass of matrix products
 constexpr int kScoreChunk = 32;                  // blocks that a CTA takes in one go
 constexpr int kSelectThreads = 256;
 constexpr int kSelectBins = 2048;
@@ -149,17 +149,22 @@ struct ScoreShape {
     float* error;         // [units][chunks]
 };
 
-// A warp takes NB blocks at a time, a lane a few pairs of channels of each; with q = q+ + q- (its positive and
-// negative parts) a block's bound is sum q+ max + q- min, two packed multiply-adds per pair.  The 32 (or
-// 16) sums of a warp are joined in one transposed reduction.  Products of 16-bit values are exact; each of the
-// 2 D additions is off by at most 2^-24 of sum |q_c| m_c <= |q| |m|, m_c = max(|min_c|, |max_c|).
+// With q = q+ + q- (its positive and negative parts) a block's bound is sum q+ max + q- min: a product of 16-bit
+// matrices, eight heads by eight blocks a warp.  The order of the channels in a sum is free, so a lane loads
+// 16-byte pieces as they lie and both operands meet them in that order.  Products of 16-bit values are exact; each
+// of the D additions that are not of zeros is off by at most 2^-23 of sum |q_c| m_c <= |q| |m|, m_c =
+// max(|min_c|, |max_c|); E allows twice that.  (Multiply-adds in the lanes and shuffles took 23 us where
+// this takes 16, at eight caches of 2048 blocks.)
 template <int DT, int D>
 __global__ void __launch_bounds__(kScoreThreads)
 lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, const ScoreShape S) {
-    constexpr int ROWB = D * Elem<DT>::EB, PAIRS = D / 2, K = (PAIRS + 31) / 32, NB = K > 2 ? 4 : 8, NV = NB * kScoreHeads;
+    using E = Elem<DT>;
+    using X = Mma<DT>;
+    constexpr int ROWB = D * E::EB, CPR = ROWB / 16, K = (CPR + 3) / 4, EPC = 16 / E::EB;  // pieces per row and lane, channels per piece
+    constexpr int W = 4 * E::PW;                                                            // 16-bit pairs per piece
     __shared__ float red[kScoreThreads / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = lane & 3, row = lane >> 2;
     const long long unit = blockIdx.x / S.chunks;  // (b * T + t) * H + h
     const int h = int(unit % P.H), t = int(unit / P.H % P.T), b = int(unit / P.H / P.T), chunk = int(blockIdx.x % S.chunks);
     const AttendSeq seq = attend_seq(P, b, false);
@@ -168,93 +173,103 @@ lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bound
     const int j0 = chunk * S.chunk, j1 = min(nb, j0 + S.chunk);
     if (j0 >= nb || nb <= P.keep) return;  // nothing to choose
     const uint8_t* rows = bounds + ((long long)b * P.H + h) * S.blocks * 2 * ROWB;
-    const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G) * P.q_sh;
-    const f32x2 zero = 0ull;
     float q2 = 0.f, m2 = 0.f;  // largest squared norms
-    for (int j = j0 + w * NB; j < j1; j += kScoreThreads / 32 * NB) {
-        f32x2 lo[NB][K], hi[NB][K];
+    for (int g0 = 0; g0 < P.G; g0 += kScoreHeads) {
+        const bool head = g0 + row < P.G;
+        const uint16_t* q = P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G + min(g0 + row, P.G - 1)) * P.q_sh;
+        // this lane's channels of its head, positive and negative parts (fp8: scaled to fp16 by a power of two)
+        uint32_t pos[K][W], neg[K][W];
+        float n2 = 0.f, back = 1.f, top = 0.f;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const uint8_t* row = rows + (long long)min(j + i, nb - 1) * 2 * ROWB;
+        for (int k = 0; k < K; ++k) {
+            const bool in = CPR % 4 == 0 || c + 4 * k < CPR;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                pos[k][i] = in ? __ldg(reinterpret_cast<const uint32_t*>(q + (c + 4 * k) * EPC) + i) : 0u;
+                const float x = q_to_float(uint16_t(pos[k][i]), DT == 1), y = q_to_float(uint16_t(pos[k][i] >> 16), DT == 1);
+                n2 = fmaf(x, x, fmaf(y, y, n2));
+                top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+            }
+        }
+        if (DT == 2) {
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+            const int e = (__float_as_int(top) >> 23) & 255;
+            const float f = e > 0 && e < 255 ? __int_as_float(min(262 - e, 254) << 23) : 1.f;
+            back = 1.f / f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < W; ++i) pos[k][i] = MmaHalf::pack(Elem<0>::lo(pos[k][i]) * f, Elem<0>::hi(pos[k][i]) * f);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                neg[k][i] = E::min2(pos[k][i], 0u);
+                pos[k][i] = E::max2(pos[k][i], 0u);
+            }
+        n2 += __shfl_xor_sync(~0u, n2, 1);
+        n2 += __shfl_xor_sync(~0u, n2, 2);
+        q2 = fmaxf(q2, n2 == n2 ? n2 : INFINITY);
+        for (int j = j0 + w * 8; j < j1; j += kScoreThreads / 32 * 8) {
+            const uint8_t* lo = rows + (long long)min(j + row, nb - 1) * 2 * ROWB;
+            uint4 vl[K], vh[K];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const bool in = PAIRS % 32 == 0 || lane + 32 * k < PAIRS;
-                lo[i][k] = in ? bound_pair<DT>(row, lane + 32 * k) : zero;
-                hi[i][k] = in ? bound_pair<DT>(row + ROWB, lane + 32 * k) : zero;
+                const bool in = CPR % 4 == 0 || c + 4 * k < CPR;
+                vl[k] = in ? __ldg(reinterpret_cast<const uint4*>(lo) + c + 4 * k) : make_uint4(0u, 0u, 0u, 0u);
+                vh[k] = in ? __ldg(reinterpret_cast<const uint4*>(lo + ROWB) + c + 4 * k) : make_uint4(0u, 0u, 0u, 0u);
             }
-        }
-        float best = -INFINITY;
-        for (int g0 = 0; g0 < P.G; g0 += kScoreHeads) {
-            float v[NV];
-#pragma unroll
-            for (int g = 0; g < kScoreHeads; ++g) {
-                const uint16_t* q = q0 + (long long)min(g0 + g, P.G - 1) * P.q_sh;  // heads behind the last repeat it
-                f32x2 pos[K], neg[K], n2 = zero;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const bool in = PAIRS % 32 == 0 || lane + 32 * k < PAIRS;
-                    const f32x2 x = in ? query_pair<DT>(q, lane + 32 * k) : zero;
-                    float a, c;
-                    unpack2(x, a, c);
-                    pos[k] = pack2(fmaxf(a, 0.f), fmaxf(c, 0.f));
-                    neg[k] = pack2(fminf(a, 0.f), fminf(c, 0.f));
-                    n2 = fma2(x, x, n2);
-                }
-                if (j == j0 + w * NB) {  // once per warp
-                    float a, c;
-                    unpack2(n2, a, c);
-                    a += c;
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
-                    q2 = fmaxf(q2, a == a ? a : INFINITY);
-                }
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    f32x2 sum = zero;
-#pragma unroll
-                    for (int k = 0; k < K; ++k) sum = fma2(pos[k], hi[i][k], fma2(neg[k], lo[i][k], sum));
-                    float a, c;
-                    unpack2(sum, a, c);
-                    v[i * kScoreHeads + g] = a + c;
-                }
-            }
-            transposed_reduce<NV, 32>(v, lane);  // lane l holds (block, head) l * NV / 32
-            constexpr int STEP = 32 / NV;
-            float s = v[0];
-            bool nan = s != s;
-            s = fmaxf(s, __shfl_xor_sync(~0u, s, STEP));
-            s = fmaxf(s, __shfl_xor_sync(~0u, s, 2 * STEP));
-            const unsigned any = __ballot_sync(~0u, nan);
-            if (any >> (lane & ~(4 * STEP - 1)) & ((1ull << (4 * STEP)) - 1)) s = NAN;  // decided in 64 bits
-            best = s != s || best != best ? NAN : fmaxf(best, s);
-        }
-        constexpr int LANES = 32 / NB;  // lanes that hold a block's score
-        const int at = j + lane / LANES;
-        if (lane % LANES == 0 && at < j1) S.approx[unit * S.blocks + at] = best;
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            float n = 0.f;
+            float acc[4] = {0.f, 0.f, 0.f, 0.f}, n = 0.f;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a, c, d, e;
-                unpack2(lo[i][k], a, c);
-                unpack2(hi[i][k], d, e);
-                const float x = fmaxf(fabsf(a), fabsf(d)), y = fmaxf(fabsf(c), fabsf(e));
-                n = fmaf(x, x, fmaf(y, y, n));
-            }
-            lo[i][0] = pack2(n, 0.f);
-        }
-        float n[NB];
+                const uint32_t wl[4] = {vl[k].x, vl[k].y, vl[k].z, vl[k].w}, wh[4] = {vh[k].x, vh[k].y, vh[k].z, vh[k].w};
+                uint32_t pl[W], ph[W];
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            float z;
-            unpack2(lo[i][0], n[i], z);
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t x[E::PW], y[E::PW];
+                    E::expand(wl[i], x);
+                    E::expand(wh[i], y);
+#pragma unroll
+                    for (int e = 0; e < E::PW; ++e) {
+                        pl[i * E::PW + e] = x[e];
+                        ph[i * E::PW + e] = y[e];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < W; i += 2) {
+                    const uint32_t ap[4] = {pos[k][i], 0u, pos[k][i + 1], 0u}, an[4] = {neg[k][i], 0u, neg[k][i + 1], 0u};
+                    X::mma(acc, ap, ph[i], ph[i + 1]);
+                    X::mma(acc, an, pl[i], pl[i + 1]);
+                }
+                if (g0 == 0) {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const float x = fmaxf(fabsf(E::lo(pl[i])), fabsf(E::lo(ph[i]))), y = fmaxf(fabsf(E::hi(pl[i])), fabsf(E::hi(ph[i])));
+                        n = fmaf(x, x, fmaf(y, y, n));
+                    }
+                }
+            }
+            // acc[0], acc[1]: head `row`, blocks 2 c and 2 c + 1: the largest over the heads
+            float s0 = head ? acc[0] * back : -INFINITY, s1 = head ? acc[1] * back : -INFINITY;
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                s0 = fmaxf(s0, __shfl_xor_sync(~0u, s0, o));
+                s1 = fmaxf(s1, __shfl_xor_sync(~0u, s1, o));
+            }
+            if (lane < 4) {
+                float* to = S.approx + unit * S.blocks + j + 2 * c;
+                if (j + 2 * c < j1) to[0] = g0 ? fmaxf(to[0], s0) : s0;
+                if (j + 2 * c + 1 < j1) to[1] = g0 ? fmaxf(to[1], s1) : s1;
+            }
+            n += __shfl_xor_sync(~0u, n, 1);
+            n += __shfl_xor_sync(~0u, n, 2);
+            m2 = fmaxf(m2, n == n ? n : INFINITY);
         }
-        transposed_reduce<NB, 32>(n, lane);
-        m2 = fmaxf(m2, n[0] == n[0] ? n[0] : INFINITY);
     }
     // 1.01: the roundings of the norms themselves
-    const float e = 1.01f * (2 * D + 8) * 0x1p-24f * sqrtf(q2) * sqrtf(max_of_warp(m2)) + 1e-37f;
+    const float e = 1.01f * (D + 16) * 0x1p-22f * sqrtf(max_of_warp(q2)) * sqrtf(max_of_warp(m2)) + 1e-37f;
     if (lane == 0) red[w] = e == e ? e : INFINITY;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -265,11 +280,12 @@ lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bound
 }
 
 // ------------------------------------------------------------------------------------ choice
-// Narrows [lo, hi] (the smallest and the largest of the keys asked about) to the key with `need` - 1 larger ones,
-// by histograms over 2048 bins: returns it and leaves in `need` how many of the keys equal to it are wanted;
-// all = every key equal to it (or, early, of its bin: then the returned key is the bin's lowest).
-template <class Key, class Get>
-__device__ __forceinline__ Key find_border(Key lo, Key hi, int n, int& need, bool& all, int* hist, int* wsum, int* found, Get&& get) {
+// Narrows [lo, hi] (the smallest and the largest of the keys asked about) around the key with `need` - 1 larger
+// ones, by histograms over 2048 bins, until enough(lo, hi) or the interval is one key; leaves in `need` how many
+// of the keys in [lo, hi] are wanted, and in `all` whether that is all of them.
+template <class Key, class Get, class Enough>
+__device__ __forceinline__ void find_border(Key& lo, Key& hi, int n, int& need, bool& all, int* hist, int* wsum, int* found, Get&& get,
+                                            Enough&& enough) {
     constexpr int NW = kSelectThreads / 32, PER = kSelectBins / kSelectThreads;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     for (;;) {
@@ -317,7 +333,7 @@ __device__ __forceinline__ Key find_border(Key lo, Key hi, int n, int& need, boo
         lo = new_lo;
         need = found[1];
         all = found[2] == need;
-        if (lo == hi || (sizeof(Key) == 8 && all)) return lo;
+        if (lo == hi || enough(lo, hi)) return;
     }
 }
 
@@ -403,11 +419,12 @@ lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ boun
         hi = uint32_t(range[1]);
         bool all;
         int rank = need;
-        const uint32_t border = find_border<uint32_t>(lo, hi, n, rank, all, hist, wsum[0], found, [&](int j) { return float_key(sa[j]); });
-        // float of the key: the need-th largest 32-bit score; the need-th largest 64-bit one is within E of it
-        const float tau = __uint_as_float(border >> 31 ? border & 0x7fffffffu : ~border);
-        const float above = tau + 2.f * error * 1.0001f, below = tau - 2.f * error * 1.0001f;
-        const float over = fabsf(tau) * 0x1p-22f;  // the two sums above are rounded
+        auto value = [](uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); };
+        find_border<uint32_t>(lo, hi, n, rank, all, hist, wsum[0], found, [&](int j) { return float_key(sa[j]); },
+                              [&](uint32_t x, uint32_t y) { return value(y) - value(x) <= error; });
+        // the need-th largest 32-bit score is in [lo, hi], the need-th largest 64-bit one within E of that
+        const float above = value(hi) + 2.f * error * 1.0001f, below = value(lo) - 2.f * error * 1.0001f;
+        const float over = fmaxf(fabsf(value(lo)), fabsf(value(hi))) * 0x1p-22f;  // the two sums above are rounded
         auto sure = [&](float a) { return a > above + over; };
         auto out_of_it = [&](float a) { return a < below - over; };
         int* near = reinterpret_cast<int*>(sa) + n;
@@ -467,8 +484,9 @@ lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ boun
                 }
             }
             __syncthreads();
-            const unsigned long long k = find_border<unsigned long long>(range[0], range[1], total_near, wanted, all, hist, wsum[0], found,
-                                                                         [&](int i) { return mine[i]; });
+            unsigned long long k = range[0], k_hi = range[1];
+            find_border<unsigned long long>(k, k_hi, total_near, wanted, all, hist, wsum[0], found, [&](int i) { return mine[i]; },
+                                            [&](unsigned long long, unsigned long long) { return all; });
             // the chosen ones become certain, the others impossible; of keys equal to k the lowest blocks
             const int pn = (total_near + kSelectThreads - 1) / kSelectThreads, i0 = min(total_near, tid * pn), i1 = min(total_near, i0 + pn);
             int ne = 0;

@@ -11,7 +11,7 @@
 namespace lagkv {
 
 constexpr int kPageThreads = 256;
-constexpr int kScanThreads = 1024;
+constexpr int kScanThreads = 512;
 constexpr int kCopyVectors = 4;                                   // 16-byte vectors per thread and step
 constexpr int kCopySlice = kPageThreads * kCopyVectors;           // vectors of one CTA step
 
@@ -41,11 +41,12 @@ __device__ __forceinline__ int cta_scan(int v, int* sums, int* total) {
     __syncthreads();
     if (lane == 31) sums[w] = inc;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int i = 0; i < nw; ++i) {
-        if (i < w) before += sums[i];
-        all += sums[i];
+    int part = lane < nw ? sums[lane] : 0;  // every warp scans the warps' sums itself
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(~0u, part, o);
+        if (lane >= o) part += u;
     }
+    const int all = __shfl_sync(~0u, part, 31), before = w ? __shfl_sync(~0u, part, w - 1) : 0;
     *total = all;
     return before + inc;
 }
@@ -239,6 +240,14 @@ lagkv_pages_fork_plan_kernel(const PageParams P, const int32_t* __restrict__ seq
     }
     const bool fits = need == 0 || find_free(P, need, sums) >= need;
     if (!fits && tid == 0) record_status(P.status, ST_ECAPACITY, -1);
+    __syncthreads();
+    // the pages to copy, in the order of those found for them
+    for (int k = tid >> 5; fits && k < n; k += kScanThreads / 32) {
+        const int32_t* u = P.work + (long long)k * kPairWords;
+        if (u[0] < 0) continue;
+        for (int j = __ldcg(u + 2) + (tid & 31); j < __ldcg(u + 1); j += 32)
+            P.list[P.num_pages + u[0] + j - __ldcg(u + 2)] = P.table[(long long)src[k] * P.max_blocks + j];
+    }
     if (tid == 0) owner[P.B] = fits ? int(need) : -1;  // copies to make; -1: too few free pages, nothing changes
 }
 
@@ -294,25 +303,7 @@ lagkv_pages_fork_kernel(const PageParams P, int32_t* seq_len, int32_t* static_le
     const long long items = 2ll * copies * slices;
     for (long long it = blockIdx.x; it < items; it += gridDim.x) {
         const int slice = int(it % slices), which = int(it / slices & 1), c = int(it / slices >> 1);
-        // the last pair that starts at or before copy c and has any
-        int lo = 0, hi = n - 1, at = 0;
-        while (lo <= hi) {
-            int mid = (lo + hi) >> 1, k = mid;
-            while (k >= lo && P.work[(long long)k * kPairWords] < 0) --k;  // refused pairs have no number
-            if (k < lo) {
-                lo = mid + 1;
-                continue;
-            }
-            if (P.work[(long long)k * kPairWords] <= c) {
-                at = k;
-                lo = mid + 1;
-            } else {
-                hi = k - 1;
-            }
-        }
-        const int32_t* w = P.work + (long long)at * kPairWords;
-        const int j = w[2] + c - w[0];
-        copy_slice(P, P.table[(long long)src[at] * P.max_blocks + j], P.list[c], which, slice, vectors);
+        copy_slice(P, P.list[P.num_pages + c], P.list[c], which, slice, vectors);
     }
 }
 
