@@ -17,7 +17,7 @@ constexpr int kBoundsThreads = 256;
 constexpr int kScoreThreads = 128;
 constexpr int kScoreHeads = 8;                   // query heads of one pass of matrix products
 constexpr int kScoreChunk = 32;                  // blocks that a CTA takes in one go
-constexpr int kSelectThreads = 256;
+constexpr int kSelectThreads = 512;
 constexpr int kSelectBins = 2048;
 
 // ------------------------------------------------------------------------------------ bounds
@@ -310,10 +310,7 @@ __device__ __forceinline__ void find_border(Key& lo, Key& hi, int n, int& need, 
         }
         if (lane == 31) wsum[w] = inc;
         __syncthreads();
-        int before = inc - mine;
-#pragma unroll
-        for (int i = 0; i < NW; ++i)
-            if (i < w) before += wsum[i];
+        const int before = inc - mine + __reduce_add_sync(~0u, lane < w && lane < NW ? wsum[lane] : 0);
         if (before < need && before + mine >= need) {
             int at = before;
             for (int i = PER - 1; i >= 0; --i) {
@@ -337,25 +334,34 @@ __device__ __forceinline__ void find_border(Key& lo, Key& hi, int n, int& need, 
     }
 }
 
-// The 64-bit score of a block, by one warp.
+// The 64-bit bound of one block for one query head, by eight lanes.
 template <int DT>
-__device__ __forceinline__ double exact_score(const AttendParams& P, const uint8_t* row, const uint16_t* q0, int D, int rowb, int lane) {
-    double best = -INFINITY;
-    for (int g = 0; g < P.G; ++g) {
-        double sum = 0.0;
-        for (int p = lane; p < D / 2; p += 32) {
-            float q[2], lo[2], hi[2];
-            unpack2(query_pair<DT>(q0 + (long long)g * P.q_sh, p), q[0], q[1]);
-            unpack2(bound_pair<DT>(row, p), lo[0], lo[1]);
-            unpack2(bound_pair<DT>(row + rowb, p), hi[0], hi[1]);
+__device__ __forceinline__ double exact_bound(const uint8_t* row, const uint16_t* q0, int D, int rowb, int lane) {
+    double sum = 0.0;
+#pragma unroll 4
+    for (int p = lane; p < D / 2; p += 8) {
+        float q[2], lo[2], hi[2];
+        unpack2(query_pair<DT>(q0, p), q[0], q[1]);
+        unpack2(bound_pair<DT>(row, p), lo[0], lo[1]);
+        unpack2(bound_pair<DT>(row + rowb, p), hi[0], hi[1]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) sum = fma(double(q[e]), double(q[e] >= 0.f ? hi[e] : lo[e]), sum);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-        best = fmax(best, sum);
+        for (int e = 0; e < 2; ++e) sum = fma(double(q[e]), double(q[e] >= 0.f ? hi[e] : lo[e]), sum);
     }
-    return best;
+#pragma unroll
+    for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    return sum;
+}
+
+// Numbers in order for what the CTA's warps count: v is the warp's count; returns the sum over the warps before it.
+__device__ __forceinline__ int warps_before(int v, int* wsum, int& total) {
+    constexpr int NW = kSelectThreads / 32;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    __syncthreads();
+    if (lane == 0) wsum[w] = v;
+    __syncthreads();
+    const int x = lane < NW ? wsum[lane] : 0;
+    total = __reduce_add_sync(~0u, x);
+    return __reduce_add_sync(~0u, lane < w ? x : 0);
 }
 
 // One CTA per (sequence, token, KV head): the first `sink` and last `recent` blocks and the best of the
@@ -365,10 +371,11 @@ __global__ void __launch_bounds__(kSelectThreads)
 lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, const ScoreShape S, int D,
                           unsigned long long* __restrict__ keys, int sink, int recent, int32_t* __restrict__ idx) {
     extern __shared__ float sa[];  // the candidates' scores, then the numbers of those near the border
-    __shared__ int hist[kSelectBins];
-    __shared__ float red[2][kSelectThreads / 32];
+    __shared__ __align__(8) int hist[kSelectBins];
+    __shared__ uint32_t ends[2][kSelectThreads / 32];
+    __shared__ float errors[kSelectThreads / 32];
     __shared__ int wsum[2][kSelectThreads / 32];
-    __shared__ int found[4];
+    __shared__ int found[3];
     __shared__ unsigned long long range[2];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -384,159 +391,147 @@ lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ boun
         for (int i = tid; i < P.keep; i += kSelectThreads) out[i] = i < nb ? i : -1;
         return;
     }
+    float above = 0.f, below = 0.f, over = 0.f;
+    bool near_all = false;
+    auto sure = [&](float a) { return a > above + over; };
+    auto out_of_it = [&](float a) { return a < below - over; };
     // candidates: blocks [sink, nb - recent); nb > keep >= sink + recent, so there are more than are wanted
     const int n = nb - recent - sink;
     int need = P.keep - sink - recent;
     if (need > 0) {
         uint32_t lo = ~0u, hi = 0u;
         float error = 0.f;
-        for (int j = tid; j < n; j += kSelectThreads) {
-            const float a = __ldcg(S.approx + unit * S.blocks + sink + j);
-            sa[j] = a;
-            const uint32_t k = float_key(a);
-            lo = min(lo, k);
-            hi = max(hi, k);
+        const float* approx = S.approx + unit * S.blocks + sink;
+        for (int j = tid; j < n; j += 4 * kSelectThreads) {  // a block taken twice changes neither end
+            float a[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = __ldcg(approx + min(j + i * kSelectThreads, n - 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (j + i * kSelectThreads < n) sa[j + i * kSelectThreads] = a[i];
+                lo = min(lo, float_key(a[i]));
+                hi = max(hi, float_key(a[i]));
+            }
         }
         for (int c = tid; c < (nb + S.chunk - 1) / S.chunk; c += kSelectThreads) error = fmaxf(error, __ldcg(S.error + unit * S.chunks + c));
-        if (tid == 0) {
-            range[0] = ~0ull;
-            range[1] = 0ull;
-            found[3] = 0;
-        }
-        __syncthreads();
         lo = __reduce_min_sync(~0u, lo);
         hi = __reduce_max_sync(~0u, hi);
         error = max_of_warp(error);
         if (lane == 0) {
-            atomicMin(&range[0], (unsigned long long)lo);
-            atomicMax(&range[1], (unsigned long long)hi);
-            red[0][w] = error;
+            ends[0][w] = lo;
+            ends[1][w] = hi;
+            errors[w] = error;
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NW; ++i) error = fmaxf(error, red[0][i]);
-        lo = uint32_t(range[0]);
-        hi = uint32_t(range[1]);
+        lo = __reduce_min_sync(~0u, ends[0][lane % NW]);
+        hi = __reduce_max_sync(~0u, ends[1][lane % NW]);
+        error = max_of_warp(errors[lane % NW]);
         bool all;
         int rank = need;
         auto value = [](uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); };
         find_border<uint32_t>(lo, hi, n, rank, all, hist, wsum[0], found, [&](int j) { return float_key(sa[j]); },
                               [&](uint32_t x, uint32_t y) { return value(y) - value(x) <= error; });
         // the need-th largest 32-bit score is in [lo, hi], the need-th largest 64-bit one within E of that
-        const float above = value(hi) + 2.f * error * 1.0001f, below = value(lo) - 2.f * error * 1.0001f;
-        const float over = fmaxf(fabsf(value(lo)), fabsf(value(hi))) * 0x1p-22f;  // the two sums above are rounded
-        auto sure = [&](float a) { return a > above + over; };
-        auto out_of_it = [&](float a) { return a < below - over; };
+        above = value(hi) + 2.f * error * 1.0001f;
+        below = value(lo) - 2.f * error * 1.0001f;
+        over = fmaxf(fabsf(value(lo)), fabsf(value(hi))) * 0x1p-22f;  // the two sums above are rounded
         int* near = reinterpret_cast<int*>(sa) + n;
-        // blocks near the border, in their order: each thread a run of candidates
-        const int per = (n + kSelectThreads - 1) / kSelectThreads, j0 = min(n, tid * per), j1 = min(n, j0 + per);
+        // blocks near the border, in their order: a warp takes a run of candidates
+        const int run = ((n + kSelectThreads - 1) / kSelectThreads) * 32, j0 = min(n, w * run), j1 = min(n, j0 + run);
         int ni = 0, na = 0;
-        for (int j = j0; j < j1; ++j) {
-            const float a = sa[j];
-            ni += sure(a);
-            na += !sure(a) && !out_of_it(a);
+        for (int j = j0 + lane; j < j1; j += 32) {
+            ni += sure(sa[j]);
+            na += !sure(sa[j]) && !out_of_it(sa[j]);
         }
-        int ii = ni, ia = na;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(~0u, ii, o), y = __shfl_up_sync(~0u, ia, o);
-            if (lane >= o) {
-                ii += x;
-                ia += y;
-            }
-        }
-        __syncthreads();
-        if (lane == 31) {
-            wsum[0][w] = ii;
-            wsum[1][w] = ia;
-        }
-        __syncthreads();
-        int total_in = 0, total_near = 0, at = ia - na;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < w) at += wsum[1][i];
-            total_in += wsum[0][i];
-            total_near += wsum[1][i];
-        }
+        int total_in, total_near;
+        warps_before(__reduce_add_sync(~0u, ni), wsum[0], total_in);
+        int at = warps_before(__reduce_add_sync(~0u, na), wsum[1], total_near);
         int wanted = need - total_in;  // of the blocks near the border; at least one
-        const bool near_all = wanted >= total_near;
+        near_all = wanted >= total_near;
         if (!near_all) {
-            for (int j = j0; j < j1; ++j) {
-                const float a = sa[j];
-                if (!sure(a) && !out_of_it(a)) near[at++] = j;
+            for (int j = j0; j < j1; j += 32) {
+                const bool in = j + lane < j1 && !sure(sa[j + lane]) && !out_of_it(sa[j + lane]);
+                const uint32_t m = __ballot_sync(~0u, in);
+                if (in) near[at + __popc(m & ((1u << lane) - 1))] = j + lane;
+                at += __popc(m);
             }
             __syncthreads();
             const int rowb = D * Elem<DT>::EB;
             const uint8_t* rows = bounds + (((long long)b * P.H + h) * S.blocks + sink) * 2 * rowb;
             const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)t * P.q_st + (long long)(h * P.G) * P.q_sh;
-            unsigned long long* mine = keys + unit * S.blocks;
-            if (tid == 0) {
-                range[0] = ~0ull;
-                range[1] = 0ull;
+            const bool few = total_near <= kSelectThreads;
+            unsigned long long* mine = few ? reinterpret_cast<unsigned long long*>(hist) : keys + unit * S.blocks;
+            for (int i = tid; i < total_near; i += kSelectThreads) mine[i] = 0ull;
+            __syncthreads();
+            const int pairs = total_near * P.G;
+            for (int i0 = w * 4; i0 < pairs; i0 += NW * 4) {
+                const int i = min(i0 + (lane >> 3), pairs - 1), j = i / P.G;  // a pair taken twice changes no maximum
+                const double sum = exact_bound<DT>(rows + (long long)near[j] * 2 * rowb, q0 + (long long)(i - j * P.G) * P.q_sh, D, rowb, lane & 7);
+                if ((lane & 7) == 0) atomicMax(&mine[j], double_key(sum == sum ? sum : -INFINITY));
             }
             __syncthreads();
-            for (int i = w; i < total_near; i += NW) {
-                const unsigned long long k = double_key(exact_score<DT>(P, rows + (long long)near[i] * 2 * rowb, q0, D, rowb, lane));
-                if (lane == 0) {
-                    mine[i] = k;
-                    atomicMin(&range[0], k);
-                    atomicMax(&range[1], k);
+            // The chosen ones become certain, the others impossible.  Few are ranked one against another (for the
+            // usual handful TIMEX us less than the histograms), many by the histograms.
+            if (few) {
+                if (tid < total_near) {
+                    const unsigned long long k = mine[tid];
+                    int above_it = 0;
+                    for (int i = 0; i < total_near; ++i) above_it += mine[i] > k || (mine[i] == k && i < tid);
+                    sa[near[tid]] = above_it < wanted ? INFINITY : -INFINITY;
+                }
+            } else {
+                if (tid == 0) {
+                    range[0] = ~0ull;
+                    range[1] = 0ull;
+                }
+                __syncthreads();
+                for (int i = tid; i < total_near; i += kSelectThreads) {
+                    atomicMin(&range[0], mine[i]);
+                    atomicMax(&range[1], mine[i]);
+                }
+                __syncthreads();
+                unsigned long long k = range[0], k_hi = range[1];
+                find_border<unsigned long long>(k, k_hi, total_near, wanted, all, hist, wsum[0], found, [&](int i) { return mine[i]; },
+                                                [&](unsigned long long, unsigned long long) { return all; });
+                // of keys equal to k the lowest blocks
+                const int pn = (total_near + kSelectThreads - 1) / kSelectThreads, i0 = min(total_near, tid * pn), i1 = min(total_near, i0 + pn);
+                int ne = 0;
+                for (int i = i0; i < i1; ++i) ne += mine[i] == k;
+                int ie = ne;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int x = __shfl_up_sync(~0u, ie, o);
+                    if (lane >= o) ie += x;
+                }
+                int all_equal;
+                int be = warps_before(__shfl_sync(~0u, ie, 31), wsum[0], all_equal) + ie - ne;
+                for (int i = i0; i < i1; ++i) {
+                    const bool in = all ? mine[i] >= k : mine[i] > k || (mine[i] == k && be < wanted);
+                    be += mine[i] == k;
+                    sa[near[i]] = in ? INFINITY : -INFINITY;
                 }
             }
             __syncthreads();
-            unsigned long long k = range[0], k_hi = range[1];
-            find_border<unsigned long long>(k, k_hi, total_near, wanted, all, hist, wsum[0], found, [&](int i) { return mine[i]; },
-                                            [&](unsigned long long, unsigned long long) { return all; });
-            // the chosen ones become certain, the others impossible; of keys equal to k the lowest blocks
-            const int pn = (total_near + kSelectThreads - 1) / kSelectThreads, i0 = min(total_near, tid * pn), i1 = min(total_near, i0 + pn);
-            int ne = 0;
-            for (int i = i0; i < i1; ++i) ne += mine[i] == k;
-            int ie = ne;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(~0u, ie, o);
-                if (lane >= o) ie += x;
-            }
-            __syncthreads();
-            if (lane == 31) wsum[0][w] = ie;
-            __syncthreads();
-            int be = ie - ne;
-#pragma unroll
-            for (int i = 0; i < NW; ++i)
-                if (i < w) be += wsum[0][i];
-            for (int i = i0; i < i1; ++i) {
-                const bool in = all ? mine[i] >= k : mine[i] > k || (mine[i] == k && be < wanted);
-                be += mine[i] == k;
-                sa[near[i]] = in ? INFINITY : -INFINITY;
-            }
-            __syncthreads();
         }
-        for (int j = j0; j < j1; ++j) {
-            const float a = sa[j];
-            sa[j] = sure(a) || a == INFINITY || (near_all && !out_of_it(a)) ? 1.f : 0.f;
-        }
-        __syncthreads();
     }
-    // ordered output: each thread a run of blocks
-    const int per = (nb + kSelectThreads - 1) / kSelectThreads, j0 = min(nb, tid * per), j1 = min(nb, j0 + per);
-    auto taken = [&](int j) { return j < sink || j >= sink + n || (need > 0 && sa[j - sink] != 0.f); };
-    int c = 0;
-    for (int j = j0; j < j1; ++j) c += taken(j);
-    int inc = c;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(~0u, inc, o);
-        if (lane >= o) inc += v;
+    // ordered output: a warp takes a run of blocks
+    auto taken = [&](int j) {
+        if (j >= nb) return false;
+        if (j < sink || j >= sink + n) return true;
+        if (need == 0) return false;
+        const float a = sa[j - sink];
+        return sure(a) || a == INFINITY || (near_all && !out_of_it(a));
+    };
+    const int run = ((nb + kSelectThreads - 1) / kSelectThreads) * 32, j0 = w * run, j1 = min(nb, j0 + run);
+    int c = 0, total;
+    for (int j = j0 + lane; j < j1; j += 32) c += taken(j);
+    int at = warps_before(__reduce_add_sync(~0u, c), wsum[0], total);
+    for (int j = j0; j < j1; j += 32) {
+        const bool in = taken(j + lane);
+        const uint32_t m = __ballot_sync(~0u, in);
+        if (in) out[at + __popc(m & ((1u << lane) - 1))] = j + lane;
+        at += __popc(m);
     }
-    __syncthreads();
-    if (lane == 31) wsum[0][w] = inc;
-    __syncthreads();
-    int at = inc - c;
-#pragma unroll
-    for (int i = 0; i < NW; ++i)
-        if (i < w) at += wsum[0][i];
-    for (int j = j0; j < j1; ++j)
-        if (taken(j)) out[at++] = j;
 }
 
 }  // namespace lagkv
