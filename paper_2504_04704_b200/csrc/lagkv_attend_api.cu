@@ -32,10 +32,9 @@ const AttendEntry* find_attend(int D, int dtype, int rows_wanted, bool blocks, i
     return best;
 }
 
-// Workspace: [status block | counters, a sixteenth of the rest | partials | block choice].  The counters'
-// place depends on the workspace's size alone, so calls of different shapes find them cleared.
+// Workspace: [status block | partials | who shares which unit | block choice].  Only the status block outlasts
+// a call.
 constexpr size_t kHead = kStatusWords * sizeof(int32_t);
-size_t counter_bytes(size_t workspace_bytes) { return ((workspace_bytes - kHead) / 16) & ~size_t(255); }
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
 size_t partial_bytes(const lagkv_plan_s* plan, const AttendEntry& e) {
@@ -147,19 +146,18 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     const long long units = attend_units(plan, *e, query_rows, tokens);
     int rc = workspace_ok(workspace, bytes, kHead + 4096);
     if (rc != LAGKV_OK) return rc;
-    // a narrow kernel's CTAs count arrivals per unit; a wide one's say who shares a unit
-    const size_t cb = counter_bytes(bytes), pb = partial_bytes(plan, *e) + (e->wide ? up256(size_t(units) * sizeof(int2)) : 0);
+    const size_t pb = partial_bytes(plan, *e), sb = up256(size_t(units) * sizeof(int2));
     if (units * e->rows > 0x7fffffffll) return LAGKV_EINVAL;
-    if (size_t(units) * sizeof(int32_t) > cb || kHead + cb + pb + extra > bytes) return LAGKV_EWORKSPACE;
+    if (kHead + pb + sb + extra > bytes) return LAGKV_EWORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(workspace);
     P->status = reinterpret_cast<int32_t*>(base);
-    P->counters = reinterpret_cast<int32_t*>(base + kHead);
-    P->partials = reinterpret_cast<float*>(base + kHead + cb);
-    P->shared = reinterpret_cast<int2*>(base + kHead + cb + partial_bytes(plan, *e));
+    P->partials = reinterpret_cast<float*>(base + kHead);
+    P->shared = reinterpret_cast<int2*>(base + kHead + pb);
     P->mtiles = (query_rows + e->rows - 1) / e->rows;
+    P->ctas = plan->sm_count * e->ctas_per_sm;
     P->lead = e->wide ? kWideLead : kAttendLead;
     *entry = e;
-    *rest = base + kHead + cb + pb;
+    *rest = base + kHead + pb + sb;
     if (!(plan->attend_ready.load(std::memory_order_acquire) >> index & 1)) {
         if (!raise_smem_limit(e->fn, e->smem)) return LAGKV_ECUDA;
         plan->attend_ready.fetch_or(1ull << index, std::memory_order_release);
@@ -198,6 +196,13 @@ int cache_map(const lagkv_config& c, const AttendParams& P, const uint8_t* base,
     return r == CUDA_SUCCESS ? LAGKV_OK : LAGKV_EUNSUPPORTED;  // strides of 2^40 bytes and more
 }
 
+// Behind an attention kernel: the kernel that joins the units which several CTAs share.
+int launch_join(const AttendEntry& e, AttendParams& P, int query_rows, long long units, cudaStream_t stream) {
+    const int rows = e.rows < query_rows ? e.rows : query_rows;
+    void* args[] = {&P};
+    return launch_behind(e.join, unsigned(units * ((rows + e.join_rows - 1) / e.join_rows)), e.join_threads, args, 0, stream);
+}
+
 int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cudaStream_t stream) {
     CUtensorMap map_k, map_v;
     if (e.wide) {
@@ -206,14 +211,11 @@ int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cuda
         if (rc != LAGKV_OK) return rc;
     }
     void* args[] = {&P, &map_k, &map_v};
-    if (cudaLaunchKernel(e.fn, dim3((unsigned)(plan->sm_count * e.ctas_per_sm)), dim3(e.threads), args, e.smem, stream) !=
+    if (cudaLaunchKernel(e.fn, dim3((unsigned)P.ctas), dim3(e.threads), args, e.smem, stream) !=
         cudaSuccess)
         return LAGKV_ECUDA;
-    if (e.join != nullptr) {
-        const long long ctas = (long long)P.B * P.H * P.mtiles * (e.rows / kJoinRows);
-        const int rc = launch_behind(e.join, unsigned(ctas), kJoinThreads, args, 0, stream);
-        if (rc != LAGKV_OK) return rc;
-    }
+    const int rc = launch_join(e, P, P.T * P.G, (long long)P.B * P.H * P.mtiles, stream);
+    if (rc != LAGKV_OK) return rc;
     return check_launch();
 }
 
@@ -367,7 +369,8 @@ int attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block
     }
     P.idx = idx;
     void* args[] = {&P};
-    rc = launch_behind(e->fn, unsigned(plan->sm_count * e->ctas_per_sm), unsigned(e->threads), args, e->smem, stream);
+    rc = launch_behind(e->fn, unsigned(P.ctas), unsigned(e->threads), args, e->smem, stream);
+    if (rc == LAGKV_OK) rc = launch_join(*e, P, P.G, units * P.mtiles, stream);
     return rc == LAGKV_OK ? check_launch() : rc;
 }
 
@@ -387,18 +390,15 @@ size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, i
             int index;
             const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows, chosen, &index);
             if (e == nullptr) return 0;
-            const size_t need = partial_bytes(plan, *e) + (e->wide ? up256(size_t(attend_units(plan, *e, T * G, 1)) * sizeof(int2)) : 0);
+            const size_t need = partial_bytes(plan, *e);
             if (need > partials) partials = need;
         }
     }
     const size_t most = size_t(T) * ((G + 15) / 16);  // units per (sequence, KV head): no unit has fewer than 16 rows
     const size_t dense = (size_t(T) * G + 15) / 16;
     units = size_t(plan->cfg.B) * plan->cfg.H_kv * (most > dense ? most : dense);
-    const size_t rest = partials + choice_bytes(plan->cfg, T, blocks, keep), counters = up256(units * sizeof(int32_t));
-    size_t body = rest + rest / 15 + 4096;          // a sixteenth of the body goes to the counters
-    if (body < 16 * (counters + 256)) body = 16 * (counters + 256);
-    if (body - counter_bytes(kHead + body) < rest) body += body / 8;
-    return kHead + up256(body);
+    const size_t body = partials + up256(units * sizeof(int2)) + choice_bytes(plan->cfg, T, blocks, keep);
+    return kHead + (body < 4096 ? 4096 : body);
 }
 
 int lagkv_attend_workspace_init(lagkv_plan_t plan, void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -406,8 +406,7 @@ int lagkv_attend_workspace_init(lagkv_plan_t plan, void* workspace, size_t works
     const int rc = workspace_ok(workspace, workspace_bytes, kHead);
     if (rc != LAGKV_OK) return rc;
     DeviceGuard guard(plan->cfg.device);
-    const size_t clear = kHead + counter_bytes(workspace_bytes);
-    return cudaMemsetAsync(workspace, 0, clear, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LAGKV_OK
+    return cudaMemsetAsync(workspace, 0, kHead, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? LAGKV_OK
                                                                                                         : LAGKV_ECUDA;
 }
 

@@ -29,7 +29,6 @@ struct AttendParams {
     const int32_t* draft_len;         // nullptr: T for every sequence
     const unsigned long long* mask;   // [B, T] visible drafted rows; nullptr: a chain (token t sees rows <= t)
     int32_t* status;
-    int32_t* counters;     // [units], zero between calls
     float* partials;       // [grid * 2][MR * (D + 2)]
     int2* shared;          // wide kernel: first and last CTA of each unit
     long long sb, sh, ss, page_stride;  // bytes
@@ -38,6 +37,7 @@ struct AttendParams {
     long long q_sb, q_st, q_sh;         // elements
     int B, H, G, T, S_cap, max_blocks, page_shift;
     int mtiles;            // groups of M rows per (sequence, KV head)
+    int ctas;              // CTAs of the attention kernel
     int lead;              // what beginning a unit costs, in tiles: counted when the work is shared out
     float scale_log2, v_scale;
     const int32_t* idx;    // blocks: [B, T, H, keep] ascending block numbers, -1 behind the last
@@ -312,43 +312,6 @@ __device__ __forceinline__ void attend_write(const AttendParams& P, int b, int h
     if (d == 0 && P.lse) P.lse[at] = live ? 0.69314718055994531f * (ref + log2f(sum)) : -INFINITY;
 }
 
-// A shared unit's result from the partials of CTAs c0 .. c1, in that order, by `threads` threads.  A CTA's
-// partials: [2 slots][MR * (D + 2)], slot 1 for the unit that starts in its share, slot 0 for the one that
-// it continues.
-template <int D, int DT, int MR>
-__device__ __forceinline__ void attend_combine(const AttendParams& P, int b, int h, int t0, int m0, int mrows, int tokens,
-                                               long long c0, long long c1, int tid, int threads) {
-    for (int i = tid; i < mrows * (D / 4); i += threads) {
-        const int m = i / (D / 4), d = (i % (D / 4)) * 4;
-        float top = -INFINITY, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int BATCH = 4;  // partials in flight: one after the other each costs an L2 round trip
-        for (long long c = c0; c <= c1; c += BATCH) {
-            float2 ml[BATCH];
-            float4 v[BATCH];
-#pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                const long long from = min(c + k, c1);
-                const float* pp = P.partials + (2 * from + (from == c0 ? 1 : 0)) * (MR * (D + 2));
-                ml[k] = __ldcg(reinterpret_cast<const float2*>(pp + MR * D + 2 * m));
-                v[k] = __ldcg(reinterpret_cast<const float4*>(pp + m * D + d));
-            }
-#pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (c + k > c1 || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;
-                const float r = fmaxf(top, ml[k].x);
-                const float fo = top == -INFINITY ? 0.f : ex2(top - r), fn = ex2(ml[k].x - r);
-                total = total * fo + ml[k].y * fn;
-                o[0] = o[0] * fo + v[k].x * fn;
-                o[1] = o[1] * fo + v[k].y * fn;
-                o[2] = o[2] * fo + v[k].z * fn;
-                o[3] = o[3] * fo + v[k].w * fn;
-                top = r;
-            }
-        }
-        attend_write<D, DT>(P, b, h, t0, m0, tokens, m, d, o, top, total);
-    }
-}
-
 template <int D, int DT, int MT>
 __global__ void __launch_bounds__(kAttendWarps * 32, AttendGeo<D, DT, MT>::CTAS)
 lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
@@ -361,7 +324,6 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
     float2* sml = reinterpret_cast<float2*>(smem + G::OFF_ML);
     float* sscale = reinterpret_cast<float*>(smem + G::OFF_SCALE);
     long long* sscan = reinterpret_cast<long long*>(smem + G::OFF_SCAN);
-    int* slast = reinterpret_cast<int*>(smem + G::OFF_SCAN + 8 * G::NW + 32);
 
     const bool blocks = P.idx != nullptr;
     const int upb = (blocks ? P.T : 1) * P.H * P.mtiles;  // units of a sequence
@@ -729,23 +691,85 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
                 if (d == 0) __stcg(reinterpret_cast<float2*>(part + G::MR * D + 2 * m), make_float2(top, total));
             }
         }
-        if (c0 != c1) {
-            __threadfence();
-            __syncthreads();
-            const long long unit = (long long)sh.b * upb + u;
-            if (tid == 0) {
-                const int n = atomicAdd(P.counters + unit, 1);
-                *slast = n == int(c1 - c0);
-                if (*slast) P.counters[unit] = 0;
-            }
-            __syncthreads();
-            if (*slast) {
-                __threadfence();
-                attend_combine<D, DT, G::MR>(P, sh.b, h, t0, m0, mrows, seq.tokens, c0, c1, tid, G::NT);
-            }
-        }
+        // who shares the unit, for the kernel that joins the partials: said once, by the CTA that starts it
+        if (tid == 0 && c0 == (long long)blockIdx.x) P.shared[(long long)sh.b * upb + u] = make_int2(int(c0), int(c1));
         attend_advance(P, sh, part_of.step, seq.tiles, upb);
     }
+}
+
+// Joins the partials of shared units, in the order of their rows: a warp per query row, with the weights of up to
+// 32 partials worked out first, one per lane, so that their reads do not wait for one another.  (The last CTA to
+// arrive joined them at first: a CTA and 37 partials of 16 rows took 20 us.)
+constexpr int kMergeWarps = 4;
+template <int D, int DT, int MT>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+lagkv_attend_merge_kernel(const __grid_constant__ AttendParams P) {
+    constexpr int MR = AttendGeo<D, DT, MT>::MR, PSIZE = MR * (D + 2);
+    constexpr int LANES = D / 4 < 32 ? D / 4 : 32;     // lanes of a row
+    constexpr int SPLIT = D == 64 ? 2 : 1;             // partials at a time
+    constexpr int N = D / LANES, BATCH = 8;            // channels of a lane, reads in flight
+    const bool blocks = P.idx != nullptr;
+    const int upb = (blocks ? P.T : 1) * P.H * P.mtiles, rows_all = blocks ? P.G : P.T * P.G;
+    const int lane = threadIdx.x & 31, groups = (min(MR, rows_all) + kMergeWarps - 1) / kMergeWarps;
+    const long long unit = blockIdx.x / groups;
+    const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, t0 = blocks ? u / P.mtiles / P.H : 0;
+    const int m0 = u % P.mtiles * MR, m = int(blockIdx.x % groups) * kMergeWarps + (threadIdx.x >> 5);
+    const AttendSeq seq = attend_seq(P, b, false);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials
+    const int2 who = __ldcg(P.shared + unit);
+    if (who.x < 0 || who.x >= who.y || who.y >= P.ctas || m >= min(MR, rows_all - m0)) return;
+    const int part = lane / LANES, d = lane % LANES * N;
+    float top = -INFINITY, total = 0.f, o[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = 0.f;
+    for (int first = who.x; first <= who.y; first += 32) {
+        auto at = [&](int c) { return P.partials + (2ll * c + (c == who.x ? 1 : 0)) * PSIZE; };
+        const int n = min(32, who.y - first + 1);
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml = __ldcg(reinterpret_cast<const float2*>(at(first + lane) + MR * D + 2 * m));
+        float r = ml.x;
+#pragma unroll
+        for (int s = 16; s; s >>= 1) r = fmaxf(r, __shfl_xor_sync(~0u, r, s));
+        r = fmaxf(r, top);
+        // a partial without rows weighs nothing; one whose sum is NaN has to stay
+        const float weight = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ex2(ml.x - r), back = top == -INFINITY ? 0.f : ex2(top - r);
+        float sum = weight == 0.f && ml.y == 0.f ? 0.f : ml.y * weight;
+#pragma unroll
+        for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(~0u, sum, s);
+        total = (top == -INFINITY ? 0.f : total * back) + sum;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = top == -INFINITY ? 0.f : o[i] * back;
+        top = r;
+        const uint32_t there = __ballot_sync(~0u, !(ml.x == -INFINITY && ml.y == 0.f));
+        for (int c = 0; c < n; c += BATCH * SPLIT) {
+            float4 v[BATCH][N / 4];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int x = c + k * SPLIT + part;
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i)
+                    v[k][i] = x < n && part < SPLIT ? __ldcg(reinterpret_cast<const float4*>(at(first + x) + m * D + d) + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int x = c + k * SPLIT + part;
+                const float f = __shfl_sync(~0u, weight, x & 31);
+                if (x >= n || part >= SPLIT || !(there >> x & 1)) continue;
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) {
+                    o[4 * i] = fmaf(v[k][i].x, f, o[4 * i]);
+                    o[4 * i + 1] = fmaf(v[k][i].y, f, o[4 * i + 1]);
+                    o[4 * i + 2] = fmaf(v[k][i].z, f, o[4 * i + 2]);
+                    o[4 * i + 3] = fmaf(v[k][i].w, f, o[4 * i + 3]);
+                }
+            }
+        }
+    }
+    if constexpr (SPLIT == 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] += __shfl_xor_sync(~0u, o[i], 16);
+    }
+    if (part == 0) attend_write<D, DT>(P, b, h, t0, m0, seq.tokens, m, d, o, top, total);
 }
 
 }  // namespace lagkv

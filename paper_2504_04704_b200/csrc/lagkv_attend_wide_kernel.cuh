@@ -876,12 +876,12 @@ constexpr int kJoinRows = 32, kJoinThreads = 256;
 template <int D, int DT, int MT>
 __global__ void __launch_bounds__(kJoinThreads)
 lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
-    constexpr int CHUNKS = MT * kWideTile / kJoinRows, N = D / 8, PSIZE = WideGeo<D, DT, MT>::PSIZE;
-    const int upb = P.H * P.mtiles, chunk = blockIdx.x % CHUNKS;
-    const long long unit = blockIdx.x / CHUNKS;
+    constexpr int N = D / 8, PSIZE = WideGeo<D, DT, MT>::PSIZE;
+    const int upb = P.H * P.mtiles, chunks = (min(MT * kWideTile, P.T * P.G) + kJoinRows - 1) / kJoinRows, chunk = blockIdx.x % chunks;
+    const long long unit = blockIdx.x / chunks;
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials
-    const int2 who = P.shared[unit];
-    if (who.x == who.y) return;
+    const int2 who = __ldcg(P.shared + unit);
+    if (who.x < 0 || who.x >= who.y || who.y >= P.ctas) return;  // not shared (or, after a wait that gave up, not said)
     const int b = int(unit / upb), u = int(unit % upb), h = u / P.mtiles % P.H, m0 = u % P.mtiles * (MT * kWideTile);
     const int mu = chunk * kJoinRows + (threadIdx.x & 31), d0 = (threadIdx.x >> 5) * N;
     if (m0 + mu >= P.T * P.G) return;
