@@ -344,9 +344,11 @@ typedef struct {
 /*
  * Bytes of workspace for lagkv_attend_tree() (blocks = keep = 0) or lagkv_attend_blocks() (blocks =
  * blocks per sequence of its bounds, keep as in its choice) with up to T tokens and H_q heads; 0 = bad
- * arguments.  A workspace may serve every smaller call, tree and blocks alike.  256-byte aligned,
- * cleared once with lagkv_attend_workspace_init() (async on the stream; the kernels leave what they
- * need cleared); starts with a status block that lagkv_read_status() reads.
+ * arguments.  A workspace may serve every smaller call, tree and blocks alike, one at a time: calls (or
+ * replayed graphs) that may overlap need workspaces of their own.  256-byte aligned; starts with a
+ * status block, cleared once with lagkv_attend_workspace_init() (async on the stream), that
+ * lagkv_read_status() reads.  LAGKV_ETIMEOUT there: a wait inside a kernel was given up, the results of
+ * that call are not valid.
  */
 size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, int64_t blocks, int32_t keep);
 int lagkv_attend_workspace_init(lagkv_plan_t plan, void *workspace, size_t workspace_bytes, void *cuda_stream);
@@ -365,7 +367,8 @@ int lagkv_attend_workspace_init(lagkv_plan_t plan, void *workspace, size_t works
  * seq_len[b] = 0 is an empty slot of the batch (no tokens when draft_len is NULL).
  * seq_len[b] outside [0, S_cap], draft_len[b] outside [0, T] or above seq_len[b]: that sequence counts as
  * without tokens and LAGKV_EINVAL is recorded in the status block.
- * One launch with the same arguments for every length; results do not depend on the schedule.
+ * Two launches, the same with the same arguments for every length, so the call may be captured into a CUDA
+ * graph.  The same call gives the same bits.
  */
 int lagkv_attend_tree(lagkv_plan_t plan, const lagkv_query *query, const void *Q, const void *K, const void *V,
                       int64_t S_cap, const int32_t *seq_len, const int32_t *draft_len, const uint64_t *tree_mask,
@@ -431,7 +434,7 @@ typedef struct {
  *   idx_out  int32 [B, T, H_kv, keep] or NULL: the chosen blocks, ascending, -1 behind the last.
  * seq_len[b] outside [0, S_cap], or in 1..T-1: LAGKV_EINVAL is recorded; such a sequence and an empty one
  * (seq_len[b] = 0) get out = 0, lse = -infinity, idx = -1.
- * out, lse_out and the rest as for lagkv_attend_tree().  Three launches.
+ * out, lse_out and the rest as for lagkv_attend_tree().  Four launches.
  */
 int lagkv_attend_blocks(lagkv_plan_t plan, const lagkv_query *query, const lagkv_block_choice *choice, const void *Q,
                         const void *K, const void *V, int64_t S_cap, const int32_t *seq_len, const void *bounds,
@@ -450,7 +453,7 @@ int lagkv_attend_blocks_paged(lagkv_plan_t plan, const lagkv_query *query, const
  * handed out lowest first, so the result depends on the state alone.  Tables of several layers (folded
  * into B) may share one pool and one refs.  num_pages < 2^30.
  * Workspace: at least lagkv_pages_workspace_bytes() (0 = bad arguments), 256-byte aligned, cleared once
- * with lagkv_pages_workspace_init(); lagkv_read_status() reads its status block.
+ * with lagkv_pages_workspace_init(), for one call at a time; lagkv_read_status() reads its status block.
  */
 size_t lagkv_pages_workspace_bytes(lagkv_plan_t plan, int64_t num_pages);
 int lagkv_pages_workspace_init(lagkv_plan_t plan, void *workspace, size_t workspace_bytes, void *cuda_stream);

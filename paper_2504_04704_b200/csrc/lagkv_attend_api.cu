@@ -19,7 +19,13 @@ const AttendEntry* find_attend(int D, int dtype, int rows_wanted, bool blocks, i
     const int n = dtype == LAGKV_DTYPE_BF16   ? attend_bf16_kernels(&t)
                   : dtype == LAGKV_DTYPE_FP16 ? attend_fp16_kernels(&t)
                                               : attend_fp8_kernels(&t);
-    // the smallest unit that holds all query rows, else the largest there is
+    // The smallest unit that holds all query rows, else the largest there is: rows of K and V are then read once.
+    // In us, at 8 KV heads of 128 channels, for the units of 16, 32, 128 and 256 rows:
+    //                            bf16: 1 x 1024 rows   16 x 8192 rows        fp8: 1 x 1024 rows   16 x 8192 rows
+    //     16 query rows           12   14   17   18    101  108   96  145         13   16   21   22     67   92  141  187
+    //     32                      13   16   17   18    180  111   97  147         13   17   22   23    118   97  141  187
+    //     64                      16   18   18   19    355  204  100  153         15   18   22   23    222  177  143  188
+    //    128                      19   19   19   20    676  425  109  167         18   19   25   25    428  334  151  194
     const AttendEntry* best = nullptr;
     for (int i = 0; i < n; ++i) {
         if (t[i].D != D || (blocks && t[i].wide)) continue;
@@ -155,6 +161,7 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     P->shared = reinterpret_cast<int2*>(base + kHead + pb);
     P->mtiles = (query_rows + e->rows - 1) / e->rows;
     P->ctas = plan->sm_count * e->ctas_per_sm;
+    P->least = e->wide ? 1 : kAttendLeast;
     P->lead = e->wide ? kWideLead : kAttendLead;
     *entry = e;
     *rest = base + kHead + pb + sb;

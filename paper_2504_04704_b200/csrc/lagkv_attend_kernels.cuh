@@ -11,9 +11,9 @@
 //
 // Work is cut on the device, from seq_len: (sequence, KV head, group of M rows) units of 64-row
 // tiles, dealt to the CTAs in equal contiguous shares, so ragged batches and a single long sequence
-// fill the GPU alike and one launch with the same arguments serves every length (CUDA graphs).  A unit
-// that several CTAs share goes through fp32 partials in the workspace; the last CTA to arrive adds
-// them in the order of the rows, so the result does not depend on who was last.
+// fill the GPU alike and the same launches with the same arguments serve every length (CUDA graphs).  A unit
+// that several CTAs share goes through fp32 partials in the workspace; a kernel launched behind adds
+// them in the order of the rows.
 #pragma once
 #include "lagkv_kernels.cuh"
 
@@ -30,7 +30,7 @@ struct AttendParams {
     const unsigned long long* mask;   // [B, T] visible drafted rows; nullptr: a chain (token t sees rows <= t)
     int32_t* status;
     float* partials;       // [grid * 2][MR * (D + 2)]
-    int2* shared;          // wide kernel: first and last CTA of each unit
+    int2* shared;          // first and last CTA of each unit
     long long sb, sh, ss, page_stride;  // bytes
     const int32_t* block_table;
     long long num_pages;
@@ -38,6 +38,7 @@ struct AttendParams {
     int B, H, G, T, S_cap, max_blocks, page_shift;
     int mtiles;            // groups of M rows per (sequence, KV head)
     int ctas;              // CTAs of the attention kernel
+    int least;             // tiles that a CTA takes at least
     int lead;              // what beginning a unit costs, in tiles: counted when the work is shared out
     float scale_log2, v_scale;
     const int32_t* idx;    // blocks: [B, T, H, keep] ascending block numbers, -1 behind the last
@@ -45,7 +46,8 @@ struct AttendParams {
 };
 
 constexpr int kAttendTile = 64;     // rows of the unit of scheduling (lagkv_attend_kernel)
-constexpr int kAttendLead = 8;      // P.lead: 16 caches of 16384 rows in 80 us, 85 with equal shares of the rows
+constexpr int kAttendLead = 6;      // P.lead: 16 caches of 16384 rows in 79 us, 85 with equal shares of the rows
+constexpr int kAttendLeast = 2;     // P.least: one cache of 1024 rows in 10.8 us, 12.2 with one tile per CTA
 constexpr int kAttendWarps = 4;
 constexpr int kWarpRows = 16;       // rows of a warp's tile: never across a page or a block (both >= 16)
 
@@ -248,7 +250,7 @@ __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int u
         total += all;
     }
     AttendShare s;
-    s.per_cta = div_small(total + gridDim.x - 1, gridDim.x);
+    s.per_cta = max((long long)P.least, div_small(total + gridDim.x - 1, gridDim.x));
     s.pos = s.per_cta * blockIdx.x;
     s.end = s.pos + s.per_cta < total ? s.pos + s.per_cta : total;
     s.b = 0;

@@ -12,8 +12,7 @@
 // cost three warps 10000 cycles a step, five times what the products take); the others help: they load the
 // next unit's queries, mend V tiles -- rows behind the last one and hidden rows that are not finite become
 // zeros, so that 0 * inf never happens -- and widen fp8 tiles, which land as they are, to fp16.
-// Partials of shared units (66 KB for 128 query rows) are joined by a kernel of their own: one CTA adding
-// up 18 of them took longer than the attention.
+// Partials of shared units are 66 KB for 128 query rows.
 // Bound: at 128 rows and 16-bit caches by HBM, at 256 by the 16384 exponentials per tile and stream (16 a
 // cycle and SM: as long as the products themselves).
 #pragma once
