@@ -36,13 +36,15 @@ struct WideGeo {
     static constexpr int SLOT = PANELS * PANEL;
     static constexpr int EXCH = 64 * kWideTile * 4;    // MT = 1: 32 channels of each stream's O for the other
     static constexpr int QBYTES = MT == 2 ? 2 * SLOT : SLOT + EXCH;
-    static constexpr int WARPS = DT_ == 2 ? 16 : 12;   // widening takes seven warps to keep up
+    static constexpr int WARPS = DT_ == 2 ? 16 : 12;   // more would leave the softmax too few registers
     static constexpr int NT = WARPS * 32;
-    // Warps 10 ..: load queries; mend V tiles (16-bit), or widen in two groups, one for K and one for V tiles
-    static constexpr int HELP_WARPS = WARPS - 10, GROUPS = DT_ == 2 ? 2 : 1, HELP = HELP_WARPS / GROUPS * 32;
+    // Warps 10 ..: load queries; mend V tiles (16-bit), or widen tiles in groups, each every GROUPS-th tile
+    static constexpr int HELP_WARPS = WARPS - 10, GROUPS = DT_ == 2 ? 3 : 1, HELP = HELP_WARPS / GROUPS * 32;
+    // fp8: rows of a pass of a group, and the threads it takes; eight rows on the swizzle is the same again
+    static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
-    static constexpr int RS = DT_ == 2 ? 4 : 0;                  // ... and how many are in flight
+    static constexpr int RS = DT_ == 2 ? (MT_ == 1 ? 3 : 4) : 0;  // ... and how many are in flight (MT = 1: 3 leave room for a 4th slot)
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
     static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
     static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
@@ -393,7 +395,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 break;
             }
             if (lane == 0) {
-                if (!is_v) gone[at.c % kWideRowFlags] = flags;
+                gone[at.c % kWideRowFlags] = flags;
                 mbar_arrive_expect_tx(bar, boxes * box_bytes);
             }
             __syncwarp();
@@ -406,7 +408,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         }
     } else if (w > 9) {
         // ------------------------------------------------------------------ help
-        const int group = (w - 10) / (G::HELP / 32), ptid = tid - 10 * 32 - group * G::HELP;  // group 0 the V tiles, 1 the K tiles
+        const int group = (w - 10) / (G::HELP / 32), ptid = tid - 10 * 32 - group * G::HELP;
         // after a wait that ran out the walk goes on to its end without waiting, so that the barrier among these
         // warps still matches
         auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -469,45 +471,56 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 if (lane == 0 && ok) mbar_arrive(b_q);
             }
             const int place = DT == 2 ? int(at.c % (G::RS ? G::RS : 1)) : int(at.c % G::NS);
-            if (at.is_v() != (group == 0)) {
+            if (DT == 2 ? int(at.c % G::GROUPS) != group : !at.is_v()) {
                 if (DT == 2) landed ^= 1u << place;  // the other group's
                 continue;
             }
             const int slot = int(at.c % G::NS);
-            const uint32_t groups = at.is_v() ? missing_groups(at) : 0u;
-            const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
-            if (DT != 2 && !mend) continue;
+            uint32_t groups = 0;
+            if (DT != 2) {
+                groups = missing_groups(at);
+                if (!at.mend(groups)) continue;
+            }
             wait(b_land + 8 * place, landed >> place & 1);
             landed ^= 1u << place;
+            if (DT == 2 && at.is_v()) groups = gone[at.c % kWideRowFlags];
+            const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
             unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
-            if constexpr (DT != 2) {
-                auto piece = [&](int id) {
-                    const int r = id / G::CPR, ch = id % G::CPR;
-                    return reinterpret_cast<uint4*>(tile + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
-                };
-                if (careful) note_odd(at, slot, [&](int id) { return *piece(id); });
-                for (int id = first_zero(at, slot, groups, careful) * G::CPR + ptid; id < G::CHUNKS; id += G::HELP)
-                    if (zero_row(at, slot, id / G::CPR, groups, careful)) *piece(id) = make_uint4(0u, 0u, 0u, 0u);
-            } else {
+            auto piece = [&](int id) {
+                constexpr int CPR16 = D / 8;
+                const int r = id / CPR16, ch = id % CPR16;
+                return reinterpret_cast<uint4*>(tile + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
+            };
+            if constexpr (DT == 2) {
                 if (at.c >= uint32_t(G::NS)) wait(b_empty + 8 * slot, (at.c / G::NS + 1) & 1);
                 const unsigned char* from = smem + (s_raw - sbase) + place * G::RAW;
                 if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
+                // A row's 16-byte pieces become two each.  Eight lanes store to one panel's halves of two rows: the
+                // swizzle gives them all the banks.
+                const int r = D == 128 ? (ptid >> 4) * 2 + (ptid >> 2 & 1) : ptid / G::CPR, ch = D == 128 ? (ptid >> 1 & 4) + (ptid & 3) : ptid % G::CPR;
+                if (ptid < G::PASS_THREADS) {
+                    from += r * G::ROWB + ch * 16;
+                    unsigned char* to = tile + (ch >> 2) * G::PANEL + r * 128;
+                    const int c0 = ((ch & 3) * 2 ^ (r & 7)) << 4, c1 = c0 ^ 16;
 #pragma unroll 4
-                for (int id = ptid; id < G::CHUNKS; id += G::HELP) {
-                    const int r = id / G::CPR, ch = id % G::CPR;
-                    uint4 x = *reinterpret_cast<const uint4*>(from + id * 16);
-                    if (mend && zero_row(at, slot, r, groups, careful)) x = make_uint4(0u, 0u, 0u, 0u);
-                    uint32_t a[2], b[2], e[2], f[2];
-                    Elem<2>::expand(x.x, a);
-                    Elem<2>::expand(x.y, b);
-                    Elem<2>::expand(x.z, e);
-                    Elem<2>::expand(x.w, f);
-                    unsigned char* row = tile + (ch >> 2) * G::PANEL + r * 128;
-                    const int c0 = (ch & 3) * 2;
-                    *reinterpret_cast<uint4*>(row + ((c0 ^ (r & 7)) << 4)) = make_uint4(a[0], a[1], b[0], b[1]);
-                    *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], f[0], f[1]);
+                    for (int i = 0; i < kWideTile / G::PASS; ++i) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(from + i * G::PASS * G::ROWB);
+                        uint32_t a[2], b[2], e[2], f[2];
+                        Elem<2>::expand(x.x, a);
+                        Elem<2>::expand(x.y, b);
+                        Elem<2>::expand(x.z, e);
+                        Elem<2>::expand(x.w, f);
+                        *reinterpret_cast<uint4*>(to + c0 + i * G::PASS * 128) = make_uint4(a[0], a[1], b[0], b[1]);
+                        *reinterpret_cast<uint4*>(to + c1 + i * G::PASS * 128) = make_uint4(e[0], e[1], f[0], f[1]);
+                    }
                 }
+                if (mend) meet();
+            } else if (careful) {
+                note_odd(at, slot, [&](int id) { return *piece(id); });
             }
+            if (mend)
+                for (int id = first_zero(at, slot, groups, careful) * (D / 8) + ptid; id < kWideTile * (D / 8); id += G::HELP)
+                    if (zero_row(at, slot, id / (D / 8), groups, careful)) *piece(id) = make_uint4(0u, 0u, 0u, 0u);
             fence_proxy_async();
             meet();
             if (ptid == 0 && ok) {
