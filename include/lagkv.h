@@ -336,8 +336,8 @@ typedef struct {
     double scale;      /* factor of q.k before the softmax, > 0; 0 = 1/sqrt(D)                  */
     double k_scale;    /* what a stored K element of 1 stands for (fp8 caches), > 0; 0 = 1      */
     double v_scale;    /* the same for V                                                        */
-    int64_t stride_b;  /* strides of Q in elements, multiples of 8; all 0 = contiguous          */
-    int64_t stride_t;  /* [B, T, H_q, D]; channel stride 1, 16-byte aligned base                */
+    int64_t stride_b;  /* strides of Q [B, T, H_q, D] in elements, multiples of 8; 0 = dense    */
+    int64_t stride_t;  /* over the dimension inside; channel stride 1, 16-byte aligned base     */
     int64_t stride_h;
 } lagkv_query;
 
@@ -483,7 +483,8 @@ int lagkv_pages_reserve(lagkv_plan_t plan, int32_t *block_table, int32_t max_blo
  * src[i] (DEVICE int32 [n] each), seq_len and static_len (DEVICE int32 [B]) included.  Pages wholly below
  * min(seq_len, static_len) are shared: those rows are never rewritten, not by the compress pass, not by
  * new rows, not by lagkv_tree_commit().  The others are copied to free pages, whole, in the order (i, block), so
- * that both sequences may go on on their own.  (A cache that is never compressed: static_len = seq_len.)
+ * that both sequences may go on on their own.  (A cache that is never compressed:
+ * static_len = seq_len, drafted rows not counted.)
  * A pair is refused (LAGKV_EINVAL recorded, the others done) when an index is outside [0, B), dst[i] holds a
  * page or is the target of an earlier pair, or a page that src[i]'s length needs is not a counted page
  * of the pool.  Too few free pages: LAGKV_ECAPACITY is recorded and nothing changes.  Two launches.

@@ -446,6 +446,12 @@ class Plan:
                "lagkv_attend_workspace_init")
         return ws
 
+    def _ws(self, ws):
+        """Address and bytes of a workspace."""
+        if ws.get_device() != self.device or not ws.is_contiguous():
+            raise TypeError(f"workspace must be a contiguous CUDA tensor on device {self.device}")
+        return ws.data_ptr(), ws.numel() * ws.element_size()
+
     def _check_ints(self, t, name: str, shape, dtype=torch.int32):
         if t is not None and (t.dtype != dtype or t.get_device() != self.device or t.shape != shape or not t.is_contiguous()):
             raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor {tuple(shape)} on device {self.device}")
@@ -470,7 +476,11 @@ class Plan:
         want = torch.float16 if self.dtype == torch.float16 else torch.bfloat16
         if Q.dtype != want or Q.get_device() != self.device or len(shape) != 4 or shape[0] != c.B or shape[3] != c.D or Q.stride(3) != 1:
             raise TypeError(f"Q must be a {want} CUDA tensor [{c.B}, T, H_q, {c.D}] with channel stride 1")
-        strides = (0, 0, 0) if Q.is_contiguous() else Q.stride()[:3]
+        strides = (0, 0, 0)
+        if not Q.is_contiguous():
+            strides = Q.stride()[:3]
+            if any(n > 1 and st == 0 for n, st in zip(shape, strides)):  # 0 would stand for dense
+                raise TypeError("Q must not be broadcast over tokens, heads or sequences")
         return lagkv_query(shape[1], shape[2], 0.0 if scale is None else scale, k_scale, v_scale, *strides)
 
     def _attend_out(self, Q, out, want_lse):
@@ -498,6 +508,12 @@ class Plan:
             num_pages = K_pool.shape[0]
         elif num_pages is None:
             raise TypeError("num_pages is needed with strides")
+        else:
+            c, (sp, sh, ss, rows) = self.cfg, strides
+            last = (num_pages - 1) * sp + (c.H_kv - 1) * sh + (rows - 1) * ss + c.D
+            size = K_pool.element_size()
+            if min(sp, sh, ss) < 0 or last > K_pool.untyped_storage().nbytes() // size - K_pool.storage_offset():
+                raise TypeError(f"num_pages = {num_pages} and strides {tuple(strides)} reach behind the pool")
         return self._paged(K_pool, block_table, strides), int(num_pages)
 
     def attend_tree(self, Q, K, V, seq_len, workspace, draft_len=None, tree_mask=None, scale=None, k_scale=1.0,
@@ -517,7 +533,7 @@ class Plan:
         out, lse = self._attend_out(Q, out, want_lse)
         rc = self.lib.lagkv_attend_tree(
             self.handle, ctypes.byref(q), _addr(Q), _addr(K), _addr(V), int(K.shape[2]), _addr(seq_len), _addr(draft_len),
-            _addr(tree_mask), _addr(out), _addr(lse), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(tree_mask), _addr(out), _addr(lse), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_attend_tree")
         return {"out": out, "lse": lse} if want_lse else {"out": out}
 
@@ -534,7 +550,7 @@ class Plan:
         out, lse = self._attend_out(Q, out, want_lse)
         rc = self.lib.lagkv_attend_tree_paged(
             self.handle, ctypes.byref(q), _addr(Q), _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(seq_len),
-            _addr(draft_len), _addr(tree_mask), _addr(out), _addr(lse), _addr(workspace), workspace.numel(),
+            _addr(draft_len), _addr(tree_mask), _addr(out), _addr(lse), *self._ws(workspace),
             _raw_stream(self.device))
         _check(rc, "lagkv_attend_tree_paged")
         return {"out": out, "lse": lse} if want_lse else {"out": out}
@@ -559,7 +575,7 @@ class Plan:
             raise TypeError("K_cache and V_cache must have the same shape")
         rc = self.lib.lagkv_tree_commit(
             self.handle, _addr(K_cache), _addr(V_cache), int(K_cache.shape[2]), _addr(seq_len), _addr(draft_len), T,
-            _addr(accepted), _addr(n_accepted), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(accepted), _addr(n_accepted), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_tree_commit")
 
     def tree_commit_paged(self, K_pool, V_pool, block_table, seq_len, accepted, n_accepted, workspace, draft_len=None,
@@ -569,7 +585,7 @@ class Plan:
         lay, pages = self._paged_pool(K_pool, V_pool, block_table, strides, num_pages)
         rc = self.lib.lagkv_tree_commit_paged(
             self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(seq_len), _addr(draft_len), T,
-            _addr(accepted), _addr(n_accepted), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(accepted), _addr(n_accepted), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_tree_commit_paged")
 
     # ---- blocks
@@ -594,7 +610,7 @@ class Plan:
         self._check_ints(seq_len, "seq_len", (self.cfg.B,))
         self._check_ints(from_len, "from_len", (self.cfg.B,))
         rc = self.lib.lagkv_block_bounds(self.handle, _addr(K), int(K.shape[2]), _addr(from_len), _addr(seq_len), int(block_rows),
-                                         _addr(bounds), blocks, _addr(workspace), workspace.numel(), _raw_stream(self.device))
+                                         _addr(bounds), blocks, *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_block_bounds")
 
     def block_bounds_paged(self, K_pool, block_table, seq_len, bounds, workspace, block_rows=64, from_len=None, strides=None,
@@ -606,7 +622,7 @@ class Plan:
         self._check_ints(from_len, "from_len", (self.cfg.B,))
         rc = self.lib.lagkv_block_bounds_paged(
             self.handle, _addr(K_pool), ctypes.byref(lay), pages, _addr(from_len), _addr(seq_len), int(block_rows), _addr(bounds),
-            blocks, _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            blocks, *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_block_bounds_paged")
 
     def _blocks_out(self, Q, seq_len, bounds, block_rows, keep, sink_blocks, recent_blocks, out, want_lse, want_idx):
@@ -636,7 +652,7 @@ class Plan:
                                                  want_idx)
         rc = self.lib.lagkv_attend_blocks(
             self.handle, ctypes.byref(q), ctypes.byref(choice), _addr(Q), _addr(K), _addr(V), int(K.shape[2]), _addr(seq_len),
-            _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_attend_blocks")
         return got
 
@@ -650,7 +666,7 @@ class Plan:
                                                  want_idx)
         rc = self.lib.lagkv_attend_blocks_paged(
             self.handle, ctypes.byref(q), ctypes.byref(choice), _addr(Q), _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages,
-            _addr(seq_len), _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), _addr(workspace), workspace.numel(),
+            _addr(seq_len), _addr(bounds), _addr(got["out"]), _addr(lse), _addr(idx), *self._ws(workspace),
             _raw_stream(self.device))
         _check(rc, "lagkv_attend_blocks_paged")
         return got
@@ -680,7 +696,7 @@ class Plan:
         self._check_ints(keep_len, "keep_len", (self.cfg.B,))
         rc = self.lib.lagkv_pages_release(
             self.handle, _addr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _addr(refs),
-            _addr(keep_len), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(keep_len), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_pages_release")
 
     def pages_reserve(self, block_table, refs, want_len, workspace, page_size) -> None:
@@ -689,7 +705,7 @@ class Plan:
         self._check_ints(want_len, "want_len", (self.cfg.B,))
         rc = self.lib.lagkv_pages_reserve(
             self.handle, _addr(block_table), int(block_table.shape[1]), int(page_size), int(refs.shape[0]), _addr(refs),
-            _addr(want_len), _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(want_len), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_pages_reserve")
 
     def pages_fork(self, K_pool, V_pool, block_table, refs, seq_len, static_len, src, dst, workspace, strides=None) -> None:
@@ -704,7 +720,7 @@ class Plan:
         self._check_ints(dst, "dst", (n,))
         rc = self.lib.lagkv_pages_fork(
             self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(refs), _addr(seq_len), _addr(static_len),
-            _addr(src), _addr(dst), n, _addr(workspace), workspace.numel(), _raw_stream(self.device))
+            _addr(src), _addr(dst), n, *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_pages_fork")
 
     def pages_compact(self, K_pool, V_pool, block_table, refs, workspace, strides=None, live_out=None) -> torch.Tensor:
@@ -714,8 +730,7 @@ class Plan:
         live = torch.empty(1, dtype=torch.int32, device=refs.device) if live_out is None else live_out
         self._check_ints(live, "live_out", (1,))
         rc = self.lib.lagkv_pages_compact(
-            self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(refs), _addr(live), _addr(workspace),
-            workspace.numel(), _raw_stream(self.device))
+            self.handle, _addr(K_pool), _addr(V_pool), ctypes.byref(lay), pages, _addr(refs), _addr(live), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_pages_compact")
         return live
 
