@@ -460,29 +460,37 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             const bool odd = careful && (odd_rows[slot * 4] | odd_rows[slot * 4 + 1] | odd_rows[slot * 4 + 2] | odd_rows[slot * 4 + 3]);
             return max(0, (odd ? min(x.U.base, x.U.lim) : x.U.lim) - x.row0());
         };
-        uint32_t landed = 0, units = 0;  // parities of the places where tiles land; units behind
+        uint32_t landed = 0, units = 0;  // parities of the places where tiles to mend land (16-bit); units behind
+        // the load's turn among the groups, slot and place, and how often slots and places have been through
+        int turn = 0, slot = 0, place = 0;
+        uint32_t slot_lap = 0, place_lap = 0;
         WideCursor<G> at;
         at.start(sh, U, any);
-        for (; at.more; at.next(P, upb)) {
+        auto go_on = [&]() {
+            if (G::GROUPS > 1 && ++turn == G::GROUPS) turn = 0;
+            if (++slot == G::NS) slot = 0, ++slot_lap;
+            if (DT == 2 && ++place == G::RS) place = 0, ++place_lap;
+            at.next(P, upb);
+        };
+        for (; at.more; go_on()) {
             if (at.l == 0 && at.c > 0) {  // the next unit's queries, once the products with those before are done
                 wait(b_q_free, units++ & 1);
                 load_queries<G>(P, at.U, at.sh.b, smem, w - 10, G::HELP_WARPS);
                 __syncwarp();
                 if (lane == 0 && ok) mbar_arrive(b_q);
             }
-            const int place = DT == 2 ? int(at.c % (G::RS ? G::RS : 1)) : int(at.c % G::NS);
-            if (DT == 2 ? int(at.c % G::GROUPS) != group : !at.is_v()) {
-                if (DT == 2) landed ^= 1u << place;  // the other group's
-                continue;
-            }
-            const int slot = int(at.c % G::NS);
+            if (DT == 2 ? turn != group : !at.is_v()) continue;
             uint32_t groups = 0;
             if (DT != 2) {
                 groups = missing_groups(at);
                 if (!at.mend(groups)) continue;
             }
-            wait(b_land + 8 * place, landed >> place & 1);
-            landed ^= 1u << place;
+            if (DT == 2) {
+                wait(b_land + 8 * place, place_lap & 1);
+            } else {
+                wait(b_land + 8 * slot, landed >> slot & 1);
+                landed ^= 1u << slot;
+            }
             if (DT == 2 && at.is_v()) groups = gone[at.c % kWideRowFlags];
             const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
             unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
@@ -492,7 +500,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 return reinterpret_cast<uint4*>(tile + (ch >> 3) * G::PANEL + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
             };
             if constexpr (DT == 2) {
-                if (at.c >= uint32_t(G::NS)) wait(b_empty + 8 * slot, (at.c / G::NS + 1) & 1);
+                if (slot_lap > 0) wait(b_empty + 8 * slot, (slot_lap + 1) & 1);
                 const unsigned char* from = smem + (s_raw - sbase) + place * G::RAW;
                 if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
                 // A row's 16-byte pieces become two each.  Eight lanes store to one panel's halves of two rows: the
