@@ -471,7 +471,7 @@ lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ boun
             }
             __syncthreads();
             // The chosen ones become certain, the others impossible.  Few are ranked one against another (for the
-            // usual handful TIMEX us less than the histograms), many by the histograms.
+            // usual handful 1.4 us less than the histograms), many by the histograms.
             if (few) {
                 if (tid < total_near) {
                     const unsigned long long k = mine[tid];
