@@ -189,6 +189,21 @@ def test_scores_next_to_the_border(binding):
     check(c, 16, 9)
 
 
+@pytest.mark.parametrize("keep", [3, 700, 1990])
+def test_thousands_of_scores_next_to_the_border(binding, keep):
+    """More blocks that 32-bit sums cannot tell apart than are ranked one against another, ties among them."""
+    n = 2000
+    c = case(binding, 1, 1, 2, 64, 16 * n, 1, BF16, 16, seed=6, lens=[16 * n], keep=keep)
+    c["Q"].fill_(1.0)
+    c["K"].fill_(1.0)
+    c["K"][..., 0], c["K"][..., 1] = 4096.0, -4096.0
+    v = (torch.arange(n, device=DEV) * 7) % 1500                  # 64 + v * 2^-20 after cancellation, 500 values twice
+    c["K"][0, 0, :, 2] = ((v % 200) * 2.0 ** -20).to(BF16).repeat_interleave(16)
+    c["K"][0, 0, :, 3] = ((v // 200) * 200 * 2.0 ** -20).to(BF16).repeat_interleave(16)
+    c["plan"].block_bounds(c["K"], c["seq"], c["bounds"], c["ws"], block_rows=16)
+    check(c, 16, keep)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP8], ids=["bf16", "fp8"])
 @pytest.mark.parametrize("page,rows", [(16, 64), (64, 16), (32, 32)])
 def test_paged_equals_contiguous(binding, dtype, page, rows):

@@ -121,3 +121,16 @@ def test_queries_as_views(binding):
     with pytest.raises(TypeError):
         c["plan"].attend_tree_paged(c["Q"], pool, pool.clone(), table, c["seq"], c["ws"], strides=(2 * 16 * 128, 16 * 128, 128, 16), num_pages=5)
     assert c["plan"].read_status(c["ws"])[0] == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP8], ids=["bf16", "fp16", "fp8"])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_the_most_query_rows(binding, dtype, D):
+    """64 tokens of 64 query heads per KV head, over a cache that is hardly longer; the blocks of 2 tokens of them."""
+    c = make(binding, 2, 1, 64, D, 190, 64, dtype, 7)
+    U.assert_attention(tree(c), U.tree_reference(c["Q"], c["K"], c["V"], c["seq"], torch.full_like(c["seq"], 64), None, None, c["ks"], c["vs"]))
+    c = make(binding, 2, 1, 64, D, 190, 2, dtype, 8)                # all blocks kept: dense attention
+    want = U.tree_reference(c["Q"], c["K"], c["V"], c["seq"], torch.full_like(c["seq"], 2), None, None, c["ks"], c["vs"])
+    U.assert_attention(tree(c), want)
+    U.assert_attention(blocks(c), want)
+    assert c["plan"].read_status(c["ws"])[0] == 0
