@@ -317,6 +317,12 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 416);       // [kWideRowFlags]
     long long* scan = reinterpret_cast<long long*>(misc + 544);                       // [16 + 2]
     uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 704);
+    // Pages of 16 or 32 rows are 16 or 8 boxes a tile, more than one warp issues in a step: one of the two
+    // helping warps fetches the V tiles (16 x 8 x 8192 rows of 128 bf16 channels under 16 tokens of 4 heads, pages of
+    // 16 / 32 / 64 rows: 104 / 102 / 105 us, without 135 / 107 / 103; fp8 tiles are half the boxes, and their helpers have
+    // no time to give).
+    const bool two = DT != 2 && P.block_table != nullptr && P.page_shift < 6;
+    const int helpers = G::HELP_WARPS - two, help = DT == 2 ? G::HELP : helpers * 32;
 
     if (tid == 0) {
         for (int i = 0; i < G::NS; ++i) {
@@ -331,7 +337,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         }
         for (int i = 0; i < (DT == 2 ? G::RS : G::NS); ++i) mbar_init(b_land + 8 * i, 1);
         for (int i = 0; i < G::RS; ++i) mbar_init(b_raw_free + 8 * i, 1);
-        mbar_init(b_q, G::HELP_WARPS);
+        mbar_init(b_q, helpers);
         mbar_init(b_q_free, 1);
         fence_mbar_init();
     }
@@ -352,7 +358,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     constexpr int kO = 256;
     bool ok = true;
 
-    if (w == 9) {
+    if (w == 9 || (two && w == 11)) {
         // ------------------------------------------------------------------ K and V tiles
         // The tile as boxes of the tensor map, a lane each: 64 channels (fp8: whole rows) of the rows of a
         // page.  Boxes behind the last row and pages outside the pool are left out.
@@ -363,6 +369,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         WideCursor<G> at;
         at.start(sh, U, any);
         for (; at.more; at.next(P, upb)) {
+            if (two && at.is_v() != (w == 11)) continue;
             const int row = at.row0() + box * box_rows;
             bool there = box < kWideTile / box_rows && row < at.U.lim;
             const bool wanted = there;
@@ -420,7 +427,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 ok = false;
             }
         };
-        auto meet = [&]() { named_bar_sync(2 + group, G::HELP); };
+        auto meet = [&]() { named_bar_sync(2 + group, help); };
         auto not_finite = [](const uint4& v) {
             const uint32_t x[4] = {v.x, v.y, v.z, v.w};
             bool odd = false;
@@ -439,7 +446,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             meet();
             const int first = max(0, x.U.base - x.row0()) * G::CPR, last = min(kWideTile, x.U.lim - x.row0()) * G::CPR;
 #pragma unroll 4
-            for (int id = first + ptid; id < last; id += G::HELP)
+            for (int id = first + ptid; id < last; id += help)
                 if (not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
             meet();
         };
@@ -478,7 +485,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         for (; at.more; go_on()) {
             if (at.l == 0 && at.c > 0) {  // the next unit's queries, once the products with those before are done
                 wait(b_q_free, units++ & 1);
-                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, G::HELP_WARPS);
+                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, helpers);
                 __syncwarp();
                 if (lane == 0 && ok) mbar_arrive(b_q);
             }
@@ -530,7 +537,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 note_odd(at, slot, [&](int id) { return *piece(id); });
             }
             if (mend)
-                for (int id = first_zero(at, slot, groups, careful) * (D / 8) + ptid; id < kWideTile * (D / 8); id += G::HELP)
+                for (int id = first_zero(at, slot, groups, careful) * (D / 8) + ptid; id < kWideTile * (D / 8); id += help)
                     if (zero_row(at, slot, id / (D / 8), groups, careful)) *piece(id) = make_uint4(0u, 0u, 0u, 0u);
             fence_proxy_async();
             meet();
