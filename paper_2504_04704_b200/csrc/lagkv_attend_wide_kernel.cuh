@@ -47,7 +47,7 @@ struct WideGeo {
     static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
-    static constexpr int RS = DT_ == 2 ? (MT_ == 1 ? 3 : 4) : 0;  // ... and how many are in flight (MT = 1: 3 leave room for a 4th slot)
+    static constexpr int RS = DT_ == 2 ? (MT_ == 1 && D_ > 64 ? 3 : 4) : 0;  // ... and how many are in flight (3 leave room for a 4th slot)
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
     static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
     static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
