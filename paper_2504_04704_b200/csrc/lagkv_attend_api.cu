@@ -142,12 +142,21 @@ int workspace_ok(const void* workspace, size_t bytes, size_t need) {
     return (reinterpret_cast<uintptr_t>(workspace) & 255u) ? LAGKV_EINVAL : LAGKV_OK;
 }
 
+// 17 to 32 query rows of large 16-bit caches go to the wide kernel as well: 20 and 32 query rows over 16 x 8 x 8192 rows
+// of 128 channels 98 and 98 us against 107 and 111, over 4 x 8 x 8192 41 and 40 against 41 and 42, over 1 x 8 x 8192 26
+// against 25; 20 and 32 over 16 x 8 x 8192 rows of 96 channels 86 and 87 against 91 and 94, 20 over 64 channels in pages
+// 68 against 74.
+int rows_of_unit(const lagkv_config& c, int query_rows, bool blocks, long long S_cap) {
+    const bool large = (long long)c.B * c.H_kv * S_cap >= 1 << 19;
+    return query_rows > 16 && query_rows <= 32 && large && !blocks && c.dtype != LAGKV_DTYPE_FP8_E4M3 ? 33 : query_rows;
+}
+
 // Picks the kernel, finds room in the workspace and launches.  `extra`: bytes of the workspace behind
 // the partials that the call uses itself.
 int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, size_t extra, void* workspace, size_t bytes,
                    AttendParams* P, const AttendEntry** entry, unsigned char** rest) {
     int index = 0;
-    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, query_rows, blocks, &index);
+    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows_of_unit(plan->cfg, query_rows, blocks, P->S_cap), blocks, &index);
     if (e == nullptr) return LAGKV_EUNSUPPORTED;
     const long long units = attend_units(plan, *e, query_rows, tokens);
     int rc = workspace_ok(workspace, bytes, kHead + 4096);
@@ -392,7 +401,7 @@ size_t lagkv_attend_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q, i
     // every smaller call of either kind: one token per unit with few query rows, all rows in one unit
     size_t partials = 0, units = 0;
     for (int rows : {1, 17, 33, 129, T * G}) {
-        if (rows > T * G) continue;
+        if (rows > T * G && !(rows == 33 && T * G > 16)) continue;  // 33: see rows_of_unit
         for (bool chosen : {false, true}) {
             int index;
             const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows, chosen, &index);

@@ -317,11 +317,11 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 416);       // [kWideRowFlags]
     long long* scan = reinterpret_cast<long long*>(misc + 544);                       // [16 + 2]
     uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 704);
-    // Pages of 16 or 32 rows are 16 or 8 boxes a tile, more than one warp issues in a step: one of the two
-    // helping warps fetches the V tiles (16 x 8 x 8192 rows of 128 bf16 channels under 16 tokens of 4 heads, pages of
-    // 16 / 32 / 64 rows: 104 / 102 / 105 us, without 135 / 107 / 103; fp8 tiles are half the boxes, and their helpers have
-    // no time to give).
-    const bool two = DT != 2 && P.block_table != nullptr && P.page_shift < 6;
+    // One warp does not get the boxes of a paged cache's tiles out in time: one of the two helping warps fetches the V
+    // tiles (16 x 8 x 8192 bf16 rows under 16 tokens of 4 heads, pages of 16 / 32 / 64 rows: 104 / 102 / 102 us at 128
+    // channels, 135 / 107 / 105 without; 64 channels 75 / 70 / 69, without 96 / 89 / 86).  fp8 tiles are half the boxes,
+    // and their helpers have no time to give.
+    const bool two = DT != 2 && P.block_table != nullptr;
     const int helpers = G::HELP_WARPS - two, help = DT == 2 ? G::HELP : helpers * 32;
 
     if (tid == 0) {

@@ -134,3 +134,20 @@ def test_the_most_query_rows(binding, dtype, D):
     U.assert_attention(tree(c), want)
     U.assert_attention(blocks(c), want)
     assert c["plan"].read_status(c["ws"])[0] == 0
+
+
+@pytest.mark.parametrize("dtype,D,T,G", [(BF16, 64, 5, 4), (FP16, 96, 4, 8), (BF16, 128, 17, 1), (FP8, 64, 8, 4)], ids=str)
+def test_large_capacities(binding, dtype, D, T, G):
+    """Half a million rows of capacity, most of them unused or all of them used, under 17 to 32 query rows."""
+    c = make(binding, 2, 1, G, D, 1 << 18, T, dtype, 9)
+    for lens in ([1 << 18, 37], [3000, T], [0, 100000]):
+        c["seq"].copy_(torch.tensor(lens, dtype=torch.int32))
+        draft = torch.tensor([min(T, n) for n in lens], dtype=torch.int32, device=DEV)
+        want = U.tree_reference(c["Q"], c["K"], c["V"], c["seq"], draft, None, None, c["ks"], c["vs"])
+        U.assert_attention(tree(c), want)
+        page = 64
+        table = torch.randperm(2 << 12, generator=torch.Generator().manual_seed(3)).view(2, -1).to(torch.int32).to(DEV)
+        pools = [U.to_pages(x, page, table, 2 << 12, 0.0) for x in (c["K"], c["V"])]
+        got = c["plan"].attend_tree_paged(c["Q"], *pools, table, c["seq"], c["ws"], k_scale=c["ks"], v_scale=c["vs"], want_lse=True)
+        U.assert_attention(got, want)
+    assert c["plan"].read_status(c["ws"])[0] == 0
