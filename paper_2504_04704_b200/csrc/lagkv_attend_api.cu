@@ -20,12 +20,13 @@ const AttendEntry* find_attend(int D, int dtype, int rows_wanted, bool blocks, i
                   : dtype == LAGKV_DTYPE_FP16 ? attend_fp16_kernels(&t)
                                               : attend_fp8_kernels(&t);
     // The smallest unit that holds all query rows, else the largest there is: rows of K and V are then read once.
-    // In us, at 8 KV heads of 128 channels, for the units of 16, 32, 128 and 256 rows:
-    //                            bf16: 1 x 1024 rows   16 x 8192 rows        fp8: 1 x 1024 rows   16 x 8192 rows
-    //     16 query rows           12   14   17   18    101  108   96  145         13   16   21   22     67   92  141  187
-    //     32                      13   16   17   18    180  111   97  147         13   17   22   23    118   97  141  187
-    //     64                      16   18   18   19    355  204  100  153         15   18   22   23    222  177  143  188
-    //    128                      19   19   19   20    676  425  109  167         18   19   25   25    428  334  151  194
+    // In us, at 8 KV heads of 128 channels and 8192 rows of 16 sequences, for the units of 16, 32, 128 and 256 rows:
+    //                           bf16                    fp8
+    //     16 query rows        101  107   97  146        71   99  136  179
+    //     32                   178  111   98  146       122  102  131  176
+    //     64                   353  203  101  155       225  181  130  175
+    //    128                   672  429  112  171       429  341  136  181
+    // rows_of_unit() below asks for other units where the cache is small or large.
     const AttendEntry* best = nullptr;
     for (int i = 0; i < n; ++i) {
         if (t[i].D != D || (blocks && t[i].wide)) continue;
@@ -142,13 +143,22 @@ int workspace_ok(const void* workspace, size_t bytes, size_t need) {
     return (reinterpret_cast<uintptr_t>(workspace) & 255u) ? LAGKV_EINVAL : LAGKV_OK;
 }
 
-// 17 to 32 query rows of large 16-bit caches go to the wide kernel as well: 20 and 32 query rows over 16 x 8 x 8192 rows
+// The query rows that find_attend() is asked for.
+// Small caches: units of 16 rows start faster and more CTAs take part; reading K and V for each of them costs little out of
+// L2.  They win up to about 4 tiles per CTA (16-bit) or 12 (fp8, where wide tiles have to be widened).  8 KV heads of 128
+// channels, units of 16 rows against the ones that hold all: bf16, 64 query rows, 256 / 1024 / 4096 rows 12.5 / 16 / 23
+// against 15 / 17.5 / 22 us, 256 query rows 16 / 24 against 17.5 / 19; fp8, 64 query rows 12 / 14 / 20.5 against 18.5 / 21 / 26.
+// Large 16-bit caches: 17 to 32 query rows go to the wide kernel as well: 20 and 32 query rows over 16 x 8 x 8192 rows
 // of 128 channels 98 and 98 us against 107 and 111, over 4 x 8 x 8192 41 and 40 against 41 and 42, over 1 x 8 x 8192 26
 // against 25; 20 and 32 over 16 x 8 x 8192 rows of 96 channels 86 and 87 against 91 and 94, 20 over 64 channels in pages
 // 68 against 74.
-int rows_of_unit(const lagkv_config& c, int query_rows, bool blocks, long long S_cap) {
-    const bool large = (long long)c.B * c.H_kv * S_cap >= 1 << 19;
-    return query_rows > 16 && query_rows <= 32 && large && !blocks && c.dtype != LAGKV_DTYPE_FP8_E4M3 ? 33 : query_rows;
+int rows_of_unit(const lagkv_plan_s* plan, int query_rows, bool blocks, long long S_cap) {
+    const lagkv_config& c = plan->cfg;
+    const bool fp8 = c.dtype == LAGKV_DTYPE_FP8_E4M3;
+    const long long heads = (long long)c.B * c.H_kv;
+    if (blocks || query_rows <= 16) return query_rows;
+    if (heads * ((query_rows + 15) / 16) * (S_cap / kAttendTile + kAttendLead) <= (long long)plan->sm_count * (fp8 ? 24 : 9)) return 16;
+    return query_rows <= 32 && !fp8 && heads * S_cap >= 1 << 19 ? 33 : query_rows;
 }
 
 // Picks the kernel, finds room in the workspace and launches.  `extra`: bytes of the workspace behind
@@ -156,7 +166,7 @@ int rows_of_unit(const lagkv_config& c, int query_rows, bool blocks, long long S
 int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, size_t extra, void* workspace, size_t bytes,
                    AttendParams* P, const AttendEntry** entry, unsigned char** rest) {
     int index = 0;
-    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows_of_unit(plan->cfg, query_rows, blocks, P->S_cap), blocks, &index);
+    const AttendEntry* e = find_attend(plan->cfg.D, plan->cfg.dtype, rows_of_unit(plan, query_rows, blocks, P->S_cap), blocks, &index);
     if (e == nullptr) return LAGKV_EUNSUPPORTED;
     const long long units = attend_units(plan, *e, query_rows, tokens);
     int rc = workspace_ok(workspace, bytes, kHead + 4096);
