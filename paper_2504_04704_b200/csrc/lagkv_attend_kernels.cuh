@@ -38,7 +38,8 @@ struct AttendParams {
     int B, H, G, T, S_cap, max_blocks, page_shift;
     int mtiles;            // groups of M rows per (sequence, KV head)
     int ctas;              // CTAs of the attention kernel
-    int least;             // tiles that a CTA takes at least
+    int least;             // wide kernel: tiles that a CTA takes at least
+    float per_units;       // the other: 1 / (6 units)
     int lead;              // what beginning a unit costs, in tiles: counted when the work is shared out
     float scale_log2, v_scale;
     const int32_t* idx;    // blocks: [B, T, H, keep] ascending block numbers, -1 behind the last
@@ -47,7 +48,6 @@ struct AttendParams {
 
 constexpr int kAttendTile = 64;     // rows of the unit of scheduling (lagkv_attend_kernel)
 constexpr int kAttendLead = 6;      // P.lead: 16 caches of 16384 rows in 79 us, 85 with equal shares of the rows
-constexpr int kAttendLeast = 2;     // P.least: one cache of 1024 rows in 10.8 us, 12.2 with one tile per CTA
 constexpr int kAttendWarps = 4;
 constexpr int kWarpRows = 16;       // rows of a warp's tile: never across a page or a block (both >= 16)
 
@@ -250,7 +250,18 @@ __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int u
         total += all;
     }
     AttendShare s;
-    s.per_cta = max((long long)P.least, div_small(total + gridDim.x - 1, gridDim.x));
+    // Equal shares, but not so small that joining them takes over: a share of p tiles takes time in p, the joining of a
+    // unit's W / p partials in W / p, so p is at least some sqrt(W); with W / 6 the least times measured are met within
+    // 10 % (128 channels, one token, one KV head of 20000 rows: 19 us, 32 in equal shares; of 100000: 34 and 54).  The wide
+    // kernel has no registers to spare for this, not even here (102 -> 109 us where it changes no share): P.least.
+    s.per_cta = div_small(total + gridDim.x - 1, gridDim.x);
+    if constexpr (TILE == kAttendTile) {
+        float p;  // approximate: it decides nothing but the shares, and the same way in every CTA
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(float(total) * P.per_units));
+        s.per_cta = max((long long)int(p + 0.999f), s.per_cta);
+    } else {
+        s.per_cta = max((long long)P.least, s.per_cta);
+    }
     s.pos = s.per_cta * blockIdx.x;
     s.end = s.pos + s.per_cta < total ? s.pos + s.per_cta : total;
     s.b = 0;
