@@ -715,7 +715,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
 // arrive joined them at first: a CTA and 37 partials of 16 rows took 20 us.)
 constexpr int kMergeWarps = 4;
 template <int D, int DT, int MT>
-__global__ void __launch_bounds__(kMergeWarps * 32)
+__global__ void __launch_bounds__(kMergeWarps * 32, 4)  // without the 4: 32 registers, hardly a read in flight, 1-3 us more
 lagkv_attend_merge_kernel(const __grid_constant__ AttendParams P) {
     constexpr int MR = AttendGeo<D, DT, MT>::MR, PSIZE = MR * (D + 2);
     constexpr int LANES = D / 4 < 32 ? D / 4 : 32;     // lanes of a row

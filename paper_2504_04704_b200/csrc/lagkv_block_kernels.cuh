@@ -24,7 +24,7 @@ constexpr int kSelectBins = 2048;
 // One warp per block: 16-byte loads, a row per group of lanes, packed min / max, groups joined by
 // shuffles.  Reads each row once and writes two rows per block: bound by HBM reads.
 template <int DT>
-__global__ void __launch_bounds__(kBoundsThreads)
+__global__ void __launch_bounds__(kBoundsThreads, 3)  // without the 3: spills, 257 us where this takes 246 (1.6 GB)
 lagkv_block_bounds_kernel(const AttendParams P, const int32_t* __restrict__ from_len, uint8_t* __restrict__ bounds,
                           long long blocks, int ctas_per_unit, int cpr) {
     using E = Elem<DT>;
@@ -367,7 +367,7 @@ __device__ __forceinline__ int warps_before(int v, int* wsum, int& total) {
 // One CTA per (sequence, token, KV head): the first `sink` and last `recent` blocks and the best of the
 // others, `keep` in all, lower block first among equals, written in ascending order with -1 behind.
 template <int DT>
-__global__ void __launch_bounds__(kSelectThreads)
+__global__ void __launch_bounds__(kSelectThreads, 2)  // without the 2: 40 registers, spills, 3 us more
 lagkv_block_select_kernel(const AttendParams P, const uint8_t* __restrict__ bounds, const ScoreShape S, int D,
                           unsigned long long* __restrict__ keys, int sink, int recent, int32_t* __restrict__ idx) {
     extern __shared__ float sa[];  // the candidates' scores, then the numbers of those near the border
