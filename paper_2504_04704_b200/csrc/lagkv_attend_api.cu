@@ -184,7 +184,7 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     // 32 tokens of 4 heads in 34 us, 45 with shares of one tile; of 8192 in 8 units 29 and 33.
     P->least = int(std::ceil(std::sqrt((P->S_cap / double(kWideTile) + kWideLead) / 6.0)));
     if (P->least > 4) P->least = 4;
-    P->per_units = 1.f / (6.f * float(units));
+    P->per_units = 1.f / (16.f * float(units));
     P->lead = e->wide ? kWideLead : kAttendLead;
     *entry = e;
     *rest = base + kHead + pb + sb;

@@ -39,7 +39,7 @@ struct AttendParams {
     int mtiles;            // groups of M rows per (sequence, KV head)
     int ctas;              // CTAs of the attention kernel
     int least;             // wide kernel: tiles that a CTA takes at least
-    float per_units;       // the other: 1 / (6 units)
+    float per_units;       // the other: 1 / (16 units)
     int lead;              // what beginning a unit costs, in tiles: counted when the work is shared out
     float scale_log2, v_scale;
     const int32_t* idx;    // blocks: [B, T, H, keep] ascending block numbers, -1 behind the last
@@ -251,9 +251,10 @@ __device__ __forceinline__ AttendShare attend_share(const AttendParams& P, int u
     }
     AttendShare s;
     // Equal shares, but not so small that joining them takes over: a share of p tiles takes time in p, the joining of a
-    // unit's W / p partials in W / p, so p is at least some sqrt(W); with W / 6 the least times measured are met within
-    // 10 % (128 channels, one token, one KV head of 20000 rows: 19 us, 32 in equal shares; of 100000: 34 and 54).  The wide
-    // kernel has no registers to spare for this, not even here (102 -> 109 us where it changes no share): P.least.
+    // unit's W / p partials in W / p, so p is at least some sqrt(W): with W / 16 the least times measured are met within
+    // 10 % (128 channels, one token, one KV head of 20000 rows: 15 us, of 100000: 30; 8 KV heads of 1216: 9.7, 10.4 with
+    // W / 6; equal shares took 32, 54 and 12 when joining was slower).  The wide kernel has no registers to spare for
+    // this, not even here (102 -> 109 us where it changes no share): P.least.
     s.per_cta = div_small(total + gridDim.x - 1, gridDim.x);
     if constexpr (TILE == kAttendTile) {
         float p;  // approximate: it decides nothing but the shares, and the same way in every CTA
