@@ -440,14 +440,15 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             return odd;
         };
-        // Notes the drafted rows of a V tile that are not finite; `piece(id)` gives 16 bytes of row id / CPR.
-        auto note_odd = [&](const WideCursor<G>& x, int slot, auto&& piece) {
+        // Notes the drafted rows of a V tile that are not finite; `piece(id)` gives 16 bytes of row id / CPR.  Rows of
+        // `groups` have no page: nothing was loaded for them, their place holds what an older tile left there.
+        auto note_odd = [&](const WideCursor<G>& x, int slot, uint32_t groups, auto&& piece) {
             if (ptid < 4) odd_rows[slot * 4 + ptid] = 0u;
             meet();
             const int first = max(0, x.U.base - x.row0()) * G::CPR, last = min(kWideTile, x.U.lim - x.row0()) * G::CPR;
 #pragma unroll 4
             for (int id = first + ptid; id < last; id += help)
-                if (not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
+                if (!(groups >> (id / G::CPR >> 4) & 1) && not_finite(piece(id))) atomicOr(&odd_rows[slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
             meet();
         };
         // the groups of 16 rows of a V tile whose pages are not in the pool
@@ -512,7 +513,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             if constexpr (DT == 2) {
                 if (slot_lap > 0) wait(b_empty + 8 * slot, (slot_lap + 1) & 1);
                 const unsigned char* from = smem + (s_raw - sbase) + place * G::RAW;
-                if (careful) note_odd(at, slot, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
+                if (careful) note_odd(at, slot, groups, [&](int id) { return *reinterpret_cast<const uint4*>(from + id * 16); });
                 // A row's 16-byte pieces become two each.  Eight lanes store to one panel's halves of two rows: the
                 // swizzle gives them all the banks.
                 const int r = D == 128 ? (ptid >> 4) * 2 + (ptid >> 2 & 1) : ptid / G::CPR, ch = D == 128 ? (ptid >> 1 & 4) + (ptid & 3) : ptid % G::CPR;
@@ -534,7 +535,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 }
                 if (mend) meet();
             } else if (careful) {
-                note_odd(at, slot, [&](int id) { return *piece(id); });
+                note_odd(at, slot, groups, [&](int id) { return *piece(id); });
             }
             if (mend)
                 for (int id = first_zero(at, slot, groups, careful) * (D / 8) + ptid; id < kWideTile * (D / 8); id += help)
@@ -750,7 +751,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                             const float z = __uint_as_float(tm_read1(t_s + 32 * q + e));
                             const bool see = seen32(r0 + 32 * q) >> e & 1;
                             const float p = see ? ex2(z * scl - at) : 0.f;
-                            const uint8_t* v = P.V + attend_offset(P, sh.b, U.h, r & ~15) + (long long)(r & 15) * P.ss;
+                            const long long off = attend_offset(P, sh.b, U.h, r & ~15);
+                            if (off < 0) continue;  // no page: never noted
+                            const uint8_t* v = P.V + off + (long long)(r & 15) * P.ss;
 #pragma unroll 1
                             for (int d = 0; d < D; d += 32) {
                                 tm_ld32(a, t_o + d);
