@@ -388,7 +388,8 @@ int lagkv_attend_tree_paged(lagkv_plan_t plan, const lagkv_query *query, const v
  * base + accepted[b*T + j], j < n_accepted[b], move to base + j in K and V (every KV head), and
  * seq_len[b] becomes base + n_accepted[b].  accepted (DEVICE int32 [B, T]) ascends strictly inside
  * [0, draft_len[b]).  A sequence whose lengths or path are not of that form is left untouched and
- * LAGKV_EINVAL is recorded.  draft_len as above, T 1..64.  The workspace needs its status block only.
+ * LAGKV_EINVAL is recorded.  draft_len as above (NULL: an empty slot, seq_len[b] = 0, has no draft and takes
+ * n_accepted[b] = 0), T 1..64.  The workspace needs its status block only.
  */
 int lagkv_tree_commit(lagkv_plan_t plan, void *K_cache, void *V_cache, int64_t S_cap, int32_t *seq_len,
                       const int32_t *draft_len, int32_t T, const int32_t *accepted, const int32_t *n_accepted,

@@ -15,7 +15,8 @@ lagkv_tree_commit_kernel(const AttendParams P, uint8_t* K, uint8_t* V, int vpr, 
                          const int32_t* __restrict__ accepted, const int32_t* __restrict__ n_accepted) {
     __shared__ int path[64];
     const int b = blockIdx.x, tid = threadIdx.x;
-    const int len = seq_len[b], draft = P.draft_len ? P.draft_len[b] : P.T, n = n_accepted[b], base = len - draft;
+    const int len = seq_len[b], n = n_accepted[b];
+    const int draft = P.draft_len ? P.draft_len[b] : len == 0 ? 0 : P.T, base = len - draft;  // an empty slot of the batch is no error
     bool bad = len < 0 || len > P.S_cap || draft < 0 || draft > P.T || draft > len || n < 0 || n > draft;
     if (!bad && tid < n) {
         const int a = accepted[(long long)b * P.T + tid];

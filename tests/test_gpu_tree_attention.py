@@ -468,3 +468,39 @@ def test_wide_trees_in_a_batch_of_short_sequences(binding, dtype, T, G):
     c = case(binding, 300, 2, G, 64, 500, T, dtype, seed=T, lens=lens)
     poison(c)
     U.assert_attention(run(c), reference(c))
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+def test_commit_of_a_batch_with_empty_slots(binding, paged):
+    """Without draft_len an empty slot has no tokens, as for the attention: no error, nothing moves.  One that claims an
+    accepted row is refused."""
+    B, H, S, D, T = 4, 2, 64, 64, 4
+    K, V, _, _ = U.make_cache((B, H, S, D), BF16, torch.Generator(device=DEV).manual_seed(1))
+    lens, paths = [0, 30, 0, T], [[], [1, 3], [], [2]]
+    wantK, wantV, want_len = commit_reference(K, V, lens, [0, T, 0, T], paths)
+    acc = torch.zeros((B, T), dtype=torch.int32)
+    for b, p in enumerate(paths):
+        acc[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+    acc, seq = acc.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    n = torch.tensor([len(p) for p in paths], dtype=torch.int32, device=DEV)
+    plan = binding.Plan(B, H, D, sink=0, lag=32)
+    ws = plan.new_workspace()
+    table = torch.arange(B * 4, dtype=torch.int32, device=DEV).view(B, 4)
+    pools = [U.to_pages(x, 16, table, B * 4, 0.0) for x in (K, V)]
+    table[0], table[2] = -1, -1
+
+    def commit():
+        if paged:
+            plan.tree_commit_paged(*pools, table, seq, acc, n, ws)
+        else:
+            plan.tree_commit(K, V, seq, acc, n, ws)
+
+    commit()
+    assert plan.read_status(ws)[0] == 0 and seq.tolist() == want_len
+    for b in (1, 3) if paged else range(B):
+        for x, pool, want in zip((K, V), pools, (wantK, wantV)):
+            got = U.from_pages(pool, table[b:b + 1], 16)[0] if paged else x[b]
+            assert torch.equal(U.bits(got), want[b])
+    n[0] = 1
+    commit()
+    assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL and int(seq[0]) == 0
