@@ -498,7 +498,8 @@ int lagkv_pages_fork(lagkv_plan_t plan, void *K_pool, void *V_pool, const lagkv_
  * Make the pool dense: with `live` pages in use, each one numbered live or higher moves, in ascending
  * order, to the lowest free numbers; K, V, refs and the block table follow.  Afterwards the pages [live,
  * num_pages) are free.  live_out: DEVICE int32 [1].  Every table that names pages of this pool has to be
- * in the call.  An entry that names a page which refs does not count: recorded as LAGKV_EINVAL, left alone.
+ * in the call.  An entry that names a page which refs does not count, or none of the pool: recorded as
+ * LAGKV_EINVAL, and it becomes -1, since its number may be another sequence's page afterwards.
  */
 int lagkv_pages_compact(lagkv_plan_t plan, void *K_pool, void *V_pool, const lagkv_paged_layout *layout,
                         int64_t num_pages, int32_t *refs, int32_t *live_out, void *workspace, size_t workspace_bytes,

@@ -13,7 +13,7 @@ namespace {
 // Workspace: [status | arrival counter, 256 bytes | per-pair and per-sequence numbers or new names | lists]
 constexpr size_t kFixedWords = 2 * kStatusWords;
 size_t work_words(const lagkv_plan_s* plan, int64_t num_pages) {
-    const size_t pairs = size_t(plan->cfg.B) * (kPairWords + 1) + 1, names = size_t(num_pages) + 2;
+    const size_t pairs = size_t(plan->cfg.B) * (kPairWords + 1) + 1, names = size_t(num_pages) + 1;
     return ((pairs > names ? pairs : names) + 63) & ~size_t(63);
 }
 

@@ -309,8 +309,8 @@ lagkv_pages_fork_kernel(const PageParams P, int32_t* seq_len, int32_t* static_le
 
 // ------------------------------------------------------------------------------------ compact
 // One CTA: counts the live pages, then lists the free ones below that number (list) and the live ones at
-// or above it (list + num_pages), both ascending, and turns work into the new names of the pages at or
-// above it (-1: not live).  work[0] = live pages, work[1] = pages to move, then the names.
+// or above it (list + num_pages), both ascending, and turns work into the new names of all pages (-1: not
+// live).  work[0] = pages to move, then the names.
 __global__ void __launch_bounds__(kScanThreads)
 lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
     __shared__ int sums[32];
@@ -334,6 +334,7 @@ lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
                 const bool used = P.refs[p] > 0;
                 if (p < live && !used) hole |= 1u << i;
                 if (p >= live && used) mover |= 1u << i;
+                P.work[1 + p] = p < live && used ? int(p) : -1;
             }
         }
         int nh, nm;
@@ -349,12 +350,9 @@ lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
     }
     __syncthreads();
     // as many holes below `live` as live pages at or above it
-    for (long long p = live + tid; p < P.num_pages; p += kScanThreads) P.work[2 + p] = -1;
-    __syncthreads();
-    for (long long i = tid; i < movers; i += kScanThreads) P.work[2 + P.list[P.num_pages + i]] = P.list[i];
+    for (long long i = tid; i < movers; i += kScanThreads) P.work[1 + P.list[P.num_pages + i]] = P.list[i];
     if (tid == 0) {
-        P.work[0] = int(live);
-        P.work[1] = int(movers);
+        P.work[0] = int(movers);
         *live_out = int(live);
     }
 }
@@ -362,16 +360,15 @@ lagkv_pages_compact_plan_kernel(const PageParams P, int32_t* live_out) {
 __global__ void __launch_bounds__(kPageThreads)
 lagkv_pages_compact_kernel(const PageParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int live = P.work[0], moves = P.work[1];
+    const int moves = P.work[0];
     const long long stride = (long long)gridDim.x * kPageThreads, first = blockIdx.x * (long long)kPageThreads + threadIdx.x;
     for (long long i = first; i < (long long)P.B * P.max_blocks; i += stride) {
         const int p = P.table[i];
-        if (p < live) continue;
-        const int to = p < P.num_pages ? P.work[2 + p] : -1;
-        if (to < 0)
-            record_status(P.status, ST_EINVAL, int(i / P.max_blocks));  // names a page that is not live
-        else
-            P.table[i] = to;
+        if (p < 0) continue;
+        const int to = p < P.num_pages ? P.work[1 + p] : -1;
+        // a page that is not live: the number may be another sequence's page from now on
+        if (to < 0) record_status(P.status, ST_EINVAL, int(i / P.max_blocks));
+        if (to != p) P.table[i] = to;
     }
     for (long long i = first; i < moves; i += stride) {
         const int from = P.list[P.num_pages + i], to = P.list[i];

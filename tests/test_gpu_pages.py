@@ -319,6 +319,33 @@ def test_an_entry_that_names_a_free_page(binding):
     assert d["table"][1, 2].item() < n or got == binding.LAGKV_EINVAL
 
 
+@pytest.mark.parametrize("name", ["hole", "behind", "outside"])
+def test_an_entry_that_names_an_uncounted_page_is_cleared(binding, name):
+    """Page 1 is free and below the number of live pages, page 7 free and behind: after the move their numbers may be
+    another sequence's page, so an entry that names one, or no page of the pool, is recorded and becomes -1."""
+    s = State(3, 3, 8, 16)
+    s.table = [[0, 2, 5], [3, -1, -1], [6, -1, -1]]
+    s.refs = [1, 0, 1, 1, 0, 1, 1, 0]
+    s.seq, s.static = [48, 16, 16], [0, 0, 0]
+    d = s.device()
+    d["table"][1, 2] = {"hole": 1, "behind": 7, "outside": 8}[name]
+    K, V = pools(s, 1, 64, BF16, 1)
+    wantK, wantV = (U.bits(x).clone() for x in (K, V))
+    plan = binding.Plan(3, 1, 64, sink=0, lag=32)
+    ws = plan.new_pages_workspace(8)
+    live = plan.pages_compact(K, V, d["table"], d["refs"], ws)
+    assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL
+    n, moves = s.compact()
+    assert moves == [(5, 1), (6, 4)]
+    for a, b in moves:
+        wantK[b], wantV[b] = wantK[a], wantV[a]
+    assert live.tolist() == [n]
+    s.same(d)
+    assert torch.equal(U.bits(K), wantK) and torch.equal(U.bits(V), wantV)
+    plan.pages_compact(K, V, d["table"], d["refs"], ws)
+    assert plan.read_status(ws)[0] == 0
+
+
 def test_refusals_touch_nothing(binding):
     import ctypes
     s = filled(2, 3, 8, 16, random.Random(2), [48, 0])
