@@ -268,8 +268,9 @@ lagkv_block_score_kernel(const AttendParams P, const uint8_t* __restrict__ bound
             m2 = fmaxf(m2, n == n ? n : INFINITY);
         }
     }
-    // 1.01: the roundings of the norms themselves
-    const float e = 1.01f * (D + 16) * 0x1p-22f * sqrtf(max_of_warp(q2)) * sqrtf(max_of_warp(m2)) + 1e-37f;
+    // 1.01: the roundings of the norms themselves.  Squares below 2^-149 vanish from them, at most D * 2^-149 in all: next
+    // to 2^-100 that is nothing, so smaller norms count as 2^-50.  Products that vanish (D * 2^-126) are covered with it.
+    const float e = 1.01f * (D + 16) * 0x1p-22f * sqrtf(fmaxf(max_of_warp(q2), 0x1p-100f)) * sqrtf(fmaxf(max_of_warp(m2), 0x1p-100f));
     if (lane == 0) red[w] = e == e ? e : INFINITY;
     __syncthreads();
     if (threadIdx.x == 0) {

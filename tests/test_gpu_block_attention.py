@@ -204,6 +204,26 @@ def test_thousands_of_scores_next_to_the_border(binding, keep):
     check(c, 16, keep)
 
 
+@pytest.mark.parametrize("q,k", [(0, 0), (-80, 0), (-100, 0), (0, -80), (-40, -60), (-126, 0)])
+def test_scores_next_to_the_border_of_tiny_values(binding, q, k):
+    """Blocks whose scores differ by less than the rounding of 32-bit sums, at queries and keys whose squares vanish."""
+    n, D, keep = 64, 128, 9
+    c = case(binding, 1, 1, 1, D, 16 * n, 1, BF16, 16, seed=11, lens=[16 * n], keep=keep)
+    g = torch.Generator(device=DEV).manual_seed(12)
+    base = (torch.randn(D - 1, generator=g, device=DEV) * torch.exp2(torch.rand(D - 1, generator=g, device=DEV) * 22 - 16)).to(BF16).float()
+    for i in range(3):                                            # large terms that cancel
+        base[i] = 0
+        base[i] = -base.sum().to(BF16).float()
+    rows = torch.zeros((n, D), device=DEV)
+    for j in range(n):                                            # the same terms in another order, and one that decides
+        rows[j, :D - 1] = base[torch.randperm(D - 1, generator=g, device=DEV)]
+        rows[j, D - 1] = ((j * 37) % n) * 2.0 ** -26
+    c["K"][0, 0] = (rows * 2.0 ** k).repeat_interleave(16, 0).to(BF16)
+    c["Q"].fill_(2.0 ** q)
+    c["plan"].block_bounds(c["K"], c["seq"], c["bounds"], c["ws"], block_rows=16)
+    check(c, 16, keep)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP8], ids=["bf16", "fp8"])
 @pytest.mark.parametrize("page,rows", [(16, 64), (64, 16), (32, 32)])
 def test_paged_equals_contiguous(binding, dtype, page, rows):
