@@ -648,7 +648,8 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 for (int d = 0; d < D; d += 8) top = fmaxf(top, largest_of(__ldg(reinterpret_cast<const uint4*>(q + d))));
                 f = query_factor(top);
             }
-            const float scl = P.scale_log2 / f;
+            // never 0, which would make NaN of the -infinity of hidden rows: below 2^-126 all logits (2^25 of it at most) are 0
+            const float scl = DT == 2 ? fmaxf(P.scale_log2 / f, 0x1p-126f) : P.scale_log2;
             unsigned long long bits = 0;
             if (there && U.masked && t < U.seq.tokens)
                 bits = P.mask ? P.mask[(long long)sh.b * P.T + t] : (t == 63 ? ~0ull : (2ull << t) - 1);

@@ -110,3 +110,16 @@ def test_missing_pages_under_drafted_rows(binding, dtype, T, G, page, D):
     assert c.plan.read_status(c.ws)[0] == binding.LAGKV_EINVAL
     U.assert_attention(got, c.reference(gone))
     assert not got["out"][4].any() and torch.isneginf(got["lse"][4]).all()
+
+
+@pytest.mark.parametrize("T,G", [(12, 4), (40, 4)])
+def test_tiny_queries_over_fp8(binding, T, G):
+    """Queries whose factor and scale multiply to less than fp32 holds: all logits are nearly 0, hidden rows stay hidden."""
+    c = Paged(binding, 3, 2, G, 128, T, FP8, 64, [T, 300, 129 + T])
+    c.Q = (c.Q.float() * 2.0 ** -122).to(BF16)
+    c.ks = 1e-7
+    pools = c.pools()
+    takes_wide(binding, lambda ws: c.call(pools, ws), c.ws, 128, 2 if T * G > 128 else 1)
+    got = c.call(pools)
+    assert c.plan.read_status(c.ws)[0] == 0
+    U.assert_attention(got, c.reference())
