@@ -334,7 +334,8 @@ typedef struct {
     int32_t T;         /* query tokens per sequence, 1..64                                      */
     int32_t H_q;       /* query heads: H_kv times 1..64                                         */
     double scale;      /* factor of q.k before the softmax, > 0; 0 = 1/sqrt(D)                  */
-    double k_scale;    /* what a stored K element of 1 stands for (fp8 caches), > 0; 0 = 1      */
+    double k_scale;    /* what a stored K element of 1 stands for (fp8 caches), > 0; 0 = 1;     */
+                       /* scale*k_scale*log2(e) and v_scale are finite in fp32                  */
     double v_scale;    /* the same for V                                                        */
     int64_t stride_b;  /* strides of Q [B, T, H_q, D] in elements, multiples of 8; 0 = dense    */
     int64_t stride_t;  /* over the dimension inside; channel stride 1, 16-byte aligned base     */

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstring>
 #include <cuda.h>
+#include <limits>
 
 #include "lagkv_attend_tables.h"
 #include "lagkv_block_kernels.cuh"
@@ -84,8 +85,9 @@ int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, vo
     if (!aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || Q == out) return LAGKV_EINVAL;
     const double scale = q->scale == 0.0 ? 1.0 / std::sqrt(double(c.D)) : q->scale;
     const double ks = q->k_scale == 0.0 ? 1.0 : q->k_scale, vs = q->v_scale == 0.0 ? 1.0 : q->v_scale;
-    if (!(scale > 0.0) || !(ks > 0.0) || !(vs > 0.0) || !std::isfinite(float(scale * ks)) || !std::isfinite(float(vs)))
-        return LAGKV_EINVAL;
+    // 0 would make NaN of the -infinity of hidden rows
+    const float scale_log2 = std::fmax(float(scale * ks * 1.4426950408889634), std::numeric_limits<float>::denorm_min());
+    if (!(scale > 0.0) || !(ks > 0.0) || !(vs > 0.0) || !std::isfinite(scale_log2) || !std::isfinite(float(vs))) return LAGKV_EINVAL;
     const int64_t sh = q->stride_h ? q->stride_h : c.D;
     const int64_t st = q->stride_t ? q->stride_t : (int64_t)q->H_q * sh;
     const int64_t sb = q->stride_b ? q->stride_b : (int64_t)q->T * st;
@@ -101,7 +103,7 @@ int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, vo
     P->H = c.H_kv;
     P->G = q->H_q / c.H_kv;
     P->T = q->T;
-    P->scale_log2 = float(scale * ks * 1.4426950408889634);
+    P->scale_log2 = scale_log2;
     P->v_scale = float(vs);
     return LAGKV_OK;
 }

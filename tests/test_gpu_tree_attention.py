@@ -504,3 +504,15 @@ def test_commit_of_a_batch_with_empty_slots(binding, paged):
     n[0] = 1
     commit()
     assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL and int(seq[0]) == 0
+
+
+def test_scales_at_the_ends_of_fp32(binding):
+    """scale * k_scale * log2(e) above fp32 is refused, also where scale * k_scale alone is not; below it all rows weigh the same."""
+    c = case(binding, 2, 2, 4, 128, 300, 3, BF16, seed=1)
+    poison(c)
+    for kw in (dict(scale=3e38), dict(scale=1e30, k_scale=2.5e8), dict(scale=1e30, k_scale=1e30), dict(v_scale=1e39)):
+        with pytest.raises(binding.LagKVError) as e:
+            c["plan"].attend_tree(c["Q"], c["K"], c["V"], c["seq"], c["ws"], **kw)
+        assert e.value.code == binding.LAGKV_EINVAL
+    for scale in (1e-37, 1e-45, 1e-60):
+        U.assert_attention(run(c, scale=scale), reference(c, scale))

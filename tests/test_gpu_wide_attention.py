@@ -123,3 +123,16 @@ def test_tiny_queries_over_fp8(binding, T, G):
     got = c.call(pools)
     assert c.plan.read_status(c.ws)[0] == 0
     U.assert_attention(got, c.reference())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_scales_that_vanish(binding, dtype):
+    """A scale that is 0 in fp32: every row that is seen weighs the same."""
+    T, G = 40, 4
+    c = Paged(binding, 2, 2, G, 64, T, dtype, 64, [300, 129 + T])
+    c.ks = 1e-60
+    pools = c.pools()
+    takes_wide(binding, lambda ws: c.call(pools, ws), c.ws, 64, 2)
+    got = c.call(pools)
+    assert c.plan.read_status(c.ws)[0] == 0
+    U.assert_attention(got, c.reference())
