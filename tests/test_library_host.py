@@ -107,3 +107,14 @@ def test_plain_c_program_links_and_runs(binding, tmp_path):
                     f"-l:{lib.name}", f"-Wl,-rpath,{lib.parent}"], check=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0 and out.stdout.strip() == "ok", out.stderr
+
+
+def test_every_source_file_triggers_a_build(binding, monkeypatch):
+    """The library counts as up to date only against every file that it is compiled from."""
+    import __graft_entry__ as g
+    seen = []
+    monkeypatch.setattr(g, "_newer", lambda target, sources: seen.append((target, list(sources))) or True)
+    g.build()
+    watched = next(set(s) for t, s in seen if t == g.LIB)
+    there = {p for d in (g.CSRC, g.ROOT / "include") for p in d.iterdir() if p.suffix in (".cu", ".cuh", ".h")}
+    assert g.CSRC / "lagkv_plan.h" in there and watched == there
