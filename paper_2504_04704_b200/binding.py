@@ -510,10 +510,13 @@ class Plan:
             raise TypeError("num_pages is needed with strides")
         else:
             c, (sp, sh, ss, rows) = self.cfg, strides
+            ss = ss or c.D                                        # 0 stands for dense, as in the library
+            sh = sh or rows * ss
+            sp = sp or c.H_kv * sh
             last = (num_pages - 1) * sp + (c.H_kv - 1) * sh + (rows - 1) * ss + c.D
-            size = K_pool.element_size()
-            if min(sp, sh, ss) < 0 or last > K_pool.untyped_storage().nbytes() // size - K_pool.storage_offset():
-                raise TypeError(f"num_pages = {num_pages} and strides {tuple(strides)} reach behind the pool")
+            for pool in (K_pool,) if V_pool is None else (K_pool, V_pool):
+                if min(sp, sh, ss) < 0 or last > pool.untyped_storage().nbytes() // pool.element_size() - pool.storage_offset():
+                    raise TypeError(f"num_pages = {num_pages} and strides {tuple(strides)} reach behind the pool")
         return self._paged(K_pool, block_table, strides), int(num_pages)
 
     def attend_tree(self, Q, K, V, seq_len, workspace, draft_len=None, tree_mask=None, scale=None, k_scale=1.0,
