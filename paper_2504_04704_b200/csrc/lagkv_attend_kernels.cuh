@@ -386,7 +386,7 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
                         const int v = vrow0 + (w + (i + lane) * G::NW) * kWarpRows;
                         int r = v;
                         if (blocks) {
-                            const int j = __ldg(bidx + (v >> P.block_shift));
+                            const int j = __ldcg(bidx + (v >> P.block_shift));  // written while this kernel was starting
                             r = j < 0 ? 0x7fffffff : (j << P.block_shift) + (v & ((1 << P.block_shift) - 1));
                         }
                         row_of = r;

@@ -151,3 +151,14 @@ def test_large_capacities(binding, dtype, D, T, G):
         got = c["plan"].attend_tree_paged(c["Q"], *pools, table, c["seq"], c["ws"], k_scale=c["ks"], v_scale=c["vs"], want_lse=True)
         U.assert_attention(got, want)
     assert c["plan"].read_status(c["ws"])[0] == 0
+
+
+def test_choices_of_one_workspace_in_turn(binding):
+    """Calls back to back on one workspace, each with another choice in the same place: none sees the other's."""
+    a = make(binding, 3, 2, 4, 64, 4000, 2, BF16, 10)
+    b = {**a, "Q": -a["Q"], "seq": a["seq"] - 900}
+    want = [blocks(c) for c in (a, b)]
+    assert not same(*want)
+    got = [(blocks(a), blocks(b)) for _ in range(50)]
+    assert all(same(g[i], want[i]) for g in got for i in (0, 1))
+    assert a["plan"].read_status(a["ws"])[0] == 0
