@@ -402,6 +402,7 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
             }
             if (!free) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+                ok = false;
                 break;
             }
             if (lane == 0) {
@@ -900,7 +901,12 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
         }
     }
     tm_fence_before();
-    __syncthreads();
+    // a wait that ran out may have left copies and products in flight: they get one more bounded chance
+    if (__syncthreads_or(!ok)) {
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 200000000ull) { /* bounded drain delay */ }
+        __syncthreads();
+    }
     if (w == 8) tm_free(tm);
 }
 
