@@ -326,9 +326,11 @@ int lagkv_gather_paged(lagkv_plan_t plan, const void *K_pool, const void *V_pool
  * keep_ratio play no part) and the same caches, one layer per call.
  *
  * Queries: T tokens per sequence, H_q heads; query head h reads KV head h / (H_q / H_kv).  Q and the
- * output are bf16 for bf16 and fp8 caches, fp16 for fp16 caches.  Products of queries and keys,
+ * output are bf16 for bf16 and fp8 caches, fp16 for fp16 caches.  Sums of products of queries and keys,
  * softmax statistics and sums are fp32; probabilities are rounded to the 16-bit type of the matrix
- * products (fp16 for fp8 caches, whose rows widen to fp16 exactly).
+ * products (fp16 for fp8 caches, whose rows widen to fp16 exactly), each by half a step of it.  Over fp8
+ * caches a row of queries becomes fp16, too, after a power of two has brought its largest element to
+ * [2^8, 2^9): elements below 2^-25 of that one lose bits, at most 2^-33 of it.
  */
 typedef struct {
     int32_t T;         /* query tokens per sequence, 1..64                                      */

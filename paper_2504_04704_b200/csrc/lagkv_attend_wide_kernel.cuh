@@ -13,11 +13,13 @@
 // next unit's queries, mend V tiles -- rows behind the last one and hidden rows that are not finite become
 // zeros, so that 0 * inf never happens -- and widen fp8 tiles, which land as they are, to fp16.
 // Partials of shared units are 66 KB for 128 query rows.
-// Bound: at 128 rows and 16-bit caches by HBM (16 x 8 x 9728 rows of 128 bf16 channels under 32 tokens of 4 heads in
-// 102 us: 64 % of the DRAM's peak, tensor cores 35 %), at 256 by the 16384 exponentials per tile and stream, 16 a
-// cycle and SM, as long as the products themselves (2 x 8 x 131072 fp16 rows under 64 tokens in 270 us, tensor cores
-// 49 %).  fp8 caches: by the way of a tile through shared memory, landed, widened and multiplied, with room for three and
-// four of them (8 x 8 x 19968 rows under 13 tokens in 123 us where HBM takes 41).
+// What it is near: at 128 rows and 16-bit caches HBM (16 x 8 x 9728 rows of 128 bf16 channels under 32 tokens of 4
+// heads in 102 us: 64 % of the DRAM's peak, tensor cores 35 %).  At 256 rows no unit is full (2 x 8 x 131072 fp16 rows
+// under 64 tokens in 270 us, tensor cores 49 %): of some 5200 cycles a step the products need 2850 and the 2 x 16384
+// exponentials, 16 a cycle, 2050 beside them; the rest is the softmax warps, two to a scheduler, waiting for one
+// part of their scores after the other.  fp8 caches: the way of a tile through shared memory, landed, widened and
+// multiplied, with three slots for widened tiles and three or four places to land in at 128 and 96 channels (8 x 8 x
+// 19968 rows under 13 tokens in 123 us where HBM takes 41).
 #pragma once
 #include <cuda.h>
 
@@ -47,7 +49,9 @@ struct WideGeo {
     static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
-    static constexpr int RS = DT_ == 2 ? (MT_ == 1 && D_ > 64 ? 3 : 4) : 0;  // ... and how many are in flight (3 leave room for a 4th slot)
+    // ... and how many are in flight.  There are 3 slots with 3 of them and with 4 at 128 channels; 3 are a little quicker:
+    // 126.1 us against 127.5 for 8 x 8 x 19968 rows under 13 tokens.
+    static constexpr int RS = DT_ == 2 ? (MT_ == 1 && D_ > 64 ? 3 : 4) : 0;
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
     static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
     static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
@@ -684,7 +688,10 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 };
                 // Two passes over the scores, the largest logit and then the probabilities (one pass that holds a
                 // tile's probabilities until the largest is known spills and misses in the instruction cache).
-                // The reference moves only when a probability would pass 2^6 of what it was set for.
+                // The reference moves only when a probability would pass 2^6 of what it was set for: 120 us against 122.5
+                // for 32 tokens, 312-317 against 326-332 for 64, where it moves with every larger logit.  In 64-bit
+                // emulation (9728 rows of 128 channels) the rounding of P then costs 0.0017 of the output's norm instead of
+                // 0.0012 in bf16, 0.00021 instead of 0.00015 in fp16: the largest probability is no longer exactly 1.
                 uint32_t a[32], b[32], c[32];
                 float top;
                 if (!hidden) {
