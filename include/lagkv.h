@@ -450,6 +450,105 @@ int lagkv_attend_blocks_paged(lagkv_plan_t plan, const lagkv_query *query, const
                               int32_t *idx_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * ---- Caches in 8 bits with block scales --------------------------------------------------------
+ * A cache for a plan of 16-bit format that stores 8-bit codes and one fp32 scale per (sequence, KV head, block of
+ * block_rows rows), for K and for V: row r stands for scale[b][h][r/block_rows] * codes.  Rows are quantised as they
+ * are written, read back in 16 bits where the compress pass is to run on them again, and attended to
+ * as they are.  plan: B, H_kv, D, dtype (bf16 or fp16: the 16-bit side, queries and outputs) and device as everywhere;
+ * its strides are those of the 16-bit cache that lagkv_quant_read() fills (and have to be 0 for paged caches).
+ */
+enum lagkv_quant_format {
+    LAGKV_QUANT_INT8 = 0, /* signed whole numbers, -127..127 as written here                     */
+    LAGKV_QUANT_E4M3 = 1  /* e4m3 as in LAGKV_DTYPE_FP8_E4M3; scales written here are powers of two */
+};
+
+typedef struct {
+    void *K, *V;          /* DEVICE codes, 16-byte aligned: [B, H_kv, S_cap, D], or pools of pages    */
+    float *K_scale;       /* DEVICE fp32 [B, H_kv, blocks], of K and of V; >= 0, finite               */
+    float *V_scale;
+    int32_t format;       /* enum lagkv_quant_format                                                  */
+    int32_t block_rows;   /* 16, 32, 64 or 128; on paged caches at most page_size                     */
+    int64_t blocks;       /* blocks*block_rows >= rows a sequence may have                            */
+    int64_t stride_b;     /* strides of the codes in bytes, multiples of 16; 0 = dense, as for other  */
+    int64_t stride_h;     /* caches; 0 on paged caches, whose layout carries them (in bytes)          */
+    int64_t stride_s;
+} lagkv_quant_cache;
+
+/* Rows to write: K, V [B, H_kv, T, D] in the plan's 16-bit format, any strides with channel stride 1. */
+typedef struct {
+    int32_t T;            /* rows per (sequence, KV head) of K and V                                  */
+    int32_t at_positions; /* 0: position p of the cache is row p - from_len[b]; else row p (T > every
+                             position written), as when a 16-bit cache is quantised                   */
+    const int32_t *take;  /* NULL, or DEVICE int32 [B, take_heads, take_rows]: position from_len[b] + i
+                             is row take[..][i] (then at_positions plays no part): the idx_out of
+                             lagkv_compress_prefill() writes the kept rows straight from the raw cache,
+                             a list of accepted tokens those of a draft                               */
+    int32_t take_heads;   /* 1 (the same for every KV head) or H_kv                                   */
+    int32_t take_rows;
+    int64_t stride_b;     /* in elements, multiples of 8; 0 = dense                                   */
+    int64_t stride_h;
+    int64_t stride_t;
+} lagkv_quant_source;
+
+/*
+ * Write rows [from_len[b], seq_len[b]) of each sequence (DEVICE int32 [B]; from_len NULL = 0; the caller's lengths are not
+ * changed).  With a = the largest magnitude of the rows of a block that the call writes,
+ *     int8:  f = max(a/127, 2^-126), a/127 correctly rounded to fp32; code = x/s, nearest whole number, ties to even
+ *     e4m3:  f = max(the least power of two with a <= 448*f, 2^-126); code = the nearest e4m3 to x/s
+ * (f = 0 where a = 0).  A block that begins at or behind from_len[b] gets s = f.  One that holds older rows gets
+ * s = max(f, its scale); where that is larger the older codes become code*(old scale)/s, rounded again.  The codes are those of
+ * exact quotients (e4m3: for scales that are powers of two).  Other blocks, and rows behind seq_len[b], stay as they are.
+ * Values that are not finite: LAGKV_EINVAL is recorded; they do not count in a, infinities become the largest code, NaN 0.
+ * Refused (LAGKV_EINVAL recorded, the sequence untouched): lengths outside 0 <= from_len <= seq_len <= S_cap, more new
+ * rows than T (take_rows), positions behind T with at_positions.  A take entry outside [0, T): recorded, that row is 0.
+ * A page outside the pool: recorded, its block is left out.  No page may be written through two table entries.
+ * One launch; the workspace needs its status block only, and any workspace of the plan will do.
+ */
+int lagkv_quant_write(lagkv_plan_t plan, const lagkv_quant_cache *cache, int64_t S_cap, const lagkv_quant_source *source,
+                      const void *K, const void *V, const int32_t *from_len, const int32_t *seq_len, void *workspace,
+                      size_t workspace_bytes, void *cuda_stream);
+int lagkv_quant_write_paged(lagkv_plan_t plan, const lagkv_quant_cache *cache, const lagkv_paged_layout *layout,
+                            int64_t num_pages, const lagkv_quant_source *source, const void *K, const void *V,
+                            const int32_t *from_len, const int32_t *seq_len, void *workspace, size_t workspace_bytes,
+                            void *cuda_stream);
+
+/*
+ * Read rows back in the plan's 16-bit format: scale*code in fp32, rounded once more to 16 bits (values beyond its largest
+ * become that).
+ *   idx NULL: K_out, V_out are caches [B, H_kv, rows_out, D] with the plan's strides (0 = dense); rows [from_len[b], seq_len[b])
+ *             go to the same positions there, others stay as they are.  rows_out >= every seq_len[b].
+ *   idx       DEVICE int32 [B, H_kv, rows_out], from_len NULL: row i of the dense outputs [B, H_kv, rows_out, D] is row
+ *             idx[b][h][i], in [0, seq_len[b]); other entries are recorded and leave their row as it is.
+ * K_out or V_out may be NULL.  Lengths that do not fit: LAGKV_EINVAL recorded, nothing read.  A page outside the pool:
+ * recorded, its rows stay as they are.  One launch; the workspace needs its status block only.
+ */
+int lagkv_quant_read(lagkv_plan_t plan, const lagkv_quant_cache *cache, int64_t S_cap, const int32_t *from_len,
+                     const int32_t *seq_len, const int32_t *idx, int64_t rows_out, void *K_out, void *V_out,
+                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+int lagkv_quant_read_paged(lagkv_plan_t plan, const lagkv_quant_cache *cache, const lagkv_paged_layout *layout,
+                           int64_t num_pages, const int32_t *from_len, const int32_t *seq_len, const int32_t *idx,
+                           int64_t rows_out, void *K_out, void *V_out, void *workspace, size_t workspace_bytes,
+                           void *cuda_stream);
+
+/*
+ * lagkv_attend_tree() over such a cache: the same lengths, masks, queries (T, heads, strides, scale; k_scale and v_scale
+ * count on top of the block scales), results and errors.  cap > 0 (2^-100 at least): every logit x becomes cap*tanh(x/cap); 0: none.
+ * Products are in fp16 (codes are exact in it) with fp32 sums; bf16 queries enter as fp16 after a power of two per row,
+ * as over fp8 caches.  K scales multiply the fp32 logits; V scales multiply the probabilities before these are rounded to
+ * fp16, relative to a power of two near the largest scale seen: a row whose scale is 2^-20 of that one or less loses bits.
+ * Workspace: lagkv_attend_quant_workspace_bytes() (0 = bad arguments), cleared once with
+ * lagkv_attend_workspace_init(); it serves every smaller call, one at a time.
+ */
+size_t lagkv_attend_quant_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q);
+int lagkv_attend_quant(lagkv_plan_t plan, const lagkv_query *query, double cap, const lagkv_quant_cache *cache, const void *Q,
+                       int64_t S_cap, const int32_t *seq_len, const int32_t *draft_len, const uint64_t *tree_mask,
+                       void *out, float *lse_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+int lagkv_attend_quant_paged(lagkv_plan_t plan, const lagkv_query *query, double cap, const lagkv_quant_cache *cache,
+                             const void *Q, const lagkv_paged_layout *layout, int64_t num_pages, const int32_t *seq_len,
+                             const int32_t *draft_len, const uint64_t *tree_mask, void *out, float *lse_out,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * ---- Pages --------------------------------------------------------------------------------
  * A pool of num_pages pages, block tables over it (lagkv_paged_layout; entries are -1 where a sequence
  * has no page) and refs (DEVICE int32 [num_pages]): refs[p] = table entries that name page p, 0 = free.

@@ -33,7 +33,9 @@ EXPORTS = (
     "lagkv_compress_append_paged", "lagkv_gather", "lagkv_gather_paged",
     "lagkv_attend_workspace_bytes", "lagkv_attend_workspace_init", "lagkv_attend_tree", "lagkv_attend_tree_paged",
     "lagkv_tree_commit", "lagkv_tree_commit_paged", "lagkv_block_bounds", "lagkv_block_bounds_paged",
-    "lagkv_attend_blocks", "lagkv_attend_blocks_paged", "lagkv_pages_workspace_bytes", "lagkv_pages_workspace_init",
+    "lagkv_attend_blocks", "lagkv_attend_blocks_paged", "lagkv_quant_write", "lagkv_quant_write_paged", "lagkv_quant_read",
+    "lagkv_quant_read_paged", "lagkv_attend_quant_workspace_bytes", "lagkv_attend_quant", "lagkv_attend_quant_paged",
+    "lagkv_pages_workspace_bytes", "lagkv_pages_workspace_init",
     "lagkv_pages_release", "lagkv_pages_reserve", "lagkv_pages_fork", "lagkv_pages_compact",
     "lagkv_read_status",
     "lagkv_launch_info", "lagkv_plan_tune", "lagkv_selftest_bounded_wait", "lagkv_status_string", "lagkv_version",
@@ -76,6 +78,21 @@ class lagkv_block_choice(ctypes.Structure):
     _fields_ = [
         ("block_rows", ctypes.c_int32), ("keep", ctypes.c_int32), ("sink_blocks", ctypes.c_int32),
         ("recent_blocks", ctypes.c_int32), ("blocks", ctypes.c_int64),
+    ]
+
+
+class lagkv_quant_cache(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+        ("format", ctypes.c_int32), ("block_rows", ctypes.c_int32), ("blocks", ctypes.c_int64),
+        ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_s", ctypes.c_int64),
+    ]
+
+
+class lagkv_quant_source(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("at_positions", ctypes.c_int32), ("take", ctypes.c_void_p), ("take_heads", ctypes.c_int32),
+        ("take_rows", ctypes.c_int32), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
     ]
 
 
@@ -151,6 +168,21 @@ def load_library() -> ctypes.CDLL:
     lib.lagkv_attend_blocks.argtypes = [vp, query, choice, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lagkv_attend_blocks_paged.restype = ctypes.c_int
     lib.lagkv_attend_blocks_paged.argtypes = [vp, query, choice, vp, vp, vp, layout, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    quant, source = ctypes.POINTER(lagkv_quant_cache), ctypes.POINTER(lagkv_quant_source)
+    lib.lagkv_quant_write.restype = ctypes.c_int
+    lib.lagkv_quant_write.argtypes = [vp, quant, i64, source, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_quant_write_paged.restype = ctypes.c_int
+    lib.lagkv_quant_write_paged.argtypes = [vp, quant, layout, i64, source, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_quant_read.restype = ctypes.c_int
+    lib.lagkv_quant_read.argtypes = [vp, quant, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.lagkv_quant_read_paged.restype = ctypes.c_int
+    lib.lagkv_quant_read_paged.argtypes = [vp, quant, layout, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.lagkv_attend_quant_workspace_bytes.restype = sz
+    lib.lagkv_attend_quant_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.lagkv_attend_quant.restype = ctypes.c_int
+    lib.lagkv_attend_quant.argtypes = [vp, query, ctypes.c_double, quant, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lagkv_attend_quant_paged.restype = ctypes.c_int
+    lib.lagkv_attend_quant_paged.argtypes = [vp, query, ctypes.c_double, quant, vp, layout, i64, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lagkv_pages_workspace_bytes.restype = sz
     lib.lagkv_pages_workspace_bytes.argtypes = [vp, i64]
     lib.lagkv_pages_workspace_init.restype = ctypes.c_int
@@ -214,6 +246,43 @@ def lagkv_keep_for_target(Ls: int, sink: int, lag: int, target_C: float) -> int:
 
 DTYPE_BF16, DTYPE_FP16, DTYPE_FP8_E4M3 = 0, 1, 2
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16, torch.float8_e4m3fn: DTYPE_FP8_E4M3}
+QUANT_INT8, QUANT_E4M3 = 0, 1
+_QUANT_FORMATS = {torch.int8: QUANT_INT8, torch.float8_e4m3fn: QUANT_E4M3}
+
+
+def _dense_strides(t, name: str):
+    """Strides of the outer dimensions of ``t`` as the library takes them: 0 where dense ones or none are meant."""
+    if t.is_contiguous():
+        return (0,) * (t.dim() - 1)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise TypeError(f"{name} must have channel stride 1")
+    if any(n > 1 and st == 0 for n, st in zip(t.shape, t.stride())):  # 0 would stand for dense
+        raise TypeError(f"{name} must not be broadcast")
+    got, dense = [], t.shape[-1]
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        got.append(st if n > 1 else dense)
+        dense = n * got[-1]
+    return tuple(reversed(got))
+
+
+class QuantCache:
+    """A cache in 8 bits with block scales (``lagkv_quant_cache``): codes ``K``, ``V`` as ``torch.int8`` or
+    ``torch.float8_e4m3fn``, ``[B, H, S_cap, D]`` or pools ``[num_pages, H, page_size, D]``, and their scales
+    ``K_scale``, ``V_scale``, fp32 ``[B, H, blocks]``, one for each ``block_rows`` rows of a sequence (of the
+    sequence on paged caches too: a fork copies its scales along with its table row)."""
+
+    def __init__(self, K, V, K_scale, V_scale, block_rows=64):
+        if K.dtype not in _QUANT_FORMATS or V.dtype != K.dtype or K.shape != V.shape or K.dim() != 4 or K.device != V.device:
+            raise TypeError("K and V must be torch.int8 or torch.float8_e4m3fn tensors of four dimensions, alike")
+        for t in (K_scale, V_scale):
+            if t.dtype != torch.float32 or t.dim() != 3 or t.shape != K_scale.shape or not t.is_contiguous() or t.device != K.device:
+                raise TypeError("K_scale and V_scale must be contiguous fp32 tensors [B, H, blocks] on the codes' device")
+        self.K, self.V, self.K_scale, self.V_scale, self.block_rows = K, V, K_scale, V_scale, int(block_rows)
+        self.strides = _dense_strides(K, "K")
+        if _dense_strides(V, "V") != self.strides:
+            raise TypeError("K and V must have the same strides")
+        self.arg = lagkv_quant_cache(K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr(), _QUANT_FORMATS[K.dtype],
+                                     self.block_rows, K_scale.shape[2], *self.strides)
 
 
 class Plan:
@@ -491,11 +560,12 @@ class Plan:
         lse = Q.new_empty(Q.shape[:3], dtype=torch.float32) if want_lse else None
         return out, lse
 
-    def _paged_pool(self, K_pool, V_pool, block_table, strides, num_pages):
+    def _paged_pool(self, K_pool, V_pool, block_table, strides, num_pages, dtype=None):
         """Layout and page count of a pool, checked against the tensors."""
+        dtype = dtype or self.dtype
         for pool in (K_pool, V_pool):
-            if pool is not None and (pool.dtype != self.dtype or pool.get_device() != self.device):
-                raise TypeError(f"the pools must be {self.dtype} CUDA tensors on device {self.device}")
+            if pool is not None and (pool.dtype != dtype or pool.get_device() != self.device):
+                raise TypeError(f"the pools must be {dtype} CUDA tensors on device {self.device}")
         if V_pool is not None:
             if V_pool.shape != K_pool.shape or V_pool.stride() != K_pool.stride():
                 raise TypeError("K_pool and V_pool must have the same shape and strides")
@@ -673,6 +743,158 @@ class Plan:
             _raw_stream(self.device))
         _check(rc, "lagkv_attend_blocks_paged")
         return got
+
+    # ---- caches in 8 bits with block scales
+    def new_quant_cache(self, S_cap: int, format: str = "int8", block_rows: int = 64, num_pages: int = 0, page_size: int = 0) -> QuantCache:
+        """An empty ``QuantCache`` of ``"int8"`` or ``"e4m3"`` codes for ``S_cap`` rows, contiguous, or a pool of
+        ``num_pages`` pages for sequences of up to ``S_cap`` rows."""
+        c, dev = self.cfg, self._dev()
+        dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[format]
+        shape = (int(num_pages), c.H_kv, int(page_size), c.D) if num_pages else (c.B, c.H_kv, int(S_cap), c.D)
+        rows = -(-int(S_cap) // int(page_size)) * int(page_size) if num_pages else int(S_cap)
+        scales = (c.B, c.H_kv, -(-rows // int(block_rows)))
+        return QuantCache(*(torch.zeros(shape, dtype=torch.uint8, device=dev).view(dtype) for _ in "KV"),
+                          *(torch.zeros(scales, dtype=torch.float32, device=dev) for _ in "KV"), block_rows=block_rows)
+
+    def _check_quant(self, cache, paged: bool):
+        c = self.cfg
+        if cache.K.get_device() != self.device:
+            raise TypeError(f"the cache must be on device {self.device}")
+        if cache.K_scale.shape[:2] != (c.B, c.H_kv) or cache.K.shape[1] != c.H_kv or cache.K.shape[3] != c.D or \
+                not paged and cache.K.shape[0] != c.B:
+            raise TypeError(f"the cache must be [{c.B}, {c.H_kv}, S_cap, {c.D}], or pages [num_pages, {c.H_kv}, page_size, {c.D}], "
+                            f"with scales [{c.B}, {c.H_kv}, blocks]")
+        if paged and any(cache.strides):
+            raise TypeError("paged codes must be contiguous")
+        return ctypes.byref(cache.arg)
+
+    def _quant_source(self, K, V, from_len, seq_len, take, at_positions):
+        c, shape = self.cfg, K.shape
+        for t, name in ((K, "K"), (V, "V")):
+            if t.dtype != self.dtype or t.get_device() != self.device or t.dim() != 4 or t.shape != (c.B, c.H_kv, shape[2], c.D):
+                raise TypeError(f"{name} must be a {self.dtype} CUDA tensor [{c.B}, {c.H_kv}, T, {c.D}] on device {self.device}")
+        strides = _dense_strides(K, "K")
+        if _dense_strides(V, "V") != strides:
+            raise TypeError("K and V must have the same strides")
+        self._check_ints(seq_len, "seq_len", (c.B,))
+        self._check_ints(from_len, "from_len", (c.B,))
+        heads = rows = 0
+        if take is not None:
+            if take.dim() == 2:
+                take = take[:, None]
+            if take.dim() != 3 or take.shape[1] not in (1, c.H_kv):
+                raise TypeError("take must be [B, rows] or [B, H_kv, rows]")
+            heads, rows = take.shape[1], take.shape[2]
+            self._check_ints(take, "take", (c.B, heads, rows))
+        return lagkv_quant_source(shape[2], int(bool(at_positions)), _addr(take), heads, rows, *strides)
+
+    def quant_write(self, cache, K, V, seq_len, workspace, from_len=None, take=None, at_positions=False) -> None:
+        """``lagkv_quant_write``: rows ``[from_len[b], seq_len[b])`` of the cache from ``K``, ``V`` ``[B, H, T, D]`` (any strides,
+        channel stride 1): row ``p - from_len[b]`` for position p, row p with ``at_positions``, or row ``take[b, h, p - from_len[b]]``
+        (``take`` int32 ``[B, H, rows]`` or ``[B, rows]``)."""
+        q = self._check_quant(cache, False)
+        src = self._quant_source(K, V, from_len, seq_len, take, at_positions)
+        rc = self.lib.lagkv_quant_write(self.handle, q, int(cache.K.shape[2]), ctypes.byref(src), _addr(K), _addr(V), _addr(from_len),
+                                        _addr(seq_len), *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_quant_write")
+
+    def quant_write_paged(self, cache, block_table, K, V, seq_len, workspace, from_len=None, take=None, at_positions=False) -> None:
+        """``lagkv_quant_write_paged``: the same into pools of pages."""
+        q = self._check_quant(cache, True)
+        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        src = self._quant_source(K, V, from_len, seq_len, take, at_positions)
+        rc = self.lib.lagkv_quant_write_paged(
+            self.handle, q, ctypes.byref(lay), pages, ctypes.byref(src), _addr(K), _addr(V), _addr(from_len), _addr(seq_len),
+            *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_quant_write_paged")
+
+    def _quant_out(self, seq_len, from_len, idx, K_out, V_out):
+        c = self.cfg
+        self._check_ints(seq_len, "seq_len", (c.B,))
+        self._check_ints(from_len, "from_len", (c.B,))
+        if idx is not None:
+            if idx.dim() != 3:
+                raise TypeError("idx must be [B, H, rows]")
+            self._check_ints(idx, "idx", (c.B, c.H_kv, idx.shape[2]))
+            want = (c.B, c.H_kv, idx.shape[2], c.D)
+            if K_out is None and V_out is None:
+                K_out, V_out = (torch.empty(want, dtype=self.dtype, device=self._dev()) for _ in "KV")
+            for t, name in ((K_out, "K_out"), (V_out, "V_out")):
+                if t is not None and (t.shape != want or t.dtype != self.dtype or t.get_device() != self.device or not t.is_contiguous()):
+                    raise TypeError(f"{name} must be a contiguous {self.dtype} CUDA tensor {want} on device {self.device}")
+            return K_out, V_out, idx.shape[2]
+        if K_out is None and V_out is None:
+            raise TypeError("K_out or V_out is needed without idx")
+        for t, name in ((K_out, "K_out"), (V_out, "V_out")):
+            if t is not None:
+                self._check_contiguous_cache(t, name)
+        if K_out is not None and V_out is not None and K_out.shape != V_out.shape:
+            raise TypeError("K_out and V_out must have the same shape")
+        return K_out, V_out, (V_out if K_out is None else K_out).shape[2]
+
+    def quant_read(self, cache, seq_len, workspace, from_len=None, idx=None, K_out=None, V_out=None):
+        """``lagkv_quant_read``: rows ``[from_len[b], seq_len[b])`` into the same positions of the 16-bit caches ``K_out``, ``V_out``
+        ``[B, H, rows, D]`` (one may be None), or rows ``idx`` int32 ``[B, H, rows]`` into dense outputs. Returns both."""
+        q = self._check_quant(cache, False)
+        K_out, V_out, rows = self._quant_out(seq_len, from_len, idx, K_out, V_out)
+        rc = self.lib.lagkv_quant_read(self.handle, q, int(cache.K.shape[2]), _addr(from_len), _addr(seq_len), _addr(idx), int(rows),
+                                       _addr(K_out), _addr(V_out), *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_quant_read")
+        return K_out, V_out
+
+    def quant_read_paged(self, cache, block_table, seq_len, workspace, from_len=None, idx=None, K_out=None, V_out=None):
+        """``lagkv_quant_read_paged``: the same from pools of pages."""
+        q = self._check_quant(cache, True)
+        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        K_out, V_out, rows = self._quant_out(seq_len, from_len, idx, K_out, V_out)
+        rc = self.lib.lagkv_quant_read_paged(
+            self.handle, q, ctypes.byref(lay), pages, _addr(from_len), _addr(seq_len), _addr(idx), int(rows), _addr(K_out), _addr(V_out),
+            *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_quant_read_paged")
+        return K_out, V_out
+
+    def new_attend_quant_workspace(self, T: int, H_q: int) -> torch.Tensor:
+        """Workspace for ``attend_quant`` calls of up to ``T`` tokens and ``H_q`` query heads."""
+        nbytes = int(self.lib.lagkv_attend_quant_workspace_bytes(self.handle, int(T), int(H_q)))
+        if nbytes == 0:
+            raise LagKVError(LAGKV_EINVAL, "lagkv_attend_quant_workspace_bytes")
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self._dev())
+        _check(self.lib.lagkv_attend_workspace_init(self.handle, _ptr(ws), ws.numel(), _stream(self._dev())),
+               "lagkv_attend_workspace_init")
+        return ws
+
+    def attend_quant(self, Q, cache, seq_len, workspace, draft_len=None, tree_mask=None, scale=None, k_scale=1.0, v_scale=1.0,
+                     cap=0.0, want_lse=False, out=None):
+        """``lagkv_attend_quant``: ``attend_tree`` over a ``QuantCache``; ``cap > 0``: logits x become cap * tanh(x / cap)."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        qc = self._check_quant(cache, False)
+        B = self.cfg.B
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(draft_len, "draft_len", (B,))
+        self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
+        out, lse = self._attend_out(Q, out, want_lse)
+        rc = self.lib.lagkv_attend_quant(
+            self.handle, ctypes.byref(q), cap, qc, _addr(Q), cache.K.shape[2], _addr(seq_len), _addr(draft_len), _addr(tree_mask),
+            _addr(out), _addr(lse), *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_attend_quant")
+        return {"out": out, "lse": lse} if want_lse else {"out": out}
+
+    def attend_quant_paged(self, Q, cache, block_table, seq_len, workspace, draft_len=None, tree_mask=None, scale=None, k_scale=1.0,
+                           v_scale=1.0, cap=0.0, want_lse=False, out=None):
+        """``lagkv_attend_quant_paged``: the same over pools of pages."""
+        q = self._query(Q, scale, k_scale, v_scale)
+        qc = self._check_quant(cache, True)
+        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        B = self.cfg.B
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(draft_len, "draft_len", (B,))
+        self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
+        out, lse = self._attend_out(Q, out, want_lse)
+        rc = self.lib.lagkv_attend_quant_paged(
+            self.handle, ctypes.byref(q), cap, qc, _addr(Q), ctypes.byref(lay), pages, _addr(seq_len), _addr(draft_len), _addr(tree_mask),
+            _addr(out), _addr(lse), *self._ws(workspace), _raw_stream(self.device))
+        _check(rc, "lagkv_attend_quant_paged")
+        return {"out": out, "lse": lse} if want_lse else {"out": out}
 
     # ---- pages
     def new_pages_workspace(self, num_pages: int) -> torch.Tensor:

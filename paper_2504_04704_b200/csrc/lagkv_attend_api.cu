@@ -4,8 +4,8 @@
 #include <cmath>
 #include <cstring>
 #include <cuda.h>
-#include <limits>
 
+#include "lagkv_attend_host.h"
 #include "lagkv_attend_tables.h"
 #include "lagkv_block_kernels.cuh"
 #include "lagkv_plan.h"
@@ -42,18 +42,11 @@ const AttendEntry* find_attend(int D, int dtype, int rows_wanted, bool blocks, i
 
 // Workspace: [status block | partials | who shares which unit | block choice].  Only the status block outlasts
 // a call.
-constexpr size_t kHead = kStatusWords * sizeof(int32_t);
-size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
-
 size_t partial_bytes(const lagkv_plan_s* plan, const AttendEntry& e) {
     return up256(size_t(plan->sm_count) * e.ctas_per_sm * 2 * e.partial_words * sizeof(float));
 }
 long long attend_units(const lagkv_plan_s* plan, const AttendEntry& e, int query_rows, int tokens) {
     return (long long)plan->cfg.B * plan->cfg.H_kv * tokens * ((query_rows + e.rows - 1) / e.rows);
-}
-// T tokens of G query heads per KV head are well formed
-bool query_shape_ok(const lagkv_config& c, int T, int H_q) {
-    return T >= 1 && T <= 64 && H_q >= c.H_kv && H_q % c.H_kv == 0 && H_q / c.H_kv <= 64;
 }
 // The choice of blocks: [chosen | 64-bit scores | 32-bit scores | how far these can be off]
 struct ChoiceLayout {
@@ -78,72 +71,7 @@ const void* score_kernel(int D) {
                       : reinterpret_cast<const void*>(&lagkv_block_score_kernel<DT, 256>);
 }
 
-int fill_query(const lagkv_plan_s* plan, const lagkv_query* q, const void* Q, void* out, float* lse, AttendParams* P) {
-    const lagkv_config& c = plan->cfg;
-    if (q == nullptr || Q == nullptr || out == nullptr || c.device < 0) return LAGKV_EINVAL;
-    if (!query_shape_ok(c, q->T, q->H_q)) return LAGKV_EINVAL;
-    if (!aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || Q == out) return LAGKV_EINVAL;
-    const double scale = q->scale == 0.0 ? 1.0 / std::sqrt(double(c.D)) : q->scale;
-    const double ks = q->k_scale == 0.0 ? 1.0 : q->k_scale, vs = q->v_scale == 0.0 ? 1.0 : q->v_scale;
-    // 0 would make NaN of the -infinity of hidden rows
-    const float scale_log2 = std::fmax(float(scale * ks * 1.4426950408889634), std::numeric_limits<float>::denorm_min());
-    if (!(scale > 0.0) || !(ks > 0.0) || !(vs > 0.0) || !std::isfinite(scale_log2) || !std::isfinite(float(vs))) return LAGKV_EINVAL;
-    const int64_t sh = q->stride_h ? q->stride_h : c.D;
-    const int64_t st = q->stride_t ? q->stride_t : (int64_t)q->H_q * sh;
-    const int64_t sb = q->stride_b ? q->stride_b : (int64_t)q->T * st;
-    if (sh < 0 || st < 0 || sb < 0 || sh % 8 || st % 8 || sb % 8) return LAGKV_EINVAL;
-    std::memset(P, 0, sizeof *P);
-    P->Q = static_cast<const uint16_t*>(Q);
-    P->out = static_cast<uint16_t*>(out);
-    P->lse = lse;
-    P->q_sb = sb;
-    P->q_st = st;
-    P->q_sh = sh;
-    P->B = c.B;
-    P->H = c.H_kv;
-    P->G = q->H_q / c.H_kv;
-    P->T = q->T;
-    P->scale_log2 = scale_log2;
-    P->v_scale = float(vs);
-    return LAGKV_OK;
-}
-
 constexpr int kMaxKeep = 4096, kMaxBlocks = 24576;  // the choice holds a unit's keys in shared memory
-
-// The cache of a call: contiguous (layout == nullptr) or paged.
-int fill_cache(const lagkv_plan_s* plan, const void* K, const void* V, int64_t S_cap, const lagkv_paged_layout* layout,
-               int64_t num_pages, AttendParams* P) {
-    const lagkv_config& c = plan->cfg;
-    if (K == nullptr || !aligned16(K) || !aligned16(V)) return LAGKV_EINVAL;
-    Strides st;
-    if (layout != nullptr) {
-        if (layout->page_size < 1 || layout->max_blocks < 1 || num_pages < 1) return LAGKV_EINVAL;
-        S_cap = (int64_t)layout->max_blocks * layout->page_size;
-    }
-    if (S_cap < 1 || S_cap > 0x7fffffffll - 65536) return LAGKV_EINVAL;
-    if (layout != nullptr) {
-        if (resolve_paged(c, layout, S_cap, &st) != LAGKV_OK) return LAGKV_EINVAL;
-    } else if (resolve_strides(c, S_cap, &st) != LAGKV_OK) {
-        return LAGKV_EINVAL;
-    }
-    P->K = static_cast<const uint8_t*>(K);
-    P->V = static_cast<const uint8_t*>(V);
-    P->S_cap = int(S_cap);
-    P->sb = st.sb * 2;
-    P->sh = st.sh * 2;
-    P->ss = st.ss * 2;
-    P->page_stride = st.page_stride * 2;
-    P->block_table = st.block_table;
-    P->max_blocks = st.max_blocks;
-    P->page_shift = st.page_shift;
-    P->num_pages = num_pages;
-    return LAGKV_OK;
-}
-
-int workspace_ok(const void* workspace, size_t bytes, size_t need) {
-    if (workspace == nullptr || bytes < need) return LAGKV_EWORKSPACE;
-    return (reinterpret_cast<uintptr_t>(workspace) & 255u) ? LAGKV_EINVAL : LAGKV_OK;
-}
 
 // The query rows that find_attend() is asked for.
 // Small caches: units of 16 rows start faster and more CTAs take part; reading K and V for each of them costs little out of
@@ -228,13 +156,6 @@ int cache_map(const lagkv_config& c, const AttendParams& P, const uint8_t* base,
     return r == CUDA_SUCCESS ? LAGKV_OK : LAGKV_EUNSUPPORTED;  // strides of 2^40 bytes and more
 }
 
-// Behind an attention kernel: the kernel that joins the units which several CTAs share.
-int launch_join(const AttendEntry& e, AttendParams& P, int query_rows, long long units, cudaStream_t stream) {
-    const int rows = e.rows < query_rows ? e.rows : query_rows;
-    void* args[] = {&P};
-    return launch_behind(e.join, unsigned(units * ((rows + e.join_rows - 1) / e.join_rows)), e.join_threads, args, 0, stream);
-}
-
 int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cudaStream_t stream) {
     CUtensorMap map_k, map_v;
     if (e.wide) {
@@ -246,7 +167,7 @@ int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cuda
     if (cudaLaunchKernel(e.fn, dim3((unsigned)P.ctas), dim3(e.threads), args, e.smem, stream) !=
         cudaSuccess)
         return LAGKV_ECUDA;
-    const int rc = launch_join(e, P, P.T * P.G, (long long)P.B * P.H * P.mtiles, stream);
+    const int rc = launch_join(e, &P, P.T * P.G, (long long)P.B * P.H * P.mtiles, stream);
     if (rc != LAGKV_OK) return rc;
     return check_launch();
 }
@@ -297,8 +218,6 @@ int tree_commit(lagkv_plan_t plan, void* K, void* V, int64_t S_cap, const lagkv_
         P, static_cast<uint8_t*>(K), static_cast<uint8_t*>(V), int(row_bytes(plan->cfg) / 16), seq_len, accepted, n_accepted);
     return check_launch();
 }
-
-int block_shift_of(int rows) { return rows == 16 ? 4 : rows == 32 ? 5 : rows == 64 ? 6 : rows == 128 ? 7 : -1; }
 
 int block_bounds(lagkv_plan_t plan, const void* K, int64_t S_cap, const lagkv_paged_layout* layout, int64_t num_pages,
                  const int32_t* from_len, const int32_t* seq_len, int32_t block_rows, void* bounds, int64_t blocks,
@@ -402,7 +321,7 @@ int attend_blocks(lagkv_plan_t plan, const lagkv_query* query, const lagkv_block
     P.idx = idx;
     void* args[] = {&P};
     rc = launch_behind(e->fn, unsigned(P.ctas), unsigned(e->threads), args, e->smem, stream);
-    if (rc == LAGKV_OK) rc = launch_join(*e, P, P.G, units * P.mtiles, stream);
+    if (rc == LAGKV_OK) rc = launch_join(*e, &P, P.G, units * P.mtiles, stream);
     return rc == LAGKV_OK ? check_launch() : rc;
 }
 

@@ -715,10 +715,9 @@ lagkv_attend_kernel(const __grid_constant__ AttendParams P) {
 // 32 partials worked out first, one per lane, so that their reads do not wait for one another.  (The last CTA to
 // arrive joined them at first: a CTA and 37 partials of 16 rows took 20 us.)
 constexpr int kMergeWarps = 4;
-template <int D, int DT, int MT>
-__global__ void __launch_bounds__(kMergeWarps * 32, 4)  // without the 4: 32 registers, hardly a read in flight, 1-3 us more
-lagkv_attend_merge_kernel(const __grid_constant__ AttendParams P) {
-    constexpr int MR = AttendGeo<D, DT, MT>::MR, PSIZE = MR * (D + 2);
+template <int D, int MR, class Write>
+__device__ __forceinline__ void attend_merge(const AttendParams& P, Write&& write) {
+    constexpr int PSIZE = MR * (D + 2);
     constexpr int LANES = D / 4 < 32 ? D / 4 : 32;     // lanes of a row
     constexpr int SPLIT = D == 64 ? 2 : 1;             // partials at a time
     constexpr int N = D / LANES, BATCH = 8;            // channels of a lane, reads in flight
@@ -783,7 +782,14 @@ lagkv_attend_merge_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] += __shfl_xor_sync(~0u, o[i], 16);
     }
-    if (part == 0) attend_write<D, DT>(P, b, h, t0, m0, seq.tokens, m, d, o, top, total);
+    if (part == 0) write(b, h, t0, m0, seq.tokens, m, d, o, top, total);
+}
+template <int D, int DT, int MT>
+__global__ void __launch_bounds__(kMergeWarps * 32, 4)  // without the 4: 32 registers, hardly a read in flight, 1-3 us more
+lagkv_attend_merge_kernel(const __grid_constant__ AttendParams P) {
+    attend_merge<D, AttendGeo<D, DT, MT>::MR>(P, [&](int b, int h, int t0, int m0, int tokens, int m, int d, const auto& o, float top, float total) {
+        attend_write<D, DT>(P, b, h, t0, m0, tokens, m, d, o, top, total);
+    });
 }
 
 }  // namespace lagkv
