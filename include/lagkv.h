@@ -497,7 +497,7 @@ typedef struct {
  *     e4m3:  f = max(the least power of two with a <= 448*f, 2^-126); code = the nearest e4m3 to x/s
  * (f = 0 where a = 0).  A block that begins at or behind from_len[b] gets s = f.  One that holds older rows gets
  * s = max(f, its scale); where that is larger the older codes become code*(old scale)/s, rounded again.  The codes are those of
- * exact quotients (e4m3: for scales that are powers of two).  Other blocks, and rows behind seq_len[b], stay as they are.
+ * exact quotients.  Other blocks, and rows behind seq_len[b], stay as they are.
  * Values that are not finite: LAGKV_EINVAL is recorded; they do not count in a, infinities become the largest code, NaN 0.
  * Refused (LAGKV_EINVAL recorded, the sequence untouched): lengths outside 0 <= from_len <= seq_len <= S_cap, more new
  * rows than T (take_rows), positions behind T with at_positions.  A take entry outside [0, T): recorded, that row is 0.

@@ -91,6 +91,14 @@ __device__ __forceinline__ float quant_fit(float top) {
     return fmaxf(f, 0x1p-126f);
 }
 
+// a / b as an fp32 value that rounds to fewer bits as the exact quotient does: what fp32 does not hold is rounded to odd.
+// a: up to 35 bits, b: 24; their 64-bit quotient is exact, or is as far from borders of fewer bits as the exact one.
+__device__ __forceinline__ float odd_quotient(double a, float b) {
+    const double q = a / b;
+    const float f = __double2float_rz(q);
+    return double(f) == q ? f : __int_as_float(__float_as_int(f) | 1);
+}
+
 // Eight codes of x / s.
 template <int FORM>
 __device__ __forceinline__ uint2 quant_encode(const float (&x)[8], float s, float inv) {
@@ -98,6 +106,10 @@ __device__ __forceinline__ uint2 quant_encode(const float (&x)[8], float s, floa
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
+        if (__float_as_int(s) & 0x7fffff) {  // no power of two: not a scale from here
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = odd_quotient(x[i], s);
+        }
         return make_uint2(pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7]));
     }
     constexpr float kMagic = 12582912.f;  // 1.5 * 2^23: the sum's low byte is the whole number
@@ -137,8 +149,9 @@ __device__ __forceinline__ uint4 quant_again(const uint4& v, float was, float no
         } else {
             uint32_t p[2];
             Elem<2>::expand(w[i], p);
-            const float f = was / now;
-            y[i] = pack_e4m3(Elem<1>::lo(p[0]) * f, Elem<1>::hi(p[0]) * f, Elem<1>::lo(p[1]) * f, Elem<1>::hi(p[1]) * f);
+            const double f = was;  // codes of 4 bits, scales of 24
+            y[i] = pack_e4m3(odd_quotient(Elem<1>::lo(p[0]) * f, now), odd_quotient(Elem<1>::hi(p[0]) * f, now),
+                             odd_quotient(Elem<1>::lo(p[1]) * f, now), odd_quotient(Elem<1>::hi(p[1]) * f, now));
         }
     }
     return make_uint4(y[0], y[1], y[2], y[3]);
