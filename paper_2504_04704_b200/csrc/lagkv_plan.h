@@ -33,7 +33,7 @@ struct lagkv_plan_s {
     int app_pair_splits;     // row splits per tensor: the cluster has twice as many CTAs
     bool app_tuned;   // lagkv_plan_tune() fixed the uniform append shape: no pair kernel
     std::atomic<unsigned long long> attend_ready{0};  // attention kernels whose shared memory limit is raised
-    std::atomic<unsigned long long> quant_ready{0};   // the same for caches in 8 bits with scales
+    std::atomic<unsigned long long> quant_ready{0}, write_ready{0};  // the same for caches in 8 bits with scales
     // lagkv_compress_prefill_host(): three streams and the events between them, made on first use
     std::mutex host_mu;
     bool host_ready = false;

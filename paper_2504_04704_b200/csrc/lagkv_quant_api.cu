@@ -80,17 +80,22 @@ int fill_quant(const lagkv_plan_s* plan, const lagkv_quant_cache* q, int64_t S_c
     P->r_sb = sb;
     P->r_sh = sh;
     P->r_st = st;
-    P->by_cpr = (65536u + c.D / 8 - 1) / (c.D / 8);
     return LAGKV_OK;
 }
 
+struct WriteKernel {
+    const void* fn;
+    size_t smem;
+};
+template <int DT, int FORM, int GT>
+WriteKernel write_kernel() { return {reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, GT>), size_t(QuantWriteGeo<GT>::SMEM)}; }
 template <int DT, int FORM>
-const void* write_kernel(int threads) {
-    return threads == 32    ? reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, 32>)
-           : threads == 64  ? reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, 64>)
-           : threads == 128 ? reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, 128>)
-           : threads == 256 ? reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, 256>)
-                            : reinterpret_cast<const void*>(&lagkv_quant_write_kernel<DT, FORM, 512>);
+WriteKernel write_kernel(int threads) {
+    return threads == 32    ? write_kernel<DT, FORM, 32>()
+           : threads == 64  ? write_kernel<DT, FORM, 64>()
+           : threads == 128 ? write_kernel<DT, FORM, 128>()
+           : threads == 256 ? write_kernel<DT, FORM, 256>()
+                            : write_kernel<DT, FORM, 512>();
 }
 
 int quant_write(lagkv_plan_t plan, const lagkv_quant_cache* cache, int64_t S_cap, const lagkv_paged_layout* layout, int64_t num_pages,
@@ -119,20 +124,25 @@ int quant_write(lagkv_plan_t plan, const lagkv_quant_cache* cache, int64_t S_cap
     const long long all = ((long long)P.S_cap - 1) / R + 1;
     if (most > all) most = all;
     int threads = 32;
-    while (threads * kQuantPieces < rows * (c.D / 8)) threads *= 2;
+    while (threads / (c.D / 8) * kQuantPieces < rows) threads *= 2;
     const int groups = threads >= 256 ? 1 : 256 / threads;
-    // groups per (sequence, head, tensor): 32 CTAs an SM even ragged lengths out
-    const long long units = 2ll * c.B * c.H_kv, want = 32ll * plan->sm_count * groups;
+    // groups per (sequence, head, tensor): 16 CTAs an SM even ragged lengths out
+    const long long units = 2ll * c.B * c.H_kv, want = 16ll * plan->sm_count * groups;
     long long per = (want + units - 1) / units;
     if (per > most) per = most;
-    if ((units * per + groups - 1) / groups > 0x7fffffffll) return LAGKV_EINVAL;
+    if (units * per > 0x7fffffffll) return LAGKV_EINVAL;
     P.per = int(per);
     const bool bf16 = c.dtype == LAGKV_DTYPE_BF16, int8 = cache->format == LAGKV_QUANT_INT8;
-    const void* fn = bf16 ? (int8 ? write_kernel<0, FORM_INT8>(threads) : write_kernel<0, FORM_E4M3>(threads))
-                          : (int8 ? write_kernel<1, FORM_INT8>(threads) : write_kernel<1, FORM_E4M3>(threads));
+    const WriteKernel w = bf16 ? (int8 ? write_kernel<0, FORM_INT8>(threads) : write_kernel<0, FORM_E4M3>(threads))
+                               : (int8 ? write_kernel<1, FORM_INT8>(threads) : write_kernel<1, FORM_E4M3>(threads));
     DeviceGuard guard(c.device);
+    const unsigned long long ready = 1ull << ((bf16 ? 0 : 8) + (int8 ? 0 : 16) + (threads >= 512 ? 4 : threads >> 6 > 2 ? 3 : threads >> 6));
+    if (!(plan->write_ready.load(std::memory_order_acquire) & ready)) {
+        if (!raise_smem_limit(w.fn, w.smem)) return LAGKV_ECUDA;
+        plan->write_ready.fetch_or(ready, std::memory_order_release);
+    }
     void* args[] = {&P};
-    if (cudaLaunchKernel(fn, dim3(unsigned((units * per + groups - 1) / groups)), dim3(threads > 256 ? threads : 256), args, 0,
+    if (cudaLaunchKernel(w.fn, dim3(unsigned((units * per + groups - 1) / groups)), dim3(threads > 256 ? threads : 256), args, w.smem,
                          static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess)
         return LAGKV_ECUDA;
     return check_launch();
@@ -155,11 +165,12 @@ int quant_read(lagkv_plan_t plan, const lagkv_quant_cache* cache, int64_t S_cap,
     P.rows[1] = static_cast<uint16_t*>(V_out);
     P.take = idx;
     P.n = int(rows_out);
-    const long long units = 2ll * c.B * c.H_kv, want = 32ll * plan->sm_count;
-    const long long longest = idx ? rows_out : P.S_cap < rows_out ? P.S_cap : rows_out;
-    const long long most = (longest * (c.D / 16) + kReadThreads * kReadPieces - 1) / (kReadThreads * kReadPieces);
+    // CTAs per (sequence, head, tensor): many for whole caches, so that ragged lengths even out; few behind from_len, where most
+    // sequences of a decode step have a block to read (32 x 8 heads: 8 us against 18)
+    const long long units = 2ll * c.B * c.H_kv, want = (from_len ? 8ll : 48ll) * plan->sm_count;
+    const long long longest = idx ? rows_out : P.S_cap < rows_out ? P.S_cap : rows_out, rows = kReadThreads / (c.D / 8) * kReadPieces;
     long long per = (want + units - 1) / units;
-    if (per > most) per = most;
+    if (per > (longest + rows - 1) / rows) per = (longest + rows - 1) / rows;
     if (units * per > 0x7fffffffll) return LAGKV_EINVAL;
     P.per = int(per);
     const bool bf16 = c.dtype == LAGKV_DTYPE_BF16, int8 = cache->format == LAGKV_QUANT_INT8;
