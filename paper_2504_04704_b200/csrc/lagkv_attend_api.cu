@@ -124,38 +124,6 @@ int attend_prepare(lagkv_plan_t plan, int query_rows, int tokens, bool blocks, s
     }
     return LAGKV_OK;
 }
-typedef CUresult (*encode_tiled_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-encode_tiled_t encode_tiled() {
-    static const encode_tiled_t fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<encode_tiled_t>(p);
-    }();
-    return fn;
-}
-// Tensor map of one cache tensor for the wide kernel: (channels, rows, heads, sequences or pages), boxes of
-// 64 channels in 128-byte swizzled rows (fp8: whole rows as they are) and of a tile's rows, or a page's if fewer.
-int cache_map(const lagkv_config& c, const AttendParams& P, const uint8_t* base, CUtensorMap* map) {
-    const bool fp8 = c.dtype == LAGKV_DTYPE_FP8_E4M3, paged = P.block_table != nullptr;
-    const cuuint64_t rows = paged ? 1ull << P.page_shift : (cuuint64_t)P.S_cap;
-    const cuuint64_t dims[4] = {(cuuint64_t)c.D, rows, (cuuint64_t)c.H_kv, paged ? (cuuint64_t)P.num_pages : (cuuint64_t)c.B};
-    const cuuint64_t strides[3] = {(cuuint64_t)P.ss, (cuuint64_t)P.sh, (cuuint64_t)(paged ? P.page_stride : P.sb)};
-    const cuuint32_t box[4] = {fp8 ? (cuuint32_t)c.D : 64u, (cuuint32_t)(paged && rows < kWideTile ? rows : kWideTile), 1u, 1u};
-    const cuuint32_t ones[4] = {1u, 1u, 1u, 1u};
-    const CUtensorMapDataType type = fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    const encode_tiled_t encode = encode_tiled();
-    if (encode == nullptr) return LAGKV_ECUDA;
-    const CUresult r = encode(map, type, 4, const_cast<uint8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? LAGKV_OK : LAGKV_EUNSUPPORTED;  // strides of 2^40 bytes and more
-}
-
 int attend_launch(lagkv_plan_t plan, const AttendEntry& e, AttendParams& P, cudaStream_t stream) {
     CUtensorMap map_k, map_v;
     if (e.wide) {

@@ -135,6 +135,16 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {  // an 8 x 8 matrix
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
+// tanh without a branch (the instructions on tensor memory need warps that are together), off by 2^-22 at most: below 3/8 the
+// series y - y^3 / 3 + 2 y^5 / 15 - 17 y^7 / 315 + 62 y^9 / 2835 (2^-20.9 of tanh y at 3/8, less below), above it 1 - 2 / (1 + e^2y), where
+// 2^-22 of e^2y count for less than half and the reciprocal for 2^-23.
+__device__ __forceinline__ float quant_tanh(float y) {
+    const float a = fabsf(y), q = y * y;
+    const float low = y * fmaf(q, fmaf(q, fmaf(q, fmaf(q, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(a * 2.885390081777927f)));
+    return a < 0.375f ? low : copysignf(fmaf(-2.f, r, 1.f), y);
+}
 __device__ __forceinline__ float pow2_of(int e) { return __int_as_float((e + 127) << 23); }  // -126 <= e <= 127
 
 // The factor that brings a row of bf16 queries with largest magnitude `top` to [2^8, 2^9); 1 where there is none.
@@ -351,7 +361,7 @@ lagkv_attend_quant_kernel(const __grid_constant__ QuantAttendParams P) {
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[m][n][e] = P.cap_log2 * tanhf(s[m][n][e] * P.cap_inv);
+                        for (int e = 0; e < 4; ++e) s[m][n][e] = P.cap_log2 * quant_tanh(s[m][n][e] * P.cap_inv);
             }
             if (hidden) {
 #pragma unroll

@@ -34,6 +34,7 @@ constexpr int kWideRowFlags = 32;     // loads whose missing rows are remembered
 template <int D_, int DT_, int MT_>
 struct WideGeo {
     static constexpr int D = D_, DT = DT_, MT = MT_;  // MT = 1: streams split the rows, 2: the query rows
+    static constexpr bool NAN_ROWS = true;             // rows may hold values that are not finite
     static constexpr int EB = Elem<DT_>::EB;
     static constexpr int ROWB = D * EB, CPR = ROWB / 16;
     static constexpr int PANELS = (D + 63) / 64;       // 64 channels of 16 bits: 128-byte rows, swizzled
@@ -49,9 +50,9 @@ struct WideGeo {
     static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
-    // ... and how many are in flight.  There are 3 slots with 3 of them and with 4 at 128 channels; 3 are a little quicker:
-    // 126.1 us against 127.5 for 8 x 8 x 19968 rows under 13 tokens.
-    static constexpr int RS = DT_ == 2 ? (MT_ == 1 && D_ > 64 ? 3 : 4) : 0;
+    // ... and how many are in flight: one for each group of helpers.  A place that groups took in turns could be waited for by
+    // a group one lap ahead of a copy that is late, and a parity does not tell that lap from the one before.
+    static constexpr int RS = DT_ == 2 ? GROUPS : 0;
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
     static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
     static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
@@ -223,7 +224,8 @@ __device__ __forceinline__ float largest_of(const uint4& v) {
 // The queries of a unit into swizzled shared memory (`to`), 32 rows at a time by warp `warp` of `warps`: a lane
 // finds its row's place once, all lanes copy.
 template <class G>
-__device__ __forceinline__ void load_queries(const AttendParams& P, const WideUnit& U, int b, unsigned char* to, int warp, int warps) {
+__device__ __forceinline__ void load_queries(const AttendParams& P, const WideUnit& U, int b, unsigned char* to, int warp, int warps,
+                                             bool copy = G::DT != 2) {
     constexpr int D = G::D, CH = D / 8;  // 16-byte pieces of a row
     const int lane = threadIdx.x & 31;
     const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)(U.h * P.G) * P.q_sh;
@@ -234,7 +236,7 @@ __device__ __forceinline__ void load_queries(const AttendParams& P, const WideUn
     for (int r0 = warp * 32; r0 < G::MT * kWideTile; r0 += warps * 32) {
         const int row = U.m0 + r0 + lane;
         const long long off = r0 + lane < U.mrows ? (long long)(row / P.G) * P.q_st + (long long)(row % P.G) * P.q_sh : -1;
-        if constexpr (G::DT != 2) {
+        if (copy) {
 #pragma unroll 4
             for (int k = 0; k < CH; ++k) {
                 const int id = k * 32 + lane, r = r0 + id / CH, ch = id % CH;
@@ -295,7 +297,7 @@ struct WideCursor {
     // a V tile with rows that enter as zeros, or that may
     __device__ __forceinline__ bool mend(uint32_t missing) const { return missing || careful() || row0() + kWideTile > U.lim; }
     // drafted V rows that are not finite are kept out of the tile
-    __device__ __forceinline__ bool careful() const { return U.masked && is_v() && row0() + kWideTile > U.base; }
+    __device__ __forceinline__ bool careful() const { return G::NAN_ROWS && U.masked && is_v() && row0() + kWideTile > U.base; }
 };
 
 template <int D, int DT, int MT>
@@ -920,10 +922,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
 // Joins the partials of shared units in the order of their rows: a CTA per 32 query rows of a unit, a lane
 // per row, a warp per eighth of the channels.
 constexpr int kJoinRows = 32, kJoinThreads = 256;
-template <int D, int DT, int MT>
-__global__ void __launch_bounds__(kJoinThreads)
-lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
-    constexpr int N = D / 8, PSIZE = WideGeo<D, DT, MT>::PSIZE;
+template <int D, int MT, class Write>
+__device__ __forceinline__ void attend_join(const AttendParams& P, Write&& write) {
+    constexpr int N = D / 8, PSIZE = MT * kWideTile * (D + 2);
     const int upb = P.H * P.mtiles, chunks = (min(MT * kWideTile, P.T * P.G) + kJoinRows - 1) / kJoinRows, chunk = blockIdx.x % chunks;
     const long long unit = blockIdx.x / chunks;
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials
@@ -963,8 +964,15 @@ lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
 #pragma unroll
     for (int d = 0; d < N; d += 4) {
         const float x[4] = {o[d], o[d + 1], o[d + 2], o[d + 3]};
-        attend_write<D, DT>(P, b, h, 0, m0, seq.tokens, mu, d0 + d, x, top, total);
+        write(b, h, m0, seq.tokens, mu, d0 + d, x, top, total);
     }
+}
+template <int D, int DT, int MT>
+__global__ void __launch_bounds__(kJoinThreads)
+lagkv_attend_join_kernel(const __grid_constant__ AttendParams P) {
+    attend_join<D, MT>(P, [&](int b, int h, int m0, int tokens, int m, int d, const auto& o, float top, float total) {
+        attend_write<D, DT>(P, b, h, 0, m0, tokens, m, d, o, top, total);
+    });
 }
 
 }  // namespace lagkv

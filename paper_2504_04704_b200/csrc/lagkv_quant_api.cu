@@ -3,6 +3,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <cuda.h>
 
 #include "lagkv_attend_host.h"
 #include "lagkv_attend_quant_tables.h"
@@ -246,14 +247,24 @@ int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const 
     P.mtiles = (query_rows + e->rows - 1) / e->rows;
     P.ctas = plan->sm_count * e->ctas_per_sm;
     P.per_units = 1.f / (16.f * float(units));
-    P.lead = kAttendLead;
+    P.least = int(std::ceil(std::sqrt((P.S_cap / double(kWideTile) + kWideLead) / 6.0)));  // as for other caches
+    if (P.least > 4) P.least = 4;
+    P.lead = e->wide ? kWideLead : kAttendLead;
     DeviceGuard guard(plan->cfg.device);
     if (!(plan->quant_ready.load(std::memory_order_acquire) >> index & 1)) {
         if (!raise_smem_limit(e->fn, e->smem)) return LAGKV_ECUDA;
         plan->quant_ready.fetch_or(1ull << index, std::memory_order_release);
     }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    void* args[] = {&P};
+    CUtensorMap map_k, map_v;
+    if (e->wide) {
+        lagkv_config codes = plan->cfg;
+        codes.dtype = LAGKV_DTYPE_FP8_E4M3;
+        rc = cache_map(codes, P, P.K, &map_k);
+        if (rc == LAGKV_OK) rc = cache_map(codes, P, P.V, &map_v);
+        if (rc != LAGKV_OK) return rc;
+    }
+    void* args[] = {&P, &map_k, &map_v};
     if (cudaLaunchKernel(e->fn, dim3((unsigned)P.ctas), dim3(e->threads), args, e->smem, stream) != cudaSuccess) return LAGKV_ECUDA;
     rc = launch_join(*e, &P, query_rows, units, stream);
     return rc == LAGKV_OK ? check_launch() : rc;
@@ -293,19 +304,16 @@ int lagkv_quant_read_paged(lagkv_plan_t plan, const lagkv_quant_cache* cache, co
 
 size_t lagkv_attend_quant_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t H_q) {
     if (plan == nullptr || !query_shape_ok(plan->cfg, T, H_q)) return 0;
-    // every smaller call, in either format: fewer query rows may take smaller units, and more of them never
-    size_t partials = 0, units = 0;
+    // every smaller call, in either format, and whichever unit it takes
+    size_t partials = 0;
     const int rows_all = T * (H_q / plan->cfg.H_kv);
     for (int format : {LAGKV_QUANT_INT8, LAGKV_QUANT_E4M3})
-        for (int rows : {1, 9, 17, rows_all}) {
-            if (rows > rows_all) continue;
+        for (int rows : {1, 9, 17, 33, 129}) {
             int index;
-            const AttendEntry* e = find_quant(plan->cfg.D, format, rows, &index);
-            if (e == nullptr) return 0;
-            const size_t need = partial_bytes(plan, *e), n = size_t(quant_units(plan->cfg, *e, rows_all));
-            if (need > partials) partials = need;
-            if (n > units) units = n;
+            const AttendEntry* e = rows > 1 && rows > rows_all ? nullptr : find_quant(plan->cfg.D, format, rows, &index);
+            if (e != nullptr && partial_bytes(plan, *e) > partials) partials = partial_bytes(plan, *e);
         }
+    const size_t units = size_t(plan->cfg.B) * plan->cfg.H_kv * ((rows_all + 7) / 8);  // none has fewer rows
     return kHead + partials + up256(units * sizeof(int2));
 }
 

@@ -164,6 +164,15 @@ def test_capped_logits(binding, kind, T, G, cap):
     QU.assert_attention(run(c, cap=cap), reference(c, cap=cap))
 
 
+@pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("T,G,cap", [(5, 7, 30.0), (5, 7, 4.0), (64, 4, 10.0)])
+def test_capped_logits_of_every_head_dim(binding, kind, D, T, G, cap):
+    """Long ragged caches whose logits lie on both sides of the cap, within warps and among them."""
+    c = case(binding, kind, 2, 1, G, D, 5000, T, 32, seed=3, lens=[5000, 3777], spread=2.0)
+    QU.assert_attention(run(c, cap=cap), reference(c, cap=cap))
+
+
 @pytest.mark.parametrize("kind", KINDS[:2], ids=KIND_IDS[:2])
 @pytest.mark.parametrize("T,G", [(1, 4), (12, 4)])
 def test_factors_and_large_logits(binding, kind, T, G):
