@@ -1,14 +1,17 @@
 // Attention for many query rows over a cache held in 8 bits with block scales -- 5th-generation tensor cores.
 //
 // The shares of the work, the tiles by TMA, the helpers that widen them to fp16 in swizzled shared memory and the partials are those
-// of lagkv_attend_wide_kernel; the mathematics of the scales is that of lagkv_attend_quant_kernel.  What differs is the
-// softmax.  Each stream (four warps, a thread owns a query row) takes items of 64 rows of a tile and has two places for
+// of lagkv_attend_wide_kernel; the mathematics of the scales is that of lagkv_attend_quant_kernel.  What differs:
+// Each softmax stream (four warps, a thread owns a query row) takes items of 64 rows of a tile and has two places for
 // their scores in tensor memory, so that the scores of its next item are there when it comes to them:
 //     up to 128 query rows: stream s takes rows 64 s .. of every tile, both streams are joined at the end,
 //     up to 256:            stream s has its own 128 query rows and takes both halves of every tile.
-// 64 scores fit a thread's registers: one pass from scores to probabilities, and nothing spills with 512 threads.
-// Products wait for probabilities only, in the order of the items; a stream waits for the product of its item before when it hands
-// over the next, long after that has ended, or before it rescales O.
+// 64 scores fit a thread's registers, and nothing spills with 512 threads.  Products wait for probabilities only, in the order of the
+// items; a stream waits for the product of its item before when it hands over the next, long after that has ended, or
+// before it rescales O.
+// The roles' loops run side by side out of one instruction cache, and with 140 KB of code its misses set the pace.  So one
+// warp walks the share of the work and tells the others the units (WideTask), waits and loads of queries are out of line, and
+// what few items need (caps, hidden rows) is a rolled loop over tensor memory.
 #pragma once
 #include "lagkv_attend_quant_kernels.cuh"
 #include "lagkv_attend_wide_kernel.cuh"
@@ -28,7 +31,12 @@ struct WideCode : WideInt8 {};
 template <>
 struct WideCode<FORM_E4M3> : Elem<2> {};
 
-constexpr int kWideScales = 16;  // K tiles whose scales are kept: more than the rings hold
+constexpr int kWideTasks = 16;   // units that are announced: the loading warp is at most 8 ahead of the softmax
+
+// A unit's part of a CTA's share; n = 0: there is none left.
+struct WideTask {
+    int b, u, tile0, n, first_cta, last_cta, len, tokens;
+};
 
 template <int D_, int FORM_, int MT_>
 struct QuantWideGeo {
@@ -41,7 +49,8 @@ struct QuantWideGeo {
     static constexpr int GROUPS = MT == 2 && D > 64 ? 2 : 3, HELP = 64;  // groups of helpers, their threads
     static constexpr int WARPS = 10 + 2 * GROUPS, NT = WARPS * 32;
     static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
-    static constexpr int MISC = 1024 + kWideScales * 16 * 4;
+    static constexpr int SCALES = D == 64 ? 16 : 8;  // K tiles whose scales are kept: more than the rings hold
+    static constexpr int MISC = 1024 + kWideTasks * int(sizeof(WideTask)) + SCALES * 16 * 4;
     static constexpr int RAW = kWideTile * ROWB, RS = GROUPS;  // (see WideGeo)
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT, NS = NS_FIT > 8 ? 8 : NS_FIT;
     static constexpr int SMEM = 1024 + QBYTES + NS * SLOT + RS * RAW + MISC;
@@ -59,6 +68,12 @@ __device__ __forceinline__ void tm_ld16(uint32_t (&r)[16], uint32_t a) {  // wai
         : "memory");
 }
 
+// mbar_wait_bounded() of which only the first look is inline: the instruction cache holds little more than the roles' loops.
+static __device__ __noinline__ bool wide_wait_long(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
+__device__ __forceinline__ bool wide_wait(uint32_t bar, uint32_t parity) {
+    return __all_sync(~0u, mbar_try_wait(bar, parity)) || wide_wait_long(bar, parity);
+}
+
 template <int D, int N>
 __device__ __forceinline__ void quant_write_out(const QuantAttendParams& P, int b, int h, int m0, int tokens, int m, int d, const float (&o)[N],
                                                 float ref, float sum) {
@@ -66,6 +81,71 @@ __device__ __forceinline__ void quant_write_out(const QuantAttendParams& P, int 
         attend_write<D, 1>(P, b, h, 0, m0, tokens, m, d, o, ref, sum);
     else
         attend_write<D, 0>(P, b, h, 0, m0, tokens, m, d, o, ref, sum);
+}
+
+// A task as the roles see it.
+struct WideView {
+    int b, h, m0, mrows, tile0, n, lim, base;  // query rows from m0 on; rows seen at all, first drafted row
+    bool masked;
+};
+__device__ __forceinline__ WideView wide_view(const QuantAttendParams& P, const WideTask& k, int rows) {
+    WideView v;
+    v.b = k.b;
+    v.h = k.u / P.mtiles;
+    v.m0 = (k.u - v.h * P.mtiles) * rows;
+    v.mrows = min(rows, P.T * P.G - v.m0);
+    v.tile0 = k.tile0;
+    v.n = k.n;
+    v.lim = k.tokens == 0 ? 0 : k.len;
+    v.base = k.len - k.tokens;
+    v.masked = P.mask != nullptr || k.tokens > 1;
+    return v;
+}
+// Loads of a task: V of step i is load load_of_v(i, n), K load_of_k(i).
+template <int MT>
+__device__ __forceinline__ bool load_is_v(int l, int n) { return MT == 2 ? (l & 1) != 0 : l == 2 * n - 1 || (l >= 2 && !(l & 1)); }
+template <int MT>
+__device__ __forceinline__ int load_step(int l, int n) {
+    return MT == 2 ? l >> 1 : load_is_v<MT>(l, n) ? (l == 2 * n - 1 ? n - 1 : l / 2 - 1) : (l + 1) >> 1;
+}
+
+// The queries of a task into swizzled shared memory (`to`) and the exponents of the powers of two that their rows were scaled
+// with (`factors`), by warp `warp` of `warps`: 8 or 16 lanes a row, several rows in flight.
+template <class G>
+__device__ __noinline__ void quant_load_queries(const QuantAttendParams& P, const WideTask* task, unsigned char* to, uint8_t* factors, int warp, int warps) {
+    constexpr int CH = G::D / 8, LPR = CH > 8 ? 16 : 8, RPI = 32 / LPR, BATCH = 4;  // 16-byte pieces and lanes of a row, rows at a time, such steps in flight
+    const WideView U = wide_view(P, *task, G::MT * kWideTile);
+    const int lane = threadIdx.x & 31, ch = lane % LPR, sub = lane / LPR;
+    const uint32_t by_g = ((1u << 20) + P.G - 1) / P.G;  // rows / G by a product: rows < 2^12, G <= 2^6
+    const uint16_t* q0 = P.Q + (long long)U.b * P.q_sb + (long long)(U.h * P.G) * P.q_sh + ch * 8;
+#pragma unroll 1
+    for (int r0 = warp * RPI * BATCH; r0 < G::MT * kWideTile; r0 += warps * RPI * BATCH) {
+        uint4 v[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = r0 + k * RPI + sub, row = U.m0 + r, t = int(row * by_g >> 20);
+            v[k] = r < U.mrows && ch < CH ? __ldg(reinterpret_cast<const uint4*>(q0 + (long long)t * P.q_st + (long long)(row - t * P.G) * P.q_sh)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = r0 + k * RPI + sub;
+            float f = 1.f;
+            if (!P.half) {
+                float top = largest_of(v[k]);
+#pragma unroll
+                for (int o = LPR / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+                f = query_factor(top);
+                uint32_t y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = MmaHalf::pack(Elem<0>::lo(y[e]) * f, Elem<0>::hi(y[e]) * f);
+                v[k] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            if (ch == 0) factors[r] = uint8_t(__float_as_int(f) >> 23);
+            if (ch < CH) *reinterpret_cast<uint4*>(to + (r >> 7) * G::SLOT + (ch >> 3) * G::PANEL + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[k];
+        }
+    }
+    fence_proxy_async();
+    __syncwarp();
 }
 
 template <int D, int FORM, int MT>
@@ -83,15 +163,18 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
     unsigned char* misc = smem + (s_misc - sbase);
     float* exch = reinterpret_cast<float*>(smem + G::SLOT);  // MT = 1
     // misc: barriers (tile ready, place free; landed, its place free; scores and probabilities of both streams' two places,
-    // products of the streams; queries in place, their place free), the rows of each V tile that are not finite, the missing
-    // 16-row groups of each load, scheduling scratch, scales of K tiles' rows
+    // products of the streams; queries in place, their place free, the first ones in place; tasks told), the rows of each V tile
+    // that are NaN, the missing 16-row groups of each load, exponents of the queries' factors (scheduling scratch before), tasks,
+    // scales of K tiles' rows
     const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_land = b_empty + 8 * 8, b_raw_free = b_land + 4 * 8, b_s = b_raw_free + 4 * 8,
-                   b_p = b_s + 4 * 8, b_o = b_p + 4 * 8, b_q = b_o + 2 * 8, b_q_free = b_q + 8;
-    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 288);                     // [8][4]
-    volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 416);       // [kWideRowFlags]
-    long long* scan = reinterpret_cast<long long*>(misc + 544);                       // [16 + 2]
-    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 704);
-    float* tile_scales = reinterpret_cast<float*>(misc + 1024);                       // [kWideScales][K, V][8]
+                   b_p = b_s + 4 * 8, b_o = b_p + 4 * 8, b_q = b_o + 2 * 8, b_q_free = b_q + 8, b_q_first = b_q_free + 8, b_task = b_q_first + 8;
+    uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 432);                     // [8][4]
+    volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 560);       // [kWideRowFlags]
+    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(misc + 688);
+    uint8_t* q_factors = misc + 704;                                                  // [MT * 128]
+    long long* scan = reinterpret_cast<long long*>(misc + 704);                       // [16 + 2]
+    WideTask* tasks = reinterpret_cast<WideTask*>(misc + 1024);                       // [kWideTasks]
+    float* tile_scales = reinterpret_cast<float*>(misc + 1024 + kWideTasks * sizeof(WideTask));  // [SCALES][K, V][8]
     if (tid == 0) {
         for (int i = 0; i < G::NS; ++i) {
             mbar_init(b_full + 8 * i, 1);
@@ -108,6 +191,8 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
         for (int s = 0; s < 2; ++s) mbar_init(b_o + 8 * s, 1);
         mbar_init(b_q, 2 * G::GROUPS);
         mbar_init(b_q_free, 1);
+        mbar_init(b_q_first, 8 + 2 * G::GROUPS);
+        for (int i = 0; i < kWideTasks; ++i) mbar_init(b_task + 8 * i, 1);
         fence_mbar_init();
     }
     if (w == 8) {
@@ -117,9 +202,6 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
     }
     const int upb = P.H * P.mtiles;
     AttendShare sh = attend_share<G::NT, kWideTile>(P, upb, scan);
-    WideUnit U;
-    bool any = wide_first<G>(P, sh, U, upb);
-    if (any) load_queries<G>(P, U, sh.b, smem, w, G::WARPS, P.half != 0);  // the first unit's, by all
     __syncthreads();
     tm_fence_after();
     const uint32_t tm = __shfl_sync(~0u, *reinterpret_cast<volatile uint32_t*>(tm_slot), 0);
@@ -127,49 +209,84 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
     auto at_s = [&](int s, int p) { return tm + (MT == 1 ? p * 128 + s * 64 : s * 128 + p * 64); };
     auto at_o = [&](int s) { return tm + 256 + s * D; };
     bool ok = true;
+    // The task told in turn `k`, once it is; false: the last one is behind, or a wait was given up.
+    auto next_task = [&](uint32_t k, WideView& U) {
+        if (!ok || !wide_wait(b_task + 8 * (k % kWideTasks), k / kWideTasks & 1)) {
+            if (ok && lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+            return ok = false;
+        }
+        U = wide_view(P, tasks[k % kWideTasks], MT * kWideTile);
+        return U.n > 0;
+    };
 
     if (w == 9) {
         // ------------------------------------------------------------------ K and V tiles: a box per page, a lane each
         const int box_rows = P.block_table == nullptr ? kWideTile : min(kWideTile, 1 << P.page_shift);
         const uint32_t box_bytes = uint32_t(box_rows) * G::ROWB;
-        WideCursor<G> at;
-        at.start(sh, U, any);
-        uint32_t place = 0, lap = 0;
-        for (; at.more; at.next(P, upb)) {
-            const int row = at.row0() + lane * box_rows;
-            bool there = lane < kWideTile / box_rows && row < at.U.lim;
-            const bool wanted = there;
-            int c1 = row, c3 = at.sh.b;
-            if (there && P.block_table != nullptr) {
-                c3 = __ldg(P.block_table + (long long)at.sh.b * P.max_blocks + (row >> P.page_shift));
-                c1 = row & ((1 << P.page_shift) - 1);
-                if (c3 < 0 || c3 >= P.num_pages) {
-                    there = false;
-                    record_status(P.status, ST_EINVAL, at.sh.b);
-                }
+        uint32_t place = 0, lap = 0, c = 0;
+        for (uint32_t task = 0; ok; ++task) {
+            AttendSeq seq;
+            AttendPart part;
+            part.n = part.step = seq.tiles = 0;
+            while (sh.pos < sh.end) {  // the next unit with rows
+                seq = attend_seq<kWideTile>(P, sh.b, false);
+                part = attend_part(P, sh, seq.tiles);
+                if (part.n > 0) break;
+                attend_advance(P, sh, part.step, seq.tiles, upb);
             }
-            const int boxes = __popc(__ballot_sync(~0u, there));
-            uint32_t flags = 0;  // a bit per group of 16 rows whose page is not in the pool
-            for (unsigned m = __ballot_sync(~0u, wanted && !there); m; m &= m - 1)
-                flags |= ((1u << box_rows / 16) - 1) << (__ffs(int(m)) - 1) * box_rows / 16;
-            if (lap > 0 && !mbar_wait_bounded(b_raw_free + 8 * place, (lap + 1) & 1)) {
-                if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
-                ok = false;
-                break;
-            }
+            const int n = sh.pos < sh.end ? part.n : 0;
             if (lane == 0) {
-                gone[at.c % kWideRowFlags] = flags;
-                mbar_arrive_expect_tx(b_land + 8 * place, boxes * box_bytes);
+                WideTask& k = tasks[task % kWideTasks];
+                k.b = sh.b;
+                k.u = part.u;
+                k.tile0 = part.tile0;
+                k.n = n;
+                k.first_cta = int(part.c0);
+                k.last_cta = int(part.c1);
+                k.len = seq.len;
+                k.tokens = seq.tokens;
+                mbar_arrive(b_task + 8 * (task % kWideTasks));
             }
-            __syncwarp();
-            if (there)
-                asm volatile(
-                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-                        s_raw + place * G::RAW + lane * box_bytes),
-                    "l"(at.is_v() ? &map_v : &map_k), "r"(0), "r"(c1), "r"(at.U.h), "r"(c3), "r"(b_land + 8 * place)
-                    : "memory");
-            __syncwarp();
-            if (++place == uint32_t(G::RS)) place = 0, ++lap;
+            if (n == 0) break;
+            const int h = part.u / P.mtiles, lim = seq.tokens == 0 ? 0 : seq.len;
+            for (int l = 0; l < 2 * n && ok; ++l, ++c) {
+                const bool is_v = load_is_v<MT>(l, n);
+                const int row = (part.tile0 + load_step<MT>(l, n)) * kWideTile + lane * box_rows;
+                bool there = lane < kWideTile / box_rows && row < lim;
+                const bool wanted = there;
+                int c1 = row, c3 = sh.b;
+                if (there && P.block_table != nullptr) {
+                    c3 = __ldg(P.block_table + (long long)sh.b * P.max_blocks + (row >> P.page_shift));
+                    c1 = row & ((1 << P.page_shift) - 1);
+                    if (c3 < 0 || c3 >= P.num_pages) {
+                        there = false;
+                        record_status(P.status, ST_EINVAL, sh.b);
+                    }
+                }
+                const int boxes = __popc(__ballot_sync(~0u, there));
+                uint32_t flags = 0;  // a bit per group of 16 rows whose page is not in the pool
+                for (unsigned m = __ballot_sync(~0u, wanted && !there); m; m &= m - 1)
+                    flags |= ((1u << box_rows / 16) - 1) << (__ffs(int(m)) - 1) * box_rows / 16;
+                if (lap > 0 && !wide_wait(b_raw_free + 8 * place, (lap + 1) & 1)) {
+                    if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+                    ok = false;
+                    break;
+                }
+                if (lane == 0) {
+                    gone[c % kWideRowFlags] = flags;
+                    mbar_arrive_expect_tx(b_land + 8 * place, boxes * box_bytes);
+                }
+                __syncwarp();
+                if (there)
+                    asm volatile(
+                        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+                            s_raw + place * G::RAW + lane * box_bytes),
+                        "l"(is_v ? &map_v : &map_k), "r"(0), "r"(c1), "r"(h), "r"(c3), "r"(b_land + 8 * place)
+                        : "memory");
+                __syncwarp();
+                if (++place == uint32_t(G::RS)) place = 0, ++lap;
+            }
+            attend_advance(P, sh, part.step, seq.tiles, upb);
         }
     } else if (w > 9) {
         // ------------------------------------------------------------------ help: queries, and tiles widened, a group every GROUPS-th
@@ -177,50 +294,51 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
         // after a wait that ran out the walk goes on to its end without waiting, so that the barrier among these
         // warps still matches
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (ok && !mbar_wait_bounded(bar, parity)) {
+            if (ok && !wide_wait(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
                 ok = false;
             }
         };
         auto meet = [&]() { named_bar_sync(2 + group, G::HELP); };
-        uint32_t units = 0, lap = 0, slot_lap = 0;  // units behind; how often this group's place and the load's slot have been through
+        uint32_t lap = 0, slot_lap = 0, c = 0;  // how often this group's place and the load's slot have been through; loads before
         int turn = 0, slot = 0;
-        WideCursor<G> at;
-        at.start(sh, U, any);
-        auto go_on = [&]() {
+        WideView U;
+        for (uint32_t task = 0; next_task(task, U); ++task) {
+        // the task's queries, once the products with those before are done
+        if (task > 0) wait(b_q_free, (task - 1) & 1);
+        quant_load_queries<G>(P, tasks + task % kWideTasks, smem, q_factors, task > 0 ? w - 10 : w - 2, 2 * G::GROUPS + (task > 0 ? 0 : 8));
+        if (lane == 0 && ok) mbar_arrive(task > 0 ? b_q : b_q_first);
+#pragma unroll 1
+        for (int l = 0; l < 2 * U.n; ++l, ++c) {
+            const bool mine = turn == group;
+            const int at_slot = slot;
+            const uint32_t at_lap = lap, at_slot_lap = slot_lap;
             if (++turn == G::GROUPS) turn = 0, ++lap;
             if (++slot == G::NS) slot = 0, ++slot_lap;
-            at.next(P, upb);
-        };
-        for (; at.more; go_on()) {
-            if (at.l == 0 && at.c > 0) {  // the next unit's queries, once the products with those before are done
-                wait(b_q_free, units++ & 1);
-                load_queries<G>(P, at.U, at.sh.b, smem, w - 10, 2 * G::GROUPS, P.half != 0);
-                __syncwarp();
-                if (lane == 0 && ok) mbar_arrive(b_q);
-            }
-            if (turn != group) continue;
-            const bool is_v = at.is_v();
+            if (!mine) continue;
+            const bool is_v = load_is_v<MT>(l, U.n);
+            const int row0 = (U.tile0 + load_step<MT>(l, U.n)) * kWideTile;
             if (!is_v && ptid < 16) {  // with the K tile come the scales of its rows, V's too
-                const int row = at.row0() + 16 * (ptid & 7);
-                const long long s = ((long long)at.sh.b * P.H + at.U.h) * P.blocks + (row >> P.block_shift);
-                tile_scales[((at.c + 1) / 2 % kWideScales) * 16 + ptid] = row < at.U.lim ? __ldg((ptid < 8 ? P.K_scale : P.V_scale) + s) : 0.f;
+                const int row = row0 + 16 * (ptid & 7);
+                const long long s = ((long long)U.b * P.H + U.h) * P.blocks + (row >> P.block_shift);
+                tile_scales[((c + 1) / 2 % G::SCALES) * 16 + ptid] = row < U.lim ? __ldg((ptid < 8 ? P.K_scale : P.V_scale) + s) : 0.f;
             }
-            wait(b_land + 8 * group, lap & 1);
-            const uint32_t groups = is_v ? gone[at.c % kWideRowFlags] : 0u;
-            const bool mend = is_v && at.mend(groups), careful = at.careful();
-            unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
-            if (slot_lap > 0) wait(b_empty + 8 * slot, (slot_lap + 1) & 1);
+            wait(b_land + 8 * group, at_lap & 1);
+            const uint32_t groups = is_v ? gone[c % kWideRowFlags] : 0u;
+            const bool careful = G::NAN_ROWS && is_v && U.masked && row0 + kWideTile > U.base;
+            const bool mend = is_v && (groups || careful || row0 + kWideTile > U.lim);
+            unsigned char* tile = smem + (s_ring - sbase) + at_slot * G::SLOT;
+            if (at_slot_lap > 0) wait(b_empty + 8 * at_slot, (at_slot_lap + 1) & 1);
             const unsigned char* from = smem + (s_raw - sbase) + group * G::RAW;
             if (careful) {  // drafted rows that are NaN; rows of `groups` have no page, their place holds what an older tile left there
-                if (ptid < 4) odd_rows[slot * 4 + ptid] = 0u;
+                if (ptid < 4) odd_rows[at_slot * 4 + ptid] = 0u;
                 meet();
-                const int first = max(0, at.U.base - at.row0()) * G::CPR, last = min(kWideTile, at.U.lim - at.row0()) * G::CPR;
+                const int first = max(0, U.base - row0) * G::CPR, last = min(kWideTile, U.lim - row0) * G::CPR;
 #pragma unroll 4
                 for (int id = first + ptid; id < last; id += G::HELP) {
                     const uint4 v = *reinterpret_cast<const uint4*>(from + id * 16);
                     const uint32_t nan = Code<FORM>::nan_bytes(v.x) | Code<FORM>::nan_bytes(v.y) | Code<FORM>::nan_bytes(v.z) | Code<FORM>::nan_bytes(v.w);
-                    if (nan && !(groups >> (id / G::CPR >> 4) & 1)) atomicOr(&odd_rows[slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
+                    if (nan && !(groups >> (id / G::CPR >> 4) & 1)) atomicOr(&odd_rows[at_slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
                 }
                 meet();
             }
@@ -245,29 +363,30 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
             }
             if (mend) {  // rows behind the last one, without a page, or noted become zeros, so that 0 * NaN never happens
                 meet();
-                const uint32_t* odd = odd_rows + slot * 4;
-                const int begin = groups ? 0 : max(0, (careful && (odd[0] | odd[1] | odd[2] | odd[3]) ? min(at.U.base, at.U.lim) : at.U.lim) - at.row0());
+                const uint32_t* odd = odd_rows + at_slot * 4;
+                const int begin = groups ? 0 : max(0, (careful && (odd[0] | odd[1] | odd[2] | odd[3]) ? min(U.base, U.lim) : U.lim) - row0);
                 for (int id = begin * (D / 8) + ptid; id < kWideTile * (D / 8); id += G::HELP) {
                     const int rr = id / (D / 8), cc = id % (D / 8);
-                    if (at.row0() + rr >= at.U.lim || (groups >> (rr >> 4) & 1) || (careful && (odd[rr >> 5] >> (rr & 31) & 1)))
+                    if (row0 + rr >= U.lim || (groups >> (rr >> 4) & 1) || (careful && (odd[rr >> 5] >> (rr & 31) & 1)))
                         *reinterpret_cast<uint4*>(tile + (cc >> 3) * G::PANEL + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                 }
             }
             fence_proxy_async();
             meet();
             if (ptid == 0 && ok) {
-                mbar_arrive(b_full + 8 * slot);
+                mbar_arrive(b_full + 8 * at_slot);
                 mbar_arrive(b_raw_free + 8 * group);
             }
+        }
         }
     } else if (w == 8) {
         // ------------------------------------------------------------------ the products
         constexpr uint32_t id_qk = mma_idesc(false, false, MT == 1 ? 128 : 64), id_pv = mma_idesc(false, true, D);
         const uint32_t lead = elect_one();
         uint32_t slot = G::NS - 1, phase = 1;  // the load taken last (loads are taken in their order)
-        uint32_t np = 0, nq = 0;               // parities of the probabilities (a bit per stream and place), of units
+        uint32_t np = 0;                       // parities of the probabilities (a bit per stream and place)
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (ok && !mbar_wait_bounded(bar, parity)) {
+            if (ok && !wide_wait(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
                 ok = false;
             }
@@ -303,12 +422,10 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
             for (int ks = 0; ks < 4; ++ks) mma_ts(lead, at_o(s), at_s(s, p) + ks * 8, v + ks * (2048 >> 4), id_pv);
             tm_commit(lead, b_o + 8 * s);
         };
-        for (bool first = true; ok && any; first = false) {
+        WideView U;
+        for (uint32_t task = 0; next_task(task, U); ++task) {
             const int n = __shfl_sync(~0u, U.n, 0);
-            if (!first) {  // the first unit's queries are there
-                if (!wait(b_q, nq)) break;
-                nq ^= 1;
-            }
+            if (!wait(task > 0 ? b_q : b_q_first, task > 0 ? (task - 1) & 1 : 0)) break;
             if constexpr (MT == 1) {
                 // step i: products with V of tile i, and the scores of tile i + 2, whose place they free
 #pragma unroll 1
@@ -356,7 +473,6 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                     if (j + 2 == 2 * n - 1) tm_commit(lead, b_q_free);
                 }
             }
-            any = wide_next<G>(P, sh, U, upb);
         }
     } else {
         // ------------------------------------------------------------------ softmax of a stream
@@ -366,29 +482,27 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
         uint32_t ns = 0, items = 0, c0 = 0;  // parities of the scores (a bit per place); items and loads of the units before
         auto wait = [&](uint32_t bar, uint32_t parity) {
             // after a wait that ran out the barriers among these warps go on, everything else stops
-            if (ok && !mbar_wait_bounded(bar, parity)) {
+            if (ok && !wide_wait(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
                 ok = false;
             }
             tm_fence_after();
         };
-        while (any) {
+        WideView U;
+        for (uint32_t task = 0; next_task(task, U); ++task) {
+            const WideTask& told = tasks[task % kWideTasks];
+            if (task == 0) {  // the first queries
+                quant_load_queries<G>(P, &told, smem, q_factors, w, 8 + 2 * G::GROUPS);
+                if (lane == 0) mbar_arrive(b_q_first);
+            }
+            const int tokens = told.tokens;
             const int mine = MT == 2 ? 2 * U.n : U.n;          // items of this stream
             const int mu = (MT == 2 ? s * kWideTile : 0) + m;  // this thread's query row in the unit
             const int row = U.m0 + mu, t = row / P.G;
             const bool there = mu < U.mrows;
-            float f = 1.f;
-            if (there && !P.half) {  // the factor that the row was stored with
-                const uint16_t* q = P.Q + (long long)sh.b * P.q_sb + (long long)t * P.q_st + (long long)(U.h * P.G + row % P.G) * P.q_sh;
-                float top = 0.f;
-#pragma unroll 8
-                for (int d = 0; d < D; d += 8) top = fmaxf(top, largest_of(__ldg(reinterpret_cast<const uint4*>(q + d))));
-                f = query_factor(top);
-            }
-            const float scl = P.scale_log2 / f;
             unsigned long long bits = 0;
-            if (there && U.masked && t < U.seq.tokens)
-                bits = P.mask ? P.mask[(long long)sh.b * P.T + t] : (t == 63 ? ~0ull : (2ull << t) - 1);
+            if (there && U.masked && t < tokens)
+                bits = P.mask ? P.mask[(long long)U.b * P.T + t] : (t == 63 ? ~0ull : (2ull << t) - 1);
             __syncwarp();  // the instructions on tensor memory need warps that are together
             {  // O starts at zero, every product adds to it
                 uint32_t z[32];
@@ -398,7 +512,7 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                 for (int d = 0; d < D; d += 32) tm_st32(t_o + d, z);
                 tm_wait_st();
             }
-            float ref = -INFINITY, sum = 0.f;
+            float ref = -INFINITY, sum = 0.f, scl = 0.f;
             int ve = -126;  // O counts in units of 2^ve
 #pragma unroll 1
             for (int k = 0; k < mine; ++k) {
@@ -407,18 +521,9 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                 const int r0 = (U.tile0 + i) * kWideTile + 64 * half;
                 wait(b_s + 8 * (2 * s + p), ns >> p & 1);
                 ns ^= 1u << p;
-                uint32_t a[32], b[32];
-                tm_ld32(a, t_s);
-                tm_ld32(b, t_s + 32);
+                if (k == 0) scl = P.scale_log2 / __int_as_float(int(q_factors[mu]) << 23);  // written before the scores were
                 const uint32_t load = c0 + load_of_k<MT>(i);
-                const float* scales = tile_scales + ((load + 1) / 2 % kWideScales) * 16 + 4 * half;
-                // factors of the logits of 16 rows each: never 0, which would make NaN of the -infinity of hidden rows
-                float fk[4], vmax = 0.f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    fk[e] = fmaxf(scl * scales[e], 0x1p-126f);
-                    vmax = fmaxf(vmax, scales[8 + e]);
-                }
+                const float* scales = tile_scales + ((load + 1) / 2 % G::SCALES) * 16 + 4 * half;
                 const bool draft = U.masked && r0 + 64 > U.base;
                 const uint32_t missing = gone[load % kWideRowFlags] >> 4 * half & 15u;  // 16-row groups without a page
                 const bool hidden = draft || missing || r0 + 64 > U.lim;
@@ -433,26 +538,37 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                     }
                     return see;
                 };
+                if (hidden || P.cap_inv != 0.f) {  // in place, out of the way of what every item runs (see the end of the file's head)
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t x[16];
+                        tm_ld16(x, t_s + 16 * q);
+                        if (P.cap_inv != 0.f) {
+                            const float fx = fmaxf(scl * scales[q], 0x1p-126f) * P.cap_inv;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(P.cap_log2 * quant_tanh(__uint_as_float(x[e]) * fx));
+                        }
+                        const uint32_t see = seen32(r0 + 32 * (q >> 1)) >> 16 * (q & 1);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (!(see >> e & 1)) x[e] = 0xff800000u;
+                        __syncwarp();
+                        tm_st16(t_s + 16 * q, x);
+                    }
+                    tm_wait_st();
+                }
+                uint32_t a[32], b[32];
+                tm_ld32(a, t_s);
+                tm_ld32(b, t_s + 32);
+                // factors of the logits of 16 rows each: never 0, which would make NaN of the -infinity of hidden rows
+                float fk[4], vmax = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    fk[e] = P.cap_inv != 0.f ? 1.f : fmaxf(scl * scales[e], 0x1p-126f);
+                    vmax = fmaxf(vmax, scales[8 + e]);
+                }
                 tm_wait_ld(a);
                 tm_wait_ld(b);
-                __syncwarp();
-                if (P.cap_inv != 0.f) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        a[e] = __float_as_uint(P.cap_log2 * quant_tanh(__uint_as_float(a[e]) * fk[e / 16] * P.cap_inv));
-                        b[e] = __float_as_uint(P.cap_log2 * quant_tanh(__uint_as_float(b[e]) * fk[2 + e / 16] * P.cap_inv));
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) fk[e] = 1.f;
-                }
-                if (hidden) {
-                    const uint32_t see_a = seen32(r0), see_b = seen32(r0 + 32);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (!(see_a >> e & 1)) a[e] = 0xff800000u;
-                        if (!(see_b >> e & 1)) b[e] = 0xff800000u;
-                    }
-                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -505,12 +621,8 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                             before();
                             const int e = __ffs(int(odd)) - 1, r = r0 + 32 * x + e;
                             const bool see = seen32(r0 + 32 * x) >> e & 1;
-                            const long long off = attend_offset(P, sh.b, U.h, r & ~15);
+                            const long long off = attend_offset(P, U.b, U.h, r & ~15);
                             if (off < 0) continue;  // no page: never noted
-                            // the row's probability, once more
-                            tm_st32(t_s, a);
-                            tm_st32(t_s + 32, b);
-                            tm_wait_st();
                             const float z = __uint_as_float(tm_read1(t_s + 32 * x + e));
                             const float prob = see ? ex2(z * fk[2 * x + e / 16] - at) * scales[8 + 2 * x + e / 16] * unit : 0.f;
                             const uint8_t* v = P.V + off + (long long)(r & 15) * P.ss;
@@ -564,9 +676,9 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
             items += mine;
 
             // ---- the unit's result
-            const int first_cta = U.first_cta, last_cta = U.last_cta;
+            const int first_cta = told.first_cta, last_cta = told.last_cta;
             const bool shared = first_cta != last_cta, writes = there && ok;
-            float* part = P.partials + (2ll * blockIdx.x + (first_cta == int(blockIdx.x) ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0);
+            float* part = P.partials + (2ll * blockIdx.x + (first_cta == int(blockIdx.x) ? 1 : 0)) * G::PSIZE + (MT == 2 ? s * kWideTile * (D + 2) : 0) + m;
             float mref = ref, msum = sum, f_own = 1.f;
             if (MT == 1) {  // both streams' references and sums; each finishes every other group of 16 channels
                 float2* ml = reinterpret_cast<float2*>(exch);
@@ -581,6 +693,16 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                 msum = s == 0 ? own + other : other + own;
             }
             f_own *= pow2_of(ve);
+            // not shared: out and lse, as attend_write() has them
+            const long long at_row = (((long long)U.b * P.T + t) * P.H + U.h) * P.G + (row - t * P.G);
+            const bool live = t < tokens && msum != 0.f;  // NaN sums stay: they compare unequal to 0
+            const float inv = live ? P.v_scale / msum : 0.f;
+            if (writes && (MT == 2 || s == 0)) {
+                if (shared)
+                    __stcg(reinterpret_cast<float2*>(part - m + kWideTile * D + 2 * m), make_float2(mref, msum));
+                else if (P.lse)
+                    P.lse[at_row] = live ? 0.69314718055994531f * (mref + log2f(msum)) : -INFINITY;
+            }
 #pragma unroll 1
             for (int d0 = 0; d0 < D; d0 += MT == 1 ? 32 : 16) {
                 uint32_t a[16];
@@ -593,26 +715,31 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                 }
                 const int d = d0 + (MT == 1 ? 16 * s : 0);
                 tm_ld16(a, t_o + d);
-                float o[2][8];
+                float o[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    o[e / 8][e % 8] = MT == 1 ? __uint_as_float(a[e]) * f_own + exch[((s ^ 1) * 16 + e) * kWideTile + m] : __uint_as_float(a[e]) * f_own;
+                    o[e] = MT == 1 ? __uint_as_float(a[e]) * f_own + exch[((s ^ 1) * 16 + e) * kWideTile + m] : __uint_as_float(a[e]) * f_own;
                 if (writes && shared) {  // channel by channel: a warp writes 32 rows side by side
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) __stcg(part + (d + e) * kWideTile + m, o[e / 8][e % 8]);
+                    for (int e = 0; e < 16; ++e) __stcg(part + (d + e) * kWideTile, o[e]);
                 } else if (writes) {
+                    uint32_t v[8];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) quant_write_out<D>(P, sh.b, U.h, U.m0, U.seq.tokens, mu, d + 8 * x, o[x], mref, msum);
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = o[2 * e] * inv, y = o[2 * e + 1] * inv;
+                        v[e] = !live ? 0u : P.half ? MmaHalf::pack(x, y) : Mma<0>::pack(x, y);
+                    }
+                    uint4* to = reinterpret_cast<uint4*>(P.out + at_row * D + d);
+                    to[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                    to[1] = make_uint4(v[4], v[5], v[6], v[7]);
                 }
                 __syncwarp();
                 if (MT == 1) named_bar_sync(1, 256);
             }
-            if (shared && writes && (MT == 2 || s == 0)) __stcg(reinterpret_cast<float2*>(part + kWideTile * D + 2 * m), make_float2(mref, msum));
             // who shares the unit, for the kernel that joins the partials: said once, by the CTA that starts it
             if (tid == 0 && first_cta == int(blockIdx.x))
-                P.shared[(long long)sh.b * upb + U.u] = ok ? make_int2(first_cta, last_cta) : make_int2(0, 0);
+                P.shared[(long long)U.b * upb + told.u] = ok ? make_int2(first_cta, last_cta) : make_int2(0, 0);
             c0 += 2 * U.n;
-            any = wide_next<G>(P, sh, U, upb);
         }
     }
     tm_fence_before();
