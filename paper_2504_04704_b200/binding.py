@@ -281,8 +281,11 @@ class QuantCache:
         self.strides = _dense_strides(K, "K")
         if _dense_strides(V, "V") != self.strides:
             raise TypeError("K and V must have the same strides")
+        # what the calls of a decode step compare
+        self.device, self.shape, self.scale_shape, self.rows = K.get_device(), tuple(K.shape), tuple(K_scale.shape), K.shape[2]
         self.arg = lagkv_quant_cache(K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr(), _QUANT_FORMATS[K.dtype],
                                      self.block_rows, K_scale.shape[2], *self.strides)
+        self.ref = ctypes.byref(self.arg)
 
 
 class Plan:
@@ -302,6 +305,7 @@ class Plan:
         _check(lib.lagkv_plan(ctypes.byref(self.cfg), ctypes.byref(self.handle)), "lagkv_plan")
         self.lib = lib
         self.device = int(device)
+        self._dims = (int(B), int(H_kv), int(D))
         self.k = int(lib.lagkv_keep_count(self.handle))
 
     def close(self):
@@ -757,36 +761,36 @@ class Plan:
                           *(torch.zeros(scales, dtype=torch.float32, device=dev) for _ in "KV"), block_rows=block_rows)
 
     def _check_quant(self, cache, paged: bool):
-        c = self.cfg
-        if cache.K.get_device() != self.device:
+        (B, H, D), (n, heads, _, channels) = self._dims, cache.shape
+        if cache.device != self.device:
             raise TypeError(f"the cache must be on device {self.device}")
-        if cache.K_scale.shape[:2] != (c.B, c.H_kv) or cache.K.shape[1] != c.H_kv or cache.K.shape[3] != c.D or \
-                not paged and cache.K.shape[0] != c.B:
-            raise TypeError(f"the cache must be [{c.B}, {c.H_kv}, S_cap, {c.D}], or pages [num_pages, {c.H_kv}, page_size, {c.D}], "
-                            f"with scales [{c.B}, {c.H_kv}, blocks]")
+        if heads != H or channels != D or cache.scale_shape[:2] != (B, H) or not paged and n != B:
+            raise TypeError(f"the cache must be [{B}, {H}, S_cap, {D}], or pages [num_pages, {H}, page_size, {D}], with scales [{B}, {H}, blocks]")
         if paged and any(cache.strides):
             raise TypeError("paged codes must be contiguous")
-        return ctypes.byref(cache.arg)
+        return cache.ref
 
     def _quant_source(self, K, V, from_len, seq_len, take, at_positions):
-        c, shape = self.cfg, K.shape
-        for t, name in ((K, "K"), (V, "V")):
-            if t.dtype != self.dtype or t.get_device() != self.device or t.dim() != 4 or t.shape != (c.B, c.H_kv, shape[2], c.D):
-                raise TypeError(f"{name} must be a {self.dtype} CUDA tensor [{c.B}, {c.H_kv}, T, {c.D}] on device {self.device}")
-        strides = _dense_strides(K, "K")
-        if _dense_strides(V, "V") != strides:
-            raise TypeError("K and V must have the same strides")
-        self._check_ints(seq_len, "seq_len", (c.B,))
-        self._check_ints(from_len, "from_len", (c.B,))
-        heads = rows = 0
-        if take is not None:
-            if take.dim() == 2:
-                take = take[:, None]
-            if take.dim() != 3 or take.shape[1] not in (1, c.H_kv):
-                raise TypeError("take must be [B, rows] or [B, H_kv, rows]")
-            heads, rows = take.shape[1], take.shape[2]
-            self._check_ints(take, "take", (c.B, heads, rows))
-        return lagkv_quant_source(shape[2], int(bool(at_positions)), _addr(take), heads, rows, *strides)
+        (B, H, D), shape, dtype, dev = self._dims, K.shape, self.dtype, self.device
+        if len(shape) != 4 or V.shape != shape or shape[0] != B or shape[1] != H or shape[3] != D or K.dtype != dtype or V.dtype != dtype or \
+                K.get_device() != dev or V.get_device() != dev:
+            raise TypeError(f"K and V must be {dtype} CUDA tensors [{B}, {H}, T, {D}] on device {dev}")
+        if K.is_contiguous() and V.is_contiguous():
+            strides = (0, 0, 0)
+        else:
+            strides = _dense_strides(K, "K")
+            if _dense_strides(V, "V") != strides:
+                raise TypeError("K and V must have the same strides")
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(from_len, "from_len", (B,))
+        if take is None:
+            return lagkv_quant_source(shape[2], 1 if at_positions else 0, None, 0, 0, *strides)
+        if take.dim() == 2:
+            take = take[:, None]
+        if take.dim() != 3 or take.shape[1] not in (1, H):
+            raise TypeError("take must be [B, rows] or [B, H_kv, rows]")
+        self._check_ints(take, "take", (B, take.shape[1], take.shape[2]))
+        return lagkv_quant_source(shape[2], 1 if at_positions else 0, take.data_ptr(), take.shape[1], take.shape[2], *strides)
 
     def quant_write(self, cache, K, V, seq_len, workspace, from_len=None, take=None, at_positions=False) -> None:
         """``lagkv_quant_write``: rows ``[from_len[b], seq_len[b])`` of the cache from ``K``, ``V`` ``[B, H, T, D]`` (any strides,
@@ -794,7 +798,7 @@ class Plan:
         (``take`` int32 ``[B, H, rows]`` or ``[B, rows]``)."""
         q = self._check_quant(cache, False)
         src = self._quant_source(K, V, from_len, seq_len, take, at_positions)
-        rc = self.lib.lagkv_quant_write(self.handle, q, int(cache.K.shape[2]), ctypes.byref(src), _addr(K), _addr(V), _addr(from_len),
+        rc = self.lib.lagkv_quant_write(self.handle, q, cache.rows, ctypes.byref(src), _addr(K), _addr(V), _addr(from_len),
                                         _addr(seq_len), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_quant_write")
 
@@ -809,35 +813,38 @@ class Plan:
         _check(rc, "lagkv_quant_write_paged")
 
     def _quant_out(self, seq_len, from_len, idx, K_out, V_out):
-        c = self.cfg
-        self._check_ints(seq_len, "seq_len", (c.B,))
-        self._check_ints(from_len, "from_len", (c.B,))
-        if idx is not None:
-            if idx.dim() != 3:
-                raise TypeError("idx must be [B, H, rows]")
-            self._check_ints(idx, "idx", (c.B, c.H_kv, idx.shape[2]))
-            want = (c.B, c.H_kv, idx.shape[2], c.D)
+        B, H, D = self._dims
+        self._check_ints(seq_len, "seq_len", (B,))
+        self._check_ints(from_len, "from_len", (B,))
+        if idx is None:
             if K_out is None and V_out is None:
-                K_out, V_out = (torch.empty(want, dtype=self.dtype, device=self._dev()) for _ in "KV")
-            for t, name in ((K_out, "K_out"), (V_out, "V_out")):
-                if t is not None and (t.shape != want or t.dtype != self.dtype or t.get_device() != self.device or not t.is_contiguous()):
-                    raise TypeError(f"{name} must be a contiguous {self.dtype} CUDA tensor {want} on device {self.device}")
-            return K_out, V_out, idx.shape[2]
+                raise TypeError("K_out or V_out is needed without idx")
+            if K_out is not None:
+                self._check_contiguous_cache(K_out, "K_out")
+            if V_out is not None:
+                self._check_contiguous_cache(V_out, "V_out")
+                if K_out is not None and K_out.shape != V_out.shape:
+                    raise TypeError("K_out and V_out must have the same shape")
+            return K_out, V_out, (V_out if K_out is None else K_out).shape[2]
+        if idx.dim() != 3:
+            raise TypeError("idx must be [B, H, rows]")
+        rows = idx.shape[2]
+        self._check_ints(idx, "idx", (B, H, rows))
+        want = (B, H, rows, D)
         if K_out is None and V_out is None:
-            raise TypeError("K_out or V_out is needed without idx")
+            K_out = torch.empty(want, dtype=self.dtype, device=idx.device)
+            return K_out, torch.empty_like(K_out), rows
         for t, name in ((K_out, "K_out"), (V_out, "V_out")):
-            if t is not None:
-                self._check_contiguous_cache(t, name)
-        if K_out is not None and V_out is not None and K_out.shape != V_out.shape:
-            raise TypeError("K_out and V_out must have the same shape")
-        return K_out, V_out, (V_out if K_out is None else K_out).shape[2]
+            if t is not None and (t.shape != want or t.dtype != self.dtype or t.get_device() != self.device or not t.is_contiguous()):
+                raise TypeError(f"{name} must be a contiguous {self.dtype} CUDA tensor {want} on device {self.device}")
+        return K_out, V_out, rows
 
     def quant_read(self, cache, seq_len, workspace, from_len=None, idx=None, K_out=None, V_out=None):
         """``lagkv_quant_read``: rows ``[from_len[b], seq_len[b])`` into the same positions of the 16-bit caches ``K_out``, ``V_out``
         ``[B, H, rows, D]`` (one may be None), or rows ``idx`` int32 ``[B, H, rows]`` into dense outputs. Returns both."""
         q = self._check_quant(cache, False)
         K_out, V_out, rows = self._quant_out(seq_len, from_len, idx, K_out, V_out)
-        rc = self.lib.lagkv_quant_read(self.handle, q, int(cache.K.shape[2]), _addr(from_len), _addr(seq_len), _addr(idx), int(rows),
+        rc = self.lib.lagkv_quant_read(self.handle, q, cache.rows, _addr(from_len), _addr(seq_len), _addr(idx), rows,
                                        _addr(K_out), _addr(V_out), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_quant_read")
         return K_out, V_out
@@ -874,7 +881,7 @@ class Plan:
         self._check_ints(tree_mask, "tree_mask", (B, q.T), torch.int64)
         out, lse = self._attend_out(Q, out, want_lse)
         rc = self.lib.lagkv_attend_quant(
-            self.handle, ctypes.byref(q), cap, qc, _addr(Q), cache.K.shape[2], _addr(seq_len), _addr(draft_len), _addr(tree_mask),
+            self.handle, ctypes.byref(q), cap, qc, _addr(Q), cache.rows, _addr(seq_len), _addr(draft_len), _addr(tree_mask),
             _addr(out), _addr(lse), *self._ws(workspace), _raw_stream(self.device))
         _check(rc, "lagkv_attend_quant")
         return {"out": out, "lse": lse} if want_lse else {"out": out}

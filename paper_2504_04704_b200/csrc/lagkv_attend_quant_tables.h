@@ -24,7 +24,6 @@ int attend_e4m3_kernels(const AttendEntry** table);
     LAGKV_QUANT_ENTRY(96, FORM, 1), LAGKV_QUANT_ENTRY(96, FORM, 2), LAGKV_QUANT_ENTRY(96, FORM, 4), \
     LAGKV_QUANT_ENTRY(128, FORM, 1), LAGKV_QUANT_ENTRY(128, FORM, 2), LAGKV_QUANT_ENTRY(128, FORM, 4), \
     LAGKV_QUANT_ENTRY(256, FORM, 1), LAGKV_QUANT_ENTRY(256, FORM, 2), \
-    LAGKV_QUANT_WIDE_ENTRY(64, FORM, 1), LAGKV_QUANT_WIDE_ENTRY(96, FORM, 1), LAGKV_QUANT_WIDE_ENTRY(128, FORM, 1), \
-    LAGKV_QUANT_WIDE_ENTRY(64, FORM, 2), LAGKV_QUANT_WIDE_ENTRY(96, FORM, 2), LAGKV_QUANT_WIDE_ENTRY(128, FORM, 2)
+    LAGKV_QUANT_WIDE_ENTRY(64, FORM, 1), LAGKV_QUANT_WIDE_ENTRY(96, FORM, 1), LAGKV_QUANT_WIDE_ENTRY(128, FORM, 1)
 
 }  // namespace lagkv

@@ -3,7 +3,8 @@
 
 namespace lagkv {
 namespace {
-const AttendEntry kTable[] = {LAGKV_QUANT_ENTRIES(FORM_INT8)};
+const AttendEntry kTable[] = {LAGKV_QUANT_ENTRIES(FORM_INT8), LAGKV_QUANT_WIDE_ENTRY(64, FORM_INT8, 2),
+                               LAGKV_QUANT_WIDE_ENTRY(96, FORM_INT8, 2), LAGKV_QUANT_WIDE_ENTRY(128, FORM_INT8, 2)};
 }  // namespace
 
 int attend_int8_kernels(const AttendEntry** table) {

@@ -184,17 +184,45 @@ int quant_read(lagkv_plan_t plan, const lagkv_quant_cache* cache, int64_t S_cap,
     return check_launch();
 }
 
-// The smallest unit that holds all query rows, else the largest there is.
-const AttendEntry* find_quant(int D, int format, int query_rows, int* index) {
+// The kernel with units of `rows` query rows.
+const AttendEntry* quant_entry(int D, int format, int rows, int* index) {
     const AttendEntry* t;
     const int n = format == LAGKV_QUANT_INT8 ? attend_int8_kernels(&t) : attend_e4m3_kernels(&t);
-    const AttendEntry* best = nullptr;
-    for (int i = 0; i < n; ++i) {
-        if (t[i].D != D) continue;
-        const bool fits = t[i].rows >= query_rows, best_fits = best && best->rows >= query_rows;
-        if (best == nullptr || (fits && (!best_fits || t[i].rows < best->rows)) || (!fits && !best_fits && t[i].rows > best->rows)) {
-            best = t + i;
+    for (int i = 0; i < n; ++i)
+        if (t[i].D == D && t[i].rows == rows) {
             *index = i + (format == LAGKV_QUANT_INT8 ? 0 : 32);
+            return t + i;
+        }
+    return nullptr;
+}
+
+// Which unit a call takes: the least of (time of a short call) + units per KV head * rows of all caches * (time per row), which
+// are what calls of 8 KV heads and 128 channels took, in us, 1 sequence of 256 and 16 of 8192 rows:
+//     unit              8           16           32          128
+//     int8         10    87     11    61    13    82     14   106      (16 query rows; 128: 36 query rows)
+//     e4m3         10    79     11    58    13    79     15   104
+//   64 query rows: 10.6 317   11.7  206   13.8  156     14.7 107     (int8)
+// A sequence costs some 384 rows more than it has (64 x 512 rows, 36 query rows: 91, 79, 82 and 51 us).  The time per row of the first three follows
+// the channels (64 of them: 61, 45, 60 and 94 us where 128 take 87, 61, 82 and 107); the cap costs the last one most (24 KV heads
+// of 16411 rows of 64 channels, 35 query rows: 52, 44, 48 and 73 us, uncapped the last one 55).
+// Units of 256 rows read K and V once for two of 128, but have two groups of helpers only: 64 tokens over 2 x 8 x 131072 int8
+// rows in 295 us against 313; 207 and 207 over 16 x 8 x 8192, 145 against 124 over 64 x 8 x 512 (e4m3 234 against 205: not built).
+const AttendEntry* find_quant(const lagkv_config& c, int format, int query_rows, int64_t S_cap, bool capped, int* index) {
+    if (format == LAGKV_QUANT_INT8 && query_rows > 128 && S_cap >= 32768 && c.D <= 128) return quant_entry(c.D, format, 256, index);
+    const int units[4] = {8, 16, 32, 128};
+    const double base[4] = {9.3, 10.6, 13.0, 16.5}, per_row[4] = {37e-6, 56e-6, 77e-6, 99e-6};
+    const double rows = double(c.B) * c.H_kv * (double(S_cap) + 384.0), narrow = 0.5 + c.D / 256.0, wide = (0.8 + c.D / 640.0) * (capped ? 1.4 : 1.0);
+    const AttendEntry* best = nullptr;
+    double least = 0.0;
+    for (int i = 0; i < 4; ++i) {
+        int at;
+        const AttendEntry* e = quant_entry(c.D, format, units[i], &at);
+        if (e == nullptr) continue;  // 256 channels: 8 and 16
+        const double time = base[i] + ((query_rows + units[i] - 1) / units[i]) * rows * per_row[i] * (e->wide ? wide : narrow);
+        if (best == nullptr || time < least) {
+            best = e;
+            least = time;
+            *index = at;
         }
     }
     return best;
@@ -232,7 +260,7 @@ int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const 
     P.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
     const int query_rows = P.T * P.G;
     int index = 0;
-    const AttendEntry* e = find_quant(plan->cfg.D, cache->format, query_rows, &index);
+    const AttendEntry* e = find_quant(plan->cfg, cache->format, query_rows, P.S_cap, cap > 0.0, &index);
     if (e == nullptr) return LAGKV_EUNSUPPORTED;
     const long long units = quant_units(plan->cfg, *e, query_rows);
     rc = workspace_ok(workspace, bytes, kHead);
@@ -308,9 +336,10 @@ size_t lagkv_attend_quant_workspace_bytes(lagkv_plan_t plan, int32_t T, int32_t 
     size_t partials = 0;
     const int rows_all = T * (H_q / plan->cfg.H_kv);
     for (int format : {LAGKV_QUANT_INT8, LAGKV_QUANT_E4M3})
-        for (int rows : {1, 9, 17, 33, 129}) {
+        for (int rows : {8, 16, 32, 128, 256}) {
+            if (rows == 256 && rows_all <= 128) continue;
             int index;
-            const AttendEntry* e = rows > 1 && rows > rows_all ? nullptr : find_quant(plan->cfg.D, format, rows, &index);
+            const AttendEntry* e = quant_entry(plan->cfg.D, format, rows, &index);
             if (e != nullptr && partial_bytes(plan, *e) > partials) partials = partial_bytes(plan, *e);
         }
     const size_t units = size_t(plan->cfg.B) * plan->cfg.H_kv * ((rows_all + 7) / 8);  // none has fewer rows

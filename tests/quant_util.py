@@ -116,8 +116,8 @@ def assert_attention(got, want):
     U.assert_attention(dict(got, out=torch.where(beyond, 0.0, got["out"])), (torch.where(beyond, 0.0, out), lse, torch.where(beyond, 0.0, t_out), t_lse))
 
 
-def attention_reference(Q, K, V, seq_len, draft_len, mask, scale=None, cap=0.0, v_scale=1.0, form="int8", V_scale=None):
-    """K, V [B, H, S, D] float64 values -> out, lse, and their tolerances [B, T, H_q, ...]."""
+def attention_reference(Q, K, V, seq_len, draft_len, mask, scale=None, cap=0.0, v_scale=1.0, form="int8", V_scale=None, gone=None):
+    """K, V [B, H, S, D] float64 values -> out, lse, and their tolerances [B, T, H_q, ...]; nobody sees rows `gone` (a slice)."""
     B, T, Hq, D = Q.shape
     H = K.shape[1]
     G = Hq // H
@@ -128,6 +128,8 @@ def attention_reference(Q, K, V, seq_len, draft_len, mask, scale=None, cap=0.0, 
     for b in range(B):
         n, d = int(seq_len[b]), int(draft_len[b])
         seen = U.tree_seen(None if mask is None else mask[b].tolist(), T, d, n).to(Q.device).repeat_interleave(G, 0)
+        if gone is not None:
+            seen[:, gone] = False
         for h in range(H):
             q = Q[b, :, h * G:(h + 1) * G].reshape(T * G, D)
             reach = (float(V_scale[b, h].max()) * TOP[form] if V_scale is not None else float(V[b, h, :n].abs().max()) if n else 0.0) * v_scale

@@ -27,14 +27,28 @@ def i32(x):
     return torch.tensor(x, dtype=torch.int32, device=DEV)
 
 
-def case(binding, kind, B, H, G, D, S, T, R, seed, lens=None, drafts=None, tree=True, spread=3.0):
+# Which kernel serves a call goes by the query rows and the capacity of the cache: small caches take units of 8 or 16 query rows,
+# with this much room units of 16 and 32 and, from some 40 query rows on, the kernel on tensor memory take over (int8: two units of 128 rows
+# in one from 129 rows on).
+ROOM = 40000
+
+
+def case(binding, kind, B, H, G, D, S, T, R, seed, lens=None, drafts=None, tree=True, spread=3.0, room=0):
     form, dtype = kind
     g = torch.Generator(device=DEV).manual_seed(seed)
     rng = random.Random(seed)
     K, V, ks, vs = QU.random_cache(B, H, S, D, form, R, g, spread)
+    if room:  # more room behind the rows
+        blocks, some = -(-room // R), ks.shape[2]
+        store = torch.full((2, B, H, room, D), 0x7f, dtype=torch.uint8, device=DEV)
+        scales = torch.full((2, B, H, blocks), float("nan"), device=DEV)
+        for i, (x, s) in enumerate(((K, ks), (V, vs))):
+            store[i, :, :, :S] = x.view(torch.uint8)
+            scales[i, :, :, :some] = s
+        K, V, ks, vs = store[0].view(K.dtype), store[1].view(K.dtype), scales[0], scales[1]
     lens = [rng.randint(T, S) for _ in range(B)] if lens is None else lens
     drafts = [min(T, n) for n in lens] if drafts is None else drafts
-    c = dict(form=form, R=R, cache=binding.QuantCache(K, V, ks, vs, block_rows=R), lens=lens, drafts=drafts,
+    c = dict(form=form, S=S, R=R, cache=binding.QuantCache(K, V, ks, vs, block_rows=R), lens=lens, drafts=drafts,
              Q=torch.randn((B, T, H * G, D), generator=g, device=DEV).to(dtype), seq=i32(lens), draft=i32(drafts),
              mask=U.random_tree(B, T, rng).to(DEV) if tree else None)
     c["plan"] = binding.Plan(B, H, D, sink=4, lag=64, dtype=dtype)
@@ -59,27 +73,28 @@ def run(c, **kw):
 
 
 def reference(c, **kw):
-    cache, R = c["cache"], c["R"]
-    K, V = QU.row_values(cache.K, cache.K_scale, R), QU.row_values(cache.V, cache.V_scale, R)
+    cache, R, S = c["cache"], c["R"], c["S"]
+    K, V = (QU.row_values(x[:, :, :S], s[:, :, :-(-S // R)], R) for x, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)))
     return QU.attention_reference(c["Q"], K, V, c["lens"], c["drafts"], c["mask"], form=c["form"],
                                   V_scale=cache.V_scale.nan_to_num(nan=0.0), **kw)
 
 
 @pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
-@pytest.mark.parametrize("T,G,H,R", [(1, 4, 2, 16), (1, 7, 4, 64), (5, 1, 3, 32), (3, 5, 2, 128), (13, 4, 2, 64), (32, 4, 1, 16), (64, 8, 1, 64)])
-def test_every_type_and_head_dim(binding, kind, D, T, G, H, R):
-    c = case(binding, kind, 3, H, G, D, 333, T, R, seed=D + T, lens=[max(T, 100), 333, max(T, 257)])
+@pytest.mark.parametrize("T,G,H,R", [(1, 4, 2, 16), (1, 7, 4, 64), (5, 1, 3, 32), (3, 5, 2, 128), (6, 5, 2, 32), (13, 4, 2, 64), (32, 4, 1, 16), (64, 8, 1, 64)])
+@pytest.mark.parametrize("room", [0, ROOM])
+def test_every_type_and_head_dim(binding, kind, D, T, G, H, R, room):
+    c = case(binding, kind, 3, H, G, D, 333, T, R, seed=D + T, lens=[max(T, 100), 333, max(T, 257)], room=room)
     poison(c)
     QU.assert_attention(run(c), reference(c))
 
 
 @pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
-@pytest.mark.parametrize("T", [1, 4, 40])
-def test_lengths_around_every_tile(binding, kind, T):
+@pytest.mark.parametrize("T,room", [(1, 0), (4, 0), (9, 8000), (40, 0), (20, 8000), (60, ROOM)])
+def test_lengths_around_every_tile(binding, kind, T, room):
     """Empty sequences, sequences that are all draft, and every length next to a multiple of 16, 32 or 64."""
     lens = [0, T, T + 1, 15 + T, 16 + T, 17 + T, 31 + T, 32 + T, 63 + T, 64 + T, 65 + T, 128, 129, 200]
-    c = case(binding, kind, len(lens), 2, 3, 128, 200, T, 32, seed=5, lens=lens)
+    c = case(binding, kind, len(lens), 2, 3, 128, 200, T, 32, seed=5, lens=lens, room=room)
     poison(c)
     got = run(c)
     QU.assert_attention(got, reference(c))
@@ -95,12 +110,12 @@ def test_chain_without_lengths_and_masks(binding, kind):
 
 
 @pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
-@pytest.mark.parametrize("T", [1, 9, 64])
-def test_padded_batch_and_rows_that_see_nothing(binding, kind, T):
+@pytest.mark.parametrize("T,room", [(1, 0), (9, 0), (64, 0), (7, ROOM), (20, ROOM), (64, ROOM)])
+def test_padded_batch_and_rows_that_see_nothing(binding, kind, T, room):
     """Draft lengths from 0 on; tokens whose mask is empty in a cache without other rows."""
     drafts = [0, min(1, T), T // 2, T, T]
     lens = [50, 33, T // 2, T, 90 + T]              # sequences 2 and 3 are nothing but their draft
-    c = case(binding, kind, 5, 2, 4, 128, 200, T, 16, seed=T, lens=lens, drafts=drafts)
+    c = case(binding, kind, 5, 2, 4, 128, 200, T, 16, seed=T, lens=lens, drafts=drafts, room=room)
     c["mask"][3, ::2] = 0
     c["mask"][4] = -1
     poison(c)
@@ -111,10 +126,10 @@ def test_padded_batch_and_rows_that_see_nothing(binding, kind, T):
 
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
-@pytest.mark.parametrize("T,G", [(7, 1), (7, 2), (40, 4), (64, 4)])
-def test_hidden_drafted_rows_may_hold_nan(binding, dtype, D, T, G):
+@pytest.mark.parametrize("T,G,room", [(7, 1, 0), (7, 2, 0), (40, 4, 0), (7, 4, ROOM), (40, 4, ROOM), (64, 4, ROOM)])
+def test_hidden_drafted_rows_may_hold_nan(binding, dtype, D, T, G, room):
     """e4m3 NaN in drafted rows reaches the tokens that see them and no others."""
-    c = case(binding, ("e4m3", dtype), 2, 2, G, D, 150, T, 16, seed=3, lens=[150, T])
+    c = case(binding, ("e4m3", dtype), 2, 2, G, D, 150, T, 16, seed=3, lens=[150, T], room=room)
     odd = [1, T - 2]
     bit = sum(1 << j for j in odd)
     m = c["mask"].cpu()
@@ -134,20 +149,20 @@ def test_hidden_drafted_rows_may_hold_nan(binding, dtype, D, T, G):
 
 
 @pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
-@pytest.mark.parametrize("T,G", [(1, 4), (6, 4), (64, 4)])
+@pytest.mark.parametrize("T,G,room", [(1, 4, 0), (6, 4, 0), (6, 4, ROOM), (32, 4, ROOM), (64, 4, ROOM)])
 @pytest.mark.parametrize("way", ["up", "down", "mixed", "zeros"])
-def test_scales_far_apart(binding, kind, T, G, way):
+def test_scales_far_apart(binding, kind, T, G, room, way):
     """V scales that climb by 2^40 in the order of the rows, fall, or lie anywhere; blocks whose scales are 0."""
-    c = case(binding, kind, 2, 2, G, 128, 640, T, 16, seed=T, lens=[640, 613])
+    c = case(binding, kind, 2, 2, G, 128, 640, T, 16, seed=T, lens=[640, 613], room=room)
     cache = c["cache"]
-    e = torch.linspace(-20, 20, cache.V_scale.shape[2], device=DEV)
+    e = torch.linspace(-20, 20, 640 // 16, device=DEV)
     if way == "zeros":
         cache.K_scale[:, :, 3::5] = 0
         cache.V_scale[:, :, ::3] = 0
         cache.V_scale[:, 1] = 0
     else:
         e = e if way == "up" else e.flip(0) if way == "down" else e[torch.randperm(len(e), generator=torch.Generator().manual_seed(1)).to(DEV)]
-        cache.V_scale.mul_(torch.exp2(e))
+        cache.V_scale[:, :, :640 // 16].mul_(torch.exp2(e))
     got = run(c)
     QU.assert_attention(got, reference(c))
     if way == "zeros":
@@ -155,11 +170,11 @@ def test_scales_far_apart(binding, kind, T, G, way):
 
 
 @pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
-@pytest.mark.parametrize("T,G", [(1, 4), (5, 7), (33, 4)])
+@pytest.mark.parametrize("T,G,room", [(1, 4, 0), (5, 7, 0), (4, 7, ROOM), (24, 4, ROOM), (33, 4, ROOM)])
 @pytest.mark.parametrize("cap", [0.5, 30.0, 1e5])
-def test_capped_logits(binding, kind, T, G, cap):
+def test_capped_logits(binding, kind, T, G, room, cap):
     """A cap far below the logits, near them, and far above (where it must not lose them)."""
-    c = case(binding, kind, 2, 2, G, 128, 500, T, 64, seed=2, lens=[500, 333])
+    c = case(binding, kind, 2, 2, G, 128, 500, T, 64, seed=2, lens=[500, 333], room=room)
     poison(c)
     QU.assert_attention(run(c, cap=cap), reference(c, cap=cap))
 
@@ -169,41 +184,45 @@ def test_capped_logits(binding, kind, T, G, cap):
 @pytest.mark.parametrize("T,G,cap", [(5, 7, 30.0), (5, 7, 4.0), (64, 4, 10.0)])
 def test_capped_logits_of_every_head_dim(binding, kind, D, T, G, cap):
     """Long ragged caches whose logits lie on both sides of the cap, within warps and among them."""
-    c = case(binding, kind, 2, 1, G, D, 5000, T, 32, seed=3, lens=[5000, 3777], spread=2.0)
+    c = case(binding, kind, 2, 1, G, D, 5000, T, 32, seed=3, lens=[5000, 3777], spread=2.0, room=2 * ROOM if T > 5 else 0)
     QU.assert_attention(run(c, cap=cap), reference(c, cap=cap))
 
 
 @pytest.mark.parametrize("kind", KINDS[:2], ids=KIND_IDS[:2])
-@pytest.mark.parametrize("T,G", [(1, 4), (12, 4)])
-def test_factors_and_large_logits(binding, kind, T, G):
+@pytest.mark.parametrize("T,G,room", [(1, 4, 0), (12, 4, 0), (5, 4, 2 * ROOM), (12, 4, 2 * ROOM), (40, 4, 2 * ROOM)])
+def test_factors_and_large_logits(binding, kind, T, G, room):
     """scale, k_scale and v_scale; logits in the hundreds, whose largest comes late."""
-    c = case(binding, kind, 2, 1, G, 128, 300, T, 32, seed=11, lens=[300, 299])
-    c["cache"].K_scale[:, :, -2:] *= 16
+    c = case(binding, kind, 2, 1, G, 128, 300, T, 32, seed=11, lens=[300, 299], room=room)
+    c["cache"].K_scale[:, :, 8:10] *= 16
     got = run(c, scale=0.5, k_scale=2.0, v_scale=0.25)
     QU.assert_attention(got, reference(c, scale=1.0, v_scale=0.25))
 
 
 @pytest.mark.parametrize("kind", KINDS[:2], ids=KIND_IDS[:2])
-def test_queries_at_the_ends_of_their_type(binding, kind):
+@pytest.mark.parametrize("T,room", [(3, 0), (15, 2 * ROOM)])
+def test_queries_at_the_ends_of_their_type(binding, kind, T, room):
     """Rows of queries of very different size keep their own factor; zero rows attend evenly."""
-    c = case(binding, kind, 1, 2, 4, 128, 200, 3, 64, seed=12, lens=[200])
-    c["Q"] *= torch.exp2(torch.linspace(-100, 3, 24, device=DEV)).view(1, 3, 8, 1).to(BF16)
+    c = case(binding, kind, 1, 2, 4, 128, 200, T, 64, seed=12, lens=[200], room=room)
+    c["Q"] *= torch.exp2(torch.linspace(-100, 3, 8 * T, device=DEV)).view(1, T, 8, 1).to(BF16)
     c["Q"][0, 0, 0] = 0
     QU.assert_attention(run(c), reference(c))
 
 
 @pytest.mark.parametrize("form", ["int8", "e4m3"])
-@pytest.mark.parametrize("T,G", [(1, 7), (4, 4), (20, 4)])
-@pytest.mark.parametrize("page,R", [(16, 16), (32, 16), (64, 64), (128, 32)])
-def test_pages(binding, form, T, G, page, R):
+@pytest.mark.parametrize("T,G,room", [(1, 7, 0), (4, 4, 0), (4, 4, ROOM), (7, 4, ROOM), (20, 4, ROOM), (40, 4, ROOM)])
+@pytest.mark.parametrize("page,R", [(16, 16), (32, 16), (64, 64), (128, 32), (256, 128)])
+def test_pages(binding, form, T, G, room, page, R):
     """Random pages; a table entry outside the pool counts as rows that nobody sees."""
-    B, H, D, S = 3, 2, 128, 384
-    c = case(binding, (form, BF16), B, H, G, D, S, T, R, seed=page + T, lens=[S, 250 + T, T])
+    B, H, D, S = 3, 2, 128, 512
+    room = room // page * page
+    c = case(binding, (form, BF16), B, H, G, D, S, T, R, seed=page + T, lens=[S, 250 + T, T], room=room)
     nb = S // page
     pages = B * nb + 2
     table = torch.randperm(pages, generator=torch.Generator().manual_seed(1))[:B * nb].view(B, nb).to(torch.int32).to(DEV)
     cache = c["cache"]
-    pool = binding.QuantCache(QU.pool_of(cache.K, page, table, pages), QU.pool_of(cache.V, page, table, pages), cache.K_scale, cache.V_scale, block_rows=R)
+    pool = binding.QuantCache(*(QU.pool_of(x[:, :, :S].contiguous(), page, table, pages) for x in (cache.K, cache.V)), cache.K_scale, cache.V_scale, block_rows=R)
+    if room:  # entries of blocks that no sequence reaches
+        table = torch.cat([table, torch.full((B, room // page - nb), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
     call = lambda tab: c["plan"].attend_quant_paged(c["Q"], pool, tab, c["seq"], c["ws"], draft_len=c["draft"], tree_mask=c["mask"], want_lse=True)  # noqa: E731
     got = call(table)
     assert c["plan"].read_status(c["ws"])[0] == 0
@@ -212,13 +231,13 @@ def test_pages(binding, form, T, G, page, R):
     assert torch.equal(flat["out"], got["out"]) and torch.equal(flat["lse"], got["lse"])
     # the second page of sequence 0 is gone: as a cache in which those rows are hidden
     bad = table.clone()
-    bad[0, 1], bad[2, -1] = -1, pages                              # the last page of sequence 2 is behind its rows
+    bad[0, 1], bad[2, nb - 1] = -1, pages                          # the last page of sequence 2 is behind its rows
     lost = call(bad)
     assert c["plan"].read_status(c["ws"])[0] == binding.LAGKV_EINVAL
     assert torch.equal(lost["out"][1:], got["out"][1:])
-    kept = torch.cat([torch.arange(page), torch.arange(2 * page, S)]).to(DEV)
-    K, V = (QU.row_values(x, s, R)[:1, :, kept] for x, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)))
-    want = QU.attention_reference(c["Q"][:1], K, V, [S - page], [c["drafts"][0]], c["mask"][:1], form=form, V_scale=cache.V_scale[:1])
+    K, V = (QU.row_values(x[:1, :, :S], s[:1, :, :S // R], R) for x, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)))
+    want = QU.attention_reference(c["Q"][:1], K, V, [S], [c["drafts"][0]], c["mask"][:1], form=form, V_scale=cache.V_scale[:1].nan_to_num(nan=0.0),
+                                  gone=slice(page, 2 * page))
     QU.assert_attention({"out": lost["out"][:1], "lse": lost["lse"][:1]}, want)
 
 
@@ -290,10 +309,10 @@ def test_bad_lengths_are_recorded(binding):
 
 
 @pytest.mark.parametrize("kind", KINDS[:2], ids=KIND_IDS[:2])
-@pytest.mark.parametrize("T,G", [(1, 4), (16, 8)])
-def test_graph_replay_and_repeats(binding, kind, T, G):
+@pytest.mark.parametrize("T,G,room", [(1, 4, 0), (4, 8, ROOM), (16, 8, ROOM), (64, 4, ROOM)])
+def test_graph_replay_and_repeats(binding, kind, T, G, room):
     """One captured call serves every length, and the same call gives the same bits; on another stream, too."""
-    c = case(binding, kind, 3, 2, G, 128, 3000, T, 64, seed=4, lens=[3000, 1700, T])
+    c = case(binding, kind, 3, 2, G, 128, 3000, T, 64, seed=4, lens=[3000, 1700, T], room=room)
     first = run(c)
     again = run(c)
     assert torch.equal(first["out"], again["out"]) and torch.equal(first["lse"], again["lse"])
@@ -313,10 +332,11 @@ def test_graph_replay_and_repeats(binding, kind, T, G):
         QU.assert_attention({"out": out}, reference(c))
 
 
-def test_two_calls_at_once_with_their_own_workspaces(binding):
-    c = case(binding, ("int8", BF16), 2, 4, 4, 128, 4096, 2, 64, seed=7, lens=[4096, 4000])
+@pytest.mark.parametrize("T", [2, 40])
+def test_two_calls_at_once_with_their_own_workspaces(binding, T):
+    c = case(binding, ("int8", BF16), 2, 4, 4, 128, 4096, T, 64, seed=7, lens=[4096, 4000], room=20000)
     want = run(c)
-    other = c["plan"].new_attend_quant_workspace(2, 16)
+    other = c["plan"].new_attend_quant_workspace(T, 16)
     streams = [torch.cuda.Stream() for _ in range(2)]
     torch.cuda.synchronize()
     got = []
@@ -330,7 +350,7 @@ def test_two_calls_at_once_with_their_own_workspaces(binding):
 
 
 @pytest.mark.parametrize("form", ["int8", "e4m3"])
-@pytest.mark.parametrize("T,G", [(1, 4), (2, 16)])
+@pytest.mark.parametrize("T,G", [(1, 4), (2, 16), (16, 4)])
 def test_a_long_cache(binding, form, T, G):
     """Offsets behind 2^32 bytes: only the last rows have large logits, the others weigh evenly."""
     D, S, R = 128, (1 << 25) + (1 << 24), 128
