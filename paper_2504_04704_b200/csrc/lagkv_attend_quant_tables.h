@@ -13,8 +13,9 @@ int attend_e4m3_kernels(const AttendEntry** table);
 #define LAGKV_QUANT_ENTRY(D, FORM, NQ) \
     { D, FORM, QuantGeo<D, FORM, NQ>::MR, false, size_t(QuantGeo<D, FORM, NQ>::MR) * (D + 2), QuantGeo<D, FORM, NQ>::NT, \
       QuantGeo<D, FORM, NQ>::CTAS, size_t(QuantGeo<D, FORM, NQ>::SMEM), \
-      reinterpret_cast<const void*>(&lagkv_attend_quant_kernel<D, FORM, NQ>), \
-      reinterpret_cast<const void*>(&lagkv_attend_quant_merge_kernel<D, FORM, NQ>), kMergeWarps, kMergeWarps * 32 }
+      reinterpret_cast<const void*>(&lagkv_attend_quant_kernel<D, FORM, NQ, false>), \
+      reinterpret_cast<const void*>(&lagkv_attend_quant_merge_kernel<D, FORM, NQ>), kMergeWarps, kMergeWarps * 32, \
+      reinterpret_cast<const void*>(&lagkv_attend_quant_kernel<D, FORM, NQ, true>) }
 #define LAGKV_QUANT_WIDE_ENTRY(D, FORM, MT) \
     { D, FORM, MT * kWideTile, true, size_t(QuantWideGeo<D, FORM, MT>::PSIZE), QuantWideGeo<D, FORM, MT>::NT, 1, \
       size_t(QuantWideGeo<D, FORM, MT>::SMEM), reinterpret_cast<const void*>(&lagkv_attend_quant_wide_kernel<D, FORM, MT>), \

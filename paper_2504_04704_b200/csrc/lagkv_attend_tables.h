@@ -15,6 +15,7 @@ struct AttendEntry {
     const void* fn;
     const void* join;  // launched behind it, for the units that several CTAs share, and the rows that a CTA takes
     int join_rows, join_threads;
+    const void* cluster = nullptr;  // the form with a cluster of CTAs for each unit, if there is one
 };
 
 // each returns the number of entries and sets *table
