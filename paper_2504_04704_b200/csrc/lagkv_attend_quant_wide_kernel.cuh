@@ -304,80 +304,80 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
         int turn = 0, slot = 0;
         WideView U;
         for (uint32_t task = 0; next_task(task, U); ++task) {
-        // the task's queries, once the products with those before are done
-        if (task > 0) wait(b_q_free, (task - 1) & 1);
-        quant_load_queries<G>(P, tasks + task % kWideTasks, smem, q_factors, task > 0 ? w - 10 : w - 2, 2 * G::GROUPS + (task > 0 ? 0 : 8));
-        if (lane == 0 && ok) mbar_arrive(task > 0 ? b_q : b_q_first);
+            // the task's queries, once the products with those before are done
+            if (task > 0) wait(b_q_free, (task - 1) & 1);
+            quant_load_queries<G>(P, tasks + task % kWideTasks, smem, q_factors, task > 0 ? w - 10 : w - 2, 2 * G::GROUPS + (task > 0 ? 0 : 8));
+            if (lane == 0 && ok) mbar_arrive(task > 0 ? b_q : b_q_first);
 #pragma unroll 1
-        for (int l = 0; l < 2 * U.n; ++l, ++c) {
-            const bool mine = turn == group;
-            const int at_slot = slot;
-            const uint32_t at_lap = lap, at_slot_lap = slot_lap;
-            if (++turn == G::GROUPS) turn = 0, ++lap;
-            if (++slot == G::NS) slot = 0, ++slot_lap;
-            if (!mine) continue;
-            const bool is_v = load_is_v<MT>(l, U.n);
-            const int row0 = (U.tile0 + load_step<MT>(l, U.n)) * kWideTile;
-            if (!is_v && ptid < 16) {  // with the K tile come the scales of its rows, V's too
-                const int row = row0 + 16 * (ptid & 7);
-                const long long s = ((long long)U.b * P.H + U.h) * P.blocks + (row >> P.block_shift);
-                tile_scales[((c + 1) / 2 % G::SCALES) * 16 + ptid] = row < U.lim ? __ldg((ptid < 8 ? P.K_scale : P.V_scale) + s) : 0.f;
-            }
-            wait(b_land + 8 * group, at_lap & 1);
-            const uint32_t groups = is_v ? gone[c % kWideRowFlags] : 0u;
-            const bool careful = G::NAN_ROWS && is_v && U.masked && row0 + kWideTile > U.base;
-            const bool mend = is_v && (groups || careful || row0 + kWideTile > U.lim);
-            unsigned char* tile = smem + (s_ring - sbase) + at_slot * G::SLOT;
-            if (at_slot_lap > 0) wait(b_empty + 8 * at_slot, (at_slot_lap + 1) & 1);
-            const unsigned char* from = smem + (s_raw - sbase) + group * G::RAW;
-            if (careful) {  // drafted rows that are NaN; rows of `groups` have no page, their place holds what an older tile left there
-                if (ptid < 4) odd_rows[at_slot * 4 + ptid] = 0u;
-                meet();
-                const int first = max(0, U.base - row0) * G::CPR, last = min(kWideTile, U.lim - row0) * G::CPR;
+            for (int l = 0; l < 2 * U.n; ++l, ++c) {
+                const bool mine = turn == group;
+                const int at_slot = slot;
+                const uint32_t at_lap = lap, at_slot_lap = slot_lap;
+                if (++turn == G::GROUPS) turn = 0, ++lap;
+                if (++slot == G::NS) slot = 0, ++slot_lap;
+                if (!mine) continue;
+                const bool is_v = load_is_v<MT>(l, U.n);
+                const int row0 = (U.tile0 + load_step<MT>(l, U.n)) * kWideTile;
+                if (!is_v && ptid < 16) {  // with the K tile come the scales of its rows, V's too
+                    const int row = row0 + 16 * (ptid & 7);
+                    const long long s = ((long long)U.b * P.H + U.h) * P.blocks + (row >> P.block_shift);
+                    tile_scales[((c + 1) / 2 % G::SCALES) * 16 + ptid] = row < U.lim ? __ldg((ptid < 8 ? P.K_scale : P.V_scale) + s) : 0.f;
+                }
+                wait(b_land + 8 * group, at_lap & 1);
+                const uint32_t groups = is_v ? gone[c % kWideRowFlags] : 0u;
+                const bool careful = G::NAN_ROWS && is_v && U.masked && row0 + kWideTile > U.base;
+                const bool mend = is_v && (groups || careful || row0 + kWideTile > U.lim);
+                unsigned char* tile = smem + (s_ring - sbase) + at_slot * G::SLOT;
+                if (at_slot_lap > 0) wait(b_empty + 8 * at_slot, (at_slot_lap + 1) & 1);
+                const unsigned char* from = smem + (s_raw - sbase) + group * G::RAW;
+                if (careful) {  // drafted rows that are NaN; rows of `groups` have no page, their place holds what an older tile left there
+                    if (ptid < 4) odd_rows[at_slot * 4 + ptid] = 0u;
+                    meet();
+                    const int first = max(0, U.base - row0) * G::CPR, last = min(kWideTile, U.lim - row0) * G::CPR;
 #pragma unroll 4
-                for (int id = first + ptid; id < last; id += G::HELP) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(from + id * 16);
-                    const uint32_t nan = Code<FORM>::nan_bytes(v.x) | Code<FORM>::nan_bytes(v.y) | Code<FORM>::nan_bytes(v.z) | Code<FORM>::nan_bytes(v.w);
-                    if (nan && !(groups >> (id / G::CPR >> 4) & 1)) atomicOr(&odd_rows[at_slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
+                    for (int id = first + ptid; id < last; id += G::HELP) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(from + id * 16);
+                        const uint32_t nan = Code<FORM>::nan_bytes(v.x) | Code<FORM>::nan_bytes(v.y) | Code<FORM>::nan_bytes(v.z) | Code<FORM>::nan_bytes(v.w);
+                        if (nan && !(groups >> (id / G::CPR >> 4) & 1)) atomicOr(&odd_rows[at_slot * 4 + id / G::CPR / 32], 1u << (id / G::CPR & 31));
+                    }
+                    meet();
                 }
-                meet();
-            }
-            // A row's 16-byte pieces become two each.  Eight lanes store to one panel's halves of two rows: the
-            // swizzle gives them all the banks.
-            const int r = D == 128 ? (ptid >> 4) * 2 + (ptid >> 2 & 1) : ptid / G::CPR, ch = D == 128 ? (ptid >> 1 & 4) + (ptid & 3) : ptid % G::CPR;
-            if (ptid < G::PASS_THREADS) {
-                from += r * G::ROWB + ch * 16;
-                unsigned char* to = tile + (ch >> 2) * G::PANEL + r * 128;
-                const int c0 = ((ch & 3) * 2 ^ (r & 7)) << 4, c1 = c0 ^ 16;
+                // A row's 16-byte pieces become two each.  Eight lanes store to one panel's halves of two rows: the
+                // swizzle gives them all the banks.
+                const int r = D == 128 ? (ptid >> 4) * 2 + (ptid >> 2 & 1) : ptid / G::CPR, ch = D == 128 ? (ptid >> 1 & 4) + (ptid & 3) : ptid % G::CPR;
+                if (ptid < G::PASS_THREADS) {
+                    from += r * G::ROWB + ch * 16;
+                    unsigned char* to = tile + (ch >> 2) * G::PANEL + r * 128;
+                    const int c0 = ((ch & 3) * 2 ^ (r & 7)) << 4, c1 = c0 ^ 16;
 #pragma unroll 4
-                for (int i = 0; i < kWideTile / G::PASS; ++i) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(from + i * G::PASS * G::ROWB);
-                    uint32_t a[2], b[2], e[2], f[2];
-                    C::expand(x.x, a);
-                    C::expand(x.y, b);
-                    C::expand(x.z, e);
-                    C::expand(x.w, f);
-                    *reinterpret_cast<uint4*>(to + c0 + i * G::PASS * 128) = make_uint4(a[0], a[1], b[0], b[1]);
-                    *reinterpret_cast<uint4*>(to + c1 + i * G::PASS * 128) = make_uint4(e[0], e[1], f[0], f[1]);
+                    for (int i = 0; i < kWideTile / G::PASS; ++i) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(from + i * G::PASS * G::ROWB);
+                        uint32_t a[2], b[2], e[2], f[2];
+                        C::expand(x.x, a);
+                        C::expand(x.y, b);
+                        C::expand(x.z, e);
+                        C::expand(x.w, f);
+                        *reinterpret_cast<uint4*>(to + c0 + i * G::PASS * 128) = make_uint4(a[0], a[1], b[0], b[1]);
+                        *reinterpret_cast<uint4*>(to + c1 + i * G::PASS * 128) = make_uint4(e[0], e[1], f[0], f[1]);
+                    }
                 }
-            }
-            if (mend) {  // rows behind the last one, without a page, or noted become zeros, so that 0 * NaN never happens
+                if (mend) {  // rows behind the last one, without a page, or noted become zeros, so that 0 * NaN never happens
+                    meet();
+                    const uint32_t* odd = odd_rows + at_slot * 4;
+                    const int begin = groups ? 0 : max(0, (careful && (odd[0] | odd[1] | odd[2] | odd[3]) ? min(U.base, U.lim) : U.lim) - row0);
+                    for (int id = begin * (D / 8) + ptid; id < kWideTile * (D / 8); id += G::HELP) {
+                        const int rr = id / (D / 8), cc = id % (D / 8);
+                        if (row0 + rr >= U.lim || (groups >> (rr >> 4) & 1) || (careful && (odd[rr >> 5] >> (rr & 31) & 1)))
+                            *reinterpret_cast<uint4*>(tile + (cc >> 3) * G::PANEL + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                fence_proxy_async();
                 meet();
-                const uint32_t* odd = odd_rows + at_slot * 4;
-                const int begin = groups ? 0 : max(0, (careful && (odd[0] | odd[1] | odd[2] | odd[3]) ? min(U.base, U.lim) : U.lim) - row0);
-                for (int id = begin * (D / 8) + ptid; id < kWideTile * (D / 8); id += G::HELP) {
-                    const int rr = id / (D / 8), cc = id % (D / 8);
-                    if (row0 + rr >= U.lim || (groups >> (rr >> 4) & 1) || (careful && (odd[rr >> 5] >> (rr & 31) & 1)))
-                        *reinterpret_cast<uint4*>(tile + (cc >> 3) * G::PANEL + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                if (ptid == 0 && ok) {
+                    mbar_arrive(b_full + 8 * at_slot);
+                    mbar_arrive(b_raw_free + 8 * group);
                 }
             }
-            fence_proxy_async();
-            meet();
-            if (ptid == 0 && ok) {
-                mbar_arrive(b_full + 8 * at_slot);
-                mbar_arrive(b_raw_free + 8 * group);
-            }
-        }
         }
     } else if (w == 8) {
         // ------------------------------------------------------------------ the products
@@ -444,7 +444,8 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                         scores(0, i & 1, slot, 0);
                         tm_commit(lead, b_empty + 8 * slot);
                     }
-                    if (i + 2 == n - 1) tm_commit(lead, b_q_free);  // the unit's last scores
+                    // behind the unit's last scores, and behind probabilities of both streams, which have read the rows' factors by then
+                    if (i == max(n - 3, 0)) tm_commit(lead, b_q_free);
                 }
             } else {
                 // step j: products with half j of the V tiles, and the scores of half j + 2
@@ -470,7 +471,7 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                     if (!ok) break;
                     if (has_v && (j & 1)) tm_commit(lead, b_empty + 8 * v_slot);
                     if (has_k && (j & 1)) tm_commit(lead, b_empty + 8 * k_slot);
-                    if (j + 2 == 2 * n - 1) tm_commit(lead, b_q_free);
+                    if (j == max(2 * n - 3, 0)) tm_commit(lead, b_q_free);  // (see above)
                 }
             }
         }

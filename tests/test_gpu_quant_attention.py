@@ -492,3 +492,30 @@ def test_forked_pages_with_their_scales(binding):
     for b, rows in enumerate(both):
         off = (K[b, :, :rows.shape[1]] - rows.double()).abs()
         assert (off <= cache.K_scale[b].double().repeat_interleave(R, -1)[:, :rows.shape[1], None] * 1.01).all()
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nb", [4, 512])
+def test_many_short_units_of_many_query_rows(binding, form, D, nb):
+    """Units of one or two tiles one behind the other in a CTA, whose query rows differ in size: each keeps its own factors."""
+    B, H, G, T, page, R = 96, 6, 4, 40, 64, 64
+    rng = random.Random(nb)
+    lens = [rng.choice([40, 100, 128, 129, 200, 256]) for _ in range(B)]
+    c = case(binding, (form, BF16), B, H, G, D, 256, T, R, seed=D + nb, lens=lens, spread=1.0)
+    c["Q"] *= torch.exp2(-torch.randint(0, 12, (B, T, H * G, 1), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).float()).to(BF16)
+    want = reference(c)
+    cache, pages = c["cache"], B * 4
+    used = torch.randperm(pages, generator=torch.Generator().manual_seed(2)).view(B, 4).to(torch.int32).to(DEV)
+    table = torch.full((B, nb), -1, dtype=torch.int32, device=DEV)
+    table[:, :4] = used
+    scales = torch.full((2, B, H, nb), float("nan"), device=DEV)
+    scales[0, :, :, :4], scales[1, :, :, :4] = cache.K_scale, cache.V_scale
+    paged = binding.QuantCache(QU.pool_of(cache.K, page, used, pages), QU.pool_of(cache.V, page, used, pages), scales[0], scales[1], block_rows=R)
+    first = None
+    for _ in range(5):
+        got = c["plan"].attend_quant_paged(c["Q"], paged, table, c["seq"], c["ws"], draft_len=c["draft"], tree_mask=c["mask"], want_lse=True)
+        assert c["plan"].read_status(c["ws"])[0] == 0
+        first = first or got
+        assert torch.equal(got["out"], first["out"]) and torch.equal(got["lse"], first["lse"])
+    QU.assert_attention(first, want)
