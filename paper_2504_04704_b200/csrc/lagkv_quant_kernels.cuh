@@ -352,7 +352,7 @@ lagkv_quant_write_kernel(const __grid_constant__ QuantParams P) {
                     }
                 }
             }
-            if (older && s > was && was > 0.f) quant_again<FORM>(to, P.ss, P.D / 16, a - start, was, s, t, GT);
+            if (older && s > was) quant_again<FORM>(to, P.ss, P.D / 16, a - start, was, s, t, GT);
         }
         if (++stage == kQuantStages) stage = 0;
     }

@@ -49,7 +49,7 @@ def write64(code, scale, X, start, end, R, form):
         if lo < start:
             was = float(scale[j])
             s = max(s, was)
-            if s > was and was > 0:
+            if s > was:
                 code[lo:start] = nearest(code[lo:start] * was / s, form)
         scale[j] = s
         x = torch.where(torch.isnan(x), 0.0, x).clamp(-TOP[form] * s, TOP[form] * s)

@@ -361,3 +361,19 @@ def test_rows_far_into_a_cache(binding):
     idx = torch.arange(e - 40, e, dtype=torch.int32, device=DEV).view(1, 1, 40)
     assert torch.equal(plan.quant_read(cache, i32([e]), ws, idx=idx)[0][0, 0], x[0, 0, e - 40:e])
     assert plan.read_status(ws)[0] == 0
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+def test_older_rows_under_a_scale_of_zero_stay_zero(binding, form):
+    """A scale of 0 makes every code stand for 0, codes of another writer too: they become codes of 0 when the scale grows."""
+    B, H, S, D, R = 2, 2, 64, 64, 32
+    g, K, V, ks, vs = start_state(B, H, S, D, form, R, seed=4)
+    ks[:, 0], vs[:, 1] = 0.0, 0.0
+    x = torch.randn((2, B, H, 20, D), generator=g, device=DEV).to(BF16)
+    plan, cache = binding.Plan(B, H, D, sink=4, lag=64), binding.QuantCache(K, V, ks, vs, block_rows=R)
+    ws = plan.new_workspace()
+    want = expected(K, V, ks, vs, x[0], x[1], [10, 33], [30, 50], R, form)
+    plan.quant_write(cache, x[0], x[1], i32([30, 50]), ws, from_len=i32([10, 33]))
+    assert plan.read_status(ws)[0] == 0
+    same(cache, want)
+    assert not cache.K[0, 0, :10].float().any() and not cache.V[1, 1, 32:33].float().any()
