@@ -535,7 +535,8 @@ int lagkv_quant_read_paged(lagkv_plan_t plan, const lagkv_quant_cache *cache, co
  * count on top of the block scales), results and errors.  cap > 0 (2^-100 at least): every logit x becomes cap*tanh(x/cap); 0: none.
  * Products are in fp16 (codes are exact in it) with fp32 sums; bf16 queries enter as fp16 after a power of two per row,
  * as over fp8 caches.  K scales multiply the fp32 logits; V scales multiply the probabilities before these are rounded to
- * fp16, relative to a power of two near the largest scale seen: a row whose scale is 2^-20 of that one or less loses bits.
+ * fp16, relative to a power of two near the largest V scale seen: a row whose probability (of the largest one) times its scale
+ * is below 2^-22 of that scale loses bits, 2^-32 of the scale times its code at most.
  * One launch for few short caches, else two; which kernels serve a call goes by its sizes and capacity, not by the lengths.
  * Workspace: lagkv_attend_quant_workspace_bytes() (0 = bad arguments), cleared once with
  * lagkv_attend_workspace_init(); it serves every smaller call, one at a time.

@@ -15,7 +15,10 @@
 // of a product is free as long as both sides agree.  A word of four channels of one row is two fragments of a
 // score product; words of two rows, their bytes paired, are two of an output product.  Probabilities get from the layout of results to
 // that of operands by movmatrix.
-// Bound by HBM: a tile of 32 rows of 128 channels (8 KB) costs a warp some 300 instructions (e4m3) or 480 (int8).
+// Bound by HBM: a tile of 32 rows of 128 channels (8 KB) costs a warp some 300 instructions (e4m3) or 480 (int8).  One token,
+// 32 x 8 heads of up to 32768 int8 rows of 128 channels: 265 us, 95 % of the copy rate; 16 x 4 heads of up to 16384 rows in pages of 64:
+// 43.3 us where the bytes take 31.5, the rest is start, tail and joining.  Units of 16 and 32 query rows: bound by issue, 6 x 4
+// heads of up to 16411 rows of 64 channels under 35 capped query rows 50 us (bytes 6.1).
 //
 // Calls of few units (a user or two) take the form with a cluster of CTAs for each unit, which join what they have found through
 // distributed shared memory: one launch, no partials in memory (1 x 8 x 1216 int8 rows 7.6 us instead of 9.5).
@@ -190,6 +193,8 @@ lagkv_attend_quant_kernel(const __grid_constant__ QuantAttendParams P) {
         sh.pos = 0;
         sh.end = 1;
     } else {
+        // the joining kernel comes up beside the tail and waits for the partials: 43.3 us instead of 43.8 for the pages above
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
         sh = attend_share<G::NT>(P, upb, sscan);
     }
     while (sh.pos < sh.end) {

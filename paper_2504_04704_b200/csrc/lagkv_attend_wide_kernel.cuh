@@ -18,7 +18,7 @@
 // under 64 tokens in 270 us, tensor cores 49 %): of some 5200 cycles a step the products need 2850 and the 2 x 16384
 // exponentials, 16 a cycle, 2050 beside them; the rest is the softmax warps, two to a scheduler, waiting for one
 // part of their scores after the other.  fp8 caches: the way of a tile through shared memory, landed, widened and
-// multiplied, with three slots for widened tiles and three or four places to land in at 128 and 96 channels (8 x 8 x
+// multiplied, with three slots for widened tiles at 128 and 96 channels and a place to land in for each group of helpers (8 x 8 x
 // 19968 rows under 13 tokens in 123 us where HBM takes 41).
 #pragma once
 #include <cuda.h>
@@ -34,7 +34,6 @@ constexpr int kWideRowFlags = 32;     // loads whose missing rows are remembered
 template <int D_, int DT_, int MT_>
 struct WideGeo {
     static constexpr int D = D_, DT = DT_, MT = MT_;  // MT = 1: streams split the rows, 2: the query rows
-    static constexpr bool NAN_ROWS = true;             // rows may hold values that are not finite
     static constexpr int EB = Elem<DT_>::EB;
     static constexpr int ROWB = D * EB, CPR = ROWB / 16;
     static constexpr int PANELS = (D + 63) / 64;       // 64 channels of 16 bits: 128-byte rows, swizzled
@@ -224,8 +223,7 @@ __device__ __forceinline__ float largest_of(const uint4& v) {
 // The queries of a unit into swizzled shared memory (`to`), 32 rows at a time by warp `warp` of `warps`: a lane
 // finds its row's place once, all lanes copy.
 template <class G>
-__device__ __forceinline__ void load_queries(const AttendParams& P, const WideUnit& U, int b, unsigned char* to, int warp, int warps,
-                                             bool copy = G::DT != 2) {
+__device__ __forceinline__ void load_queries(const AttendParams& P, const WideUnit& U, int b, unsigned char* to, int warp, int warps) {
     constexpr int D = G::D, CH = D / 8;  // 16-byte pieces of a row
     const int lane = threadIdx.x & 31;
     const uint16_t* q0 = P.Q + (long long)b * P.q_sb + (long long)(U.h * P.G) * P.q_sh;
@@ -236,7 +234,7 @@ __device__ __forceinline__ void load_queries(const AttendParams& P, const WideUn
     for (int r0 = warp * 32; r0 < G::MT * kWideTile; r0 += warps * 32) {
         const int row = U.m0 + r0 + lane;
         const long long off = r0 + lane < U.mrows ? (long long)(row / P.G) * P.q_st + (long long)(row % P.G) * P.q_sh : -1;
-        if (copy) {
+        if constexpr (G::DT != 2) {
 #pragma unroll 4
             for (int k = 0; k < CH; ++k) {
                 const int id = k * 32 + lane, r = r0 + id / CH, ch = id % CH;
@@ -297,7 +295,7 @@ struct WideCursor {
     // a V tile with rows that enter as zeros, or that may
     __device__ __forceinline__ bool mend(uint32_t missing) const { return missing || careful() || row0() + kWideTile > U.lim; }
     // drafted V rows that are not finite are kept out of the tile
-    __device__ __forceinline__ bool careful() const { return G::NAN_ROWS && U.masked && is_v() && row0() + kWideTile > U.base; }
+    __device__ __forceinline__ bool careful() const { return U.masked && is_v() && row0() + kWideTile > U.base; }
 };
 
 template <int D, int DT, int MT>

@@ -12,7 +12,8 @@
 // One read of the new rows: a group of threads fetches a block's new rows to shared memory (eight 16-byte pieces a thread, which
 // nobody else reads, so that there is no barrier but the one of the reduction), two blocks ahead, finds the largest magnitude
 // as integers (16-bit floats without their sign are ordered like them) and encodes.  Bound by HBM: 2 bytes read and 1
-// written an element.
+// written an element; 32 x 8 heads of 9728 rows of 128 channels in 316 us (int8) and 289 (e4m3) where the copy rate takes 292; kept rows by
+// a list, 256 bytes at random places, 401 and 381.  (Registers only, 2-4 CTAs an SM: 610 and more.)
 //
 // Reading back: code * s in fp32, rounded to 16 bits; values that 16 bits do not hold become the largest that they do.
 #pragma once
