@@ -18,6 +18,7 @@
 #pragma once
 #include "lagkv_attend_quant_kernels.cuh"
 #include "lagkv_attend_wide_kernel.cuh"
+#include "lagkv_wide_walk.h"
 
 namespace lagkv {
 
@@ -212,15 +213,19 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
     auto at_s = [&](int s, int p) { return tm + (MT == 1 ? p * 128 + s * 64 : s * 128 + p * 64); };
     auto at_o = [&](int s) { return tm + 256 + s * D; };
     bool ok = true;
-    // The task told in turn `k`, once it is; false: the last one is behind, or a wait was given up.
-    auto next_task = [&](uint32_t k, WideView& U) {
-        if (!ok || !wide_wait(b_task + 8 * (k % kWideTasks), k / kWideTasks & 1)) {
-            if (ok && lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
-            return ok = false;
-        }
+    // The task told in turn `k`, once it is; false: the last one is behind, or a wait was given up.  `agree`: see wide_go_on();
+    // all threads of the barriers inside a task.
+    auto next_task = [&](uint32_t k, WideView& U, auto&& agree) {
+        auto told = [&]() {
+            if (wide_wait(b_task + 8 * (k % kWideTasks), k / kWideTasks & 1)) return true;
+            if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
+            return false;
+        };
+        if (!wide_go_on(ok, told, agree)) return false;
         U = wide_view(P, tasks[k % kWideTasks], MT * kWideTile);
         return U.n > 0;
     };
+    auto alone = [](bool mine) { return mine; };
 
     if (w == 9) {
         // ------------------------------------------------------------------ K and V tiles: a box per page, a lane each
@@ -294,8 +299,8 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
     } else if (w > 9) {
         // ------------------------------------------------------------------ help: queries, and tiles widened, a group every GROUPS-th
         const int group = (w - 10) / 2, ptid = tid - 10 * 32 - group * G::HELP;
-        // after a wait that ran out the walk goes on to its end without waiting, so that the barrier among these
-        // warps still matches
+        // after a wait that ran out this warp goes on to the end of its task without waiting, so that it comes to every barrier of
+        // its group: how many a tile has follows from the task alone.  Then the group leaves together.
         auto wait = [&](uint32_t bar, uint32_t parity) {
             if (ok && !wide_wait(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
@@ -303,10 +308,11 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
             }
         };
         auto meet = [&]() { named_bar_sync(2 + group, G::HELP); };
+        auto agree = [&](bool mine) { return !named_bar_or(2 + group, G::HELP, !mine); };
         uint32_t lap = 0, slot_lap = 0, c = 0;  // how often this group's place and the load's slot have been through; loads before
         int turn = 0, slot = 0;
         WideView U;
-        for (uint32_t task = 0; next_task(task, U); ++task) {
+        for (uint32_t task = 0; next_task(task, U, agree); ++task) {
             // the task's queries, once the products with those before are done
             if (task > 0) wait(b_q_free, (task - 1) & 1);
             quant_load_queries<G>(P, tasks + task % kWideTasks, smem, q_factors, task > 0 ? w - 10 : w - 2, 2 * G::GROUPS + (task > 0 ? 0 : 8));
@@ -329,7 +335,7 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
                 wait(b_land + 8 * group, at_lap & 1);
                 const uint32_t groups = is_v ? gone[c % kWideRowFlags] : 0u;
                 const bool careful = G::NAN_ROWS && is_v && U.masked && row0 + kWideTile > U.base;
-                const bool mend = is_v && (groups || careful || row0 + kWideTile > U.lim);
+                const bool mend = is_v && (P.block_table != nullptr || careful || row0 + kWideTile > U.lim);
                 unsigned char* tile = smem + (s_ring - sbase) + at_slot * G::SLOT;
                 if (at_slot_lap > 0) wait(b_empty + 8 * at_slot, (at_slot_lap + 1) & 1);
                 const unsigned char* from = smem + (s_raw - sbase) + group * G::RAW;
@@ -426,7 +432,7 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
             tm_commit(lead, b_o + 8 * s);
         };
         WideView U;
-        for (uint32_t task = 0; next_task(task, U); ++task) {
+        for (uint32_t task = 0; next_task(task, U, alone); ++task) {
             const int n = __shfl_sync(~0u, U.n, 0);
             if (!wait(task > 0 ? b_q : b_q_first, task > 0 ? (task - 1) & 1 : 0)) break;
             if constexpr (MT == 1) {
@@ -485,15 +491,17 @@ lagkv_attend_quant_wide_kernel(const __grid_constant__ QuantAttendParams P, cons
         const uint32_t t_o = at_o(s) + lanes;
         uint32_t ns = 0, items = 0, c0 = 0;  // parities of the scores (a bit per place); items and loads of the units before
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            // after a wait that ran out the barriers among these warps go on, everything else stops
+            // after a wait that ran out the barriers of this task go on, everything else stops; then all these warps leave together
             if (ok && !wide_wait(bar, parity)) {
                 if (lane == 0) record_status(P.status, ST_ETIMEOUT, blockIdx.x);
                 ok = false;
             }
             tm_fence_after();
         };
+        // up to 128 query rows: the streams meet to join their results; else no warp waits for another at a barrier
+        auto agree = [&](bool mine) { return MT == 1 ? !named_bar_or(1, 256, !mine) : mine; };
         WideView U;
-        for (uint32_t task = 0; next_task(task, U); ++task) {
+        for (uint32_t task = 0; next_task(task, U, agree); ++task) {
             const WideTask& told = tasks[task % kWideTasks];
             if (task == 0) {  // the first queries
                 quant_load_queries<G>(P, &told, smem, q_factors, w, 8 + 2 * G::GROUPS);
