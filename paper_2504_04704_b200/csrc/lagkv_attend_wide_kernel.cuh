@@ -508,7 +508,9 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
                 landed ^= 1u << slot;
             }
             if (DT == 2 && at.is_v()) groups = gone[at.c % kWideRowFlags];
-            const bool mend = at.is_v() && at.mend(groups), careful = at.careful();
+            // fp8: `groups` is what the fetching warp has left, which two warps of a group may read differently once a wait has run
+            // out; whether they meet must not depend on it
+            const bool mend = at.is_v() && at.mend(DT == 2 ? P.block_table != nullptr : groups), careful = at.careful();
             unsigned char* tile = smem + (s_ring - sbase) + slot * G::SLOT;
             auto piece = [&](int id) {
                 constexpr int CPR16 = D / 8;
