@@ -49,9 +49,11 @@ struct WideGeo {
     static constexpr int PASS = HELP / CPR & ~7, PASS_THREADS = PASS * CPR;
     static constexpr int MISC = 1024;
     static constexpr int RAW = DT_ == 2 ? kWideTile * ROWB : 0;  // an fp8 tile as it is stored ...
-    // ... and how many are in flight: one for each group of helpers.  A place that groups took in turns could be waited for by
-    // a group one lap ahead of a copy that is late, and a parity does not tell that lap from the one before.
-    static constexpr int RS = DT_ == 2 ? GROUPS : 0;
+    // ... and how many are in flight: one or two for each group of helpers, which takes its own in turn.  A place that groups took in
+    // turns could be waited for by a group one lap ahead of a copy that is late, and a parity does not tell that lap from the one before.
+    // Two at 64 channels, where all eight slots still fit: 16 x 8 x 8192 rows under 64 query rows 86.5 us, 93.5 with one, 8 x 8 x 16384
+    // under 256 query rows 110.4 and 109.2, so one there.
+    static constexpr int RS = DT_ != 2 ? 0 : D_ == 64 && MT_ == 1 ? 2 * GROUPS : GROUPS;
     static constexpr int NS_FIT = (232448 - 1024 - MISC - QBYTES - RS * RAW) / SLOT;
     static constexpr int NS = NS_FIT > 8 ? 8 : NS_FIT;           // tiles of K or V in the ring
     static constexpr int CHUNKS = kWideTile * CPR;               // 16-byte pieces of a stored tile
@@ -314,8 +316,8 @@ lagkv_attend_wide_kernel(const __grid_constant__ AttendParams P, const __grid_co
     float* exch = reinterpret_cast<float*>(smem + G::SLOT);  // MT = 1
     // misc: barriers (tile ready, place free, landed but not ready; scores, probabilities twice, O; queries in
     // place, their place free), the rows of each V tile that are not finite, the missing 16-row groups of each
-    // load, scheduling scratch
-    const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_land = b_empty + 8 * 8, b_raw_free = b_land + 4 * 8, b_s = b_land + 8 * 8,
+    // load, scheduling scratch, barriers (places to land in free)
+    const uint32_t b_full = s_misc, b_empty = b_full + 8 * 8, b_land = b_empty + 8 * 8, b_raw_free = s_misc + 768, b_s = b_land + 8 * 8,
                    b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_q = b_o + 16, b_q_free = b_q + 8;
     uint32_t* odd_rows = reinterpret_cast<uint32_t*>(misc + 288);                     // [8][4]
     volatile uint32_t* gone = reinterpret_cast<volatile uint32_t*>(misc + 416);       // [kWideRowFlags]
