@@ -269,7 +269,9 @@ class QuantCache:
     """A cache in 8 bits with block scales (``lagkv_quant_cache``): codes ``K``, ``V`` as ``torch.int8`` or
     ``torch.float8_e4m3fn``, ``[B, H, S_cap, D]`` or pools ``[num_pages, H, page_size, D]``, and their scales
     ``K_scale``, ``V_scale``, fp32 ``[B, H, blocks]``, one for each ``block_rows`` rows of a sequence (of the
-    sequence on paged caches too: a fork copies its scales along with its table row)."""
+    sequence on paged caches too: a fork copies its scales along with its table row).  The tensors are taken for good: what is
+    in them may change, but attributes cannot be assigned, and a tensor whose memory was exchanged (``set_``, ``resize_``,
+    ``.data``) is refused by every call.  Other tensors need another ``QuantCache``."""
 
     def __init__(self, K, V, K_scale, V_scale, block_rows=64):
         if K.dtype not in _QUANT_FORMATS or V.dtype != K.dtype or K.shape != V.shape or K.dim() != 4 or K.device != V.device:
@@ -277,15 +279,22 @@ class QuantCache:
         for t in (K_scale, V_scale):
             if t.dtype != torch.float32 or t.dim() != 3 or t.shape != K_scale.shape or not t.is_contiguous() or t.device != K.device:
                 raise TypeError("K_scale and V_scale must be contiguous fp32 tensors [B, H, blocks] on the codes' device")
-        self.K, self.V, self.K_scale, self.V_scale, self.block_rows = K, V, K_scale, V_scale, int(block_rows)
-        self.strides = _dense_strides(K, "K")
-        if _dense_strides(V, "V") != self.strides:
+        block_rows, strides = int(block_rows), _dense_strides(K, "K")
+        if _dense_strides(V, "V") != strides:
             raise TypeError("K and V must have the same strides")
-        # what the calls of a decode step compare
-        self.device, self.shape, self.scale_shape, self.rows = K.get_device(), tuple(K.shape), tuple(K_scale.shape), K.shape[2]
-        self.arg = lagkv_quant_cache(K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr(), _QUANT_FORMATS[K.dtype],
-                                     self.block_rows, K_scale.shape[2], *self.strides)
-        self.ref = ctypes.byref(self.arg)
+        addresses = (K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
+        arg = lagkv_quant_cache(*addresses, _QUANT_FORMATS[K.dtype], block_rows, K_scale.shape[2], *strides)
+        # the tensors, and what the calls of a decode step pass and compare
+        self.__dict__.update(
+            K=K, V=V, K_scale=K_scale, V_scale=V_scale, block_rows=block_rows, strides=strides, device=K.get_device(),
+            shape=tuple(K.shape), scale_shape=tuple(K_scale.shape), rows=K.shape[2], arg=arg, ref=ctypes.byref(arg),
+            addresses=addresses, address_of=(K.data_ptr, V.data_ptr, K_scale.data_ptr, V_scale.data_ptr))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: a QuantCache keeps its tensors; make another one for others")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
 
 
 class Plan:
@@ -768,6 +777,9 @@ class Plan:
             raise TypeError(f"the cache must be [{B}, {H}, S_cap, {D}], or pages [num_pages, {H}, page_size, {D}], with scales [{B}, {H}, blocks]")
         if paged and any(cache.strides):
             raise TypeError("paged codes must be contiguous")
+        a, b, c, d = cache.address_of
+        if (a(), b(), c(), d()) != cache.addresses:
+            raise TypeError("a tensor of the cache has other memory than when the QuantCache was made: make another one")
         return cache.ref
 
     def _quant_source(self, K, V, from_len, seq_len, take, at_positions):

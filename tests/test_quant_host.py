@@ -81,3 +81,33 @@ def test_tensors_elsewhere_are_refused(binding):
         plan.quant_read(cache, n, ws, K_out=x)
     with pytest.raises(TypeError):
         plan.attend_quant(x.transpose(1, 2).contiguous(), cache, n, ws)
+
+
+def test_cache_object_keeps_its_tensors(binding):
+    """What a call passes is what the attributes name: nothing can be assigned, and memory that was exchanged is refused."""
+    plan = binding.Plan(1, 2, 128, 4, 64, device=-1)
+    cache = cpu_cache(binding)
+    was = bytes(cache.arg)
+    for name in ("K", "V", "K_scale", "V_scale", "block_rows", "rows", "shape", "arg", "other"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name, 1))
+    with pytest.raises(AttributeError):
+        del cache.K_scale
+    with pytest.raises(AttributeError):                            # sequences in another order, as a batch's slots change hands
+        cache.K_scale = cache.K_scale[torch.zeros(1, dtype=torch.long)]
+    assert bytes(cache.arg) == was and cache.arg.K == cache.K.data_ptr() and cache.arg.K_scale == cache.K_scale.data_ptr()
+    cache.K.add_(1)
+    cache.K_scale.fill_(2.0)
+    assert plan._check_quant(cache, False) is cache.ref and plan._check_quant(cache, True) is cache.ref
+    for name in ("K", "V", "K_scale", "V_scale"):
+        cache = cpu_cache(binding)
+        t = getattr(cache, name)
+        t.resize_((1, 2, 4 * t.shape[2]) + t.shape[3:])            # a pool that grows
+        for paged in (False, True):
+            with pytest.raises(TypeError):
+                plan._check_quant(cache, paged)
+        cache = cpu_cache(binding)
+        t = getattr(cache, name)
+        t.data = t.clone()
+        with pytest.raises(TypeError):
+            plan._check_quant(cache, False)
