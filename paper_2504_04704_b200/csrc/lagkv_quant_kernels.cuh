@@ -248,12 +248,12 @@ lagkv_quant_write_kernel(const __grid_constant__ QuantParams P) {
     uint8_t* codes = P.codes[which];
     float* scales = P.scale[which] + ((long long)b * P.H + h) * P.blocks;
     auto place = [&](int stage, int k) { return ring + (stage * kQuantPieces + k) * G::NT + tid; };
-    int row[kQuantPieces];  // take: rows of the source for the block that is fetched next, looked up a block ahead; -1: none
+    int row[kQuantPieces];  // take: rows of the source for the block that is fetched next, looked up a block ahead and not looked at before
     auto look = [&](int j) {
         if (take == nullptr) return;
         const int i0 = max(from, j << P.block_shift) + r0 - from, e = j < blocks ? min(seq, (j + 1) << P.block_shift) - from : 0;
 #pragma unroll
-        for (int k = 0; k < kQuantPieces; ++k) row[k] = r0 < pass && i0 + k * pass < e ? __ldg(take + i0 + k * pass) : -2;
+        for (int k = 0; k < kQuantPieces; ++k) row[k] = r0 < pass && i0 + k * pass < e ? __ldg(take + i0 + k * pass) : 0;
     };
     auto fetch = [&](int j, int stage) {
         if (j < blocks) {
@@ -263,8 +263,9 @@ lagkv_quant_write_kernel(const __grid_constant__ QuantParams P) {
             for (int k = 0; k < kQuantPieces; ++k) {
                 bool ok = r0 < pass && i0 + k * pass < e;  // what is not there becomes zeros
                 if (take) {
-                    ok = row[k] >= 0 && row[k] < P.T;
-                    if (!ok && row[k] != -2) record_status(P.status, ST_EINVAL, b);
+                    const bool in = row[k] >= 0 && row[k] < P.T;
+                    if (ok && !in) record_status(P.status, ST_EINVAL, b);
+                    ok = ok && in;
                     p = src + (long long)row[k] * P.r_st + piece * 8;
                 }
                 asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(smem_u32(place(stage, k))), "l"(ok ? p : src), "r"(ok ? 16 : 0)

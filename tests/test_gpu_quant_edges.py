@@ -1,0 +1,37 @@
+"""Caches in 8 bits with block scales: calls at the edges of what the header promises, every kernel family at odd layouts."""
+import pytest
+import torch
+
+import quant_util as QU
+import test_gpu_quant_attention as A
+import test_gpu_quant_cache as W
+from test_gpu_quant_attention import BF16, DEV, FP16, ROOM, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2504_04704_b200 import binding as b
+    b.load_library()
+    return b
+
+
+@pytest.mark.parametrize("bad", [-1, -2, -3, -2 ** 31, 40, 2 ** 31 - 1])
+def test_every_entry_outside_the_source_is_recorded(binding, bad):
+    """Whatever number it is: recorded, and its row is 0."""
+    D, R, T, n = 64, 32, 40, 50
+    g, K, V, ks, vs = W.start_state(1, 2, 64, D, "int8", R, seed=1)
+    x = torch.randn((2, 1, 2, T, D), generator=g, device=DEV).to(BF16)
+    plan, cache = binding.Plan(1, 2, D, sink=4, lag=64), binding.QuantCache(K, V, ks, vs, block_rows=R)
+    ws = plan.new_workspace()
+    take = torch.randint(0, T - 1, (1, n), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    pick = take.clone()
+    take[0, 7], pick[0, 7] = bad, T - 1
+    clean = x.clone()
+    clean[:, :, :, T - 1] = 0                                      # the statement's stand-in for a row that is not there
+    want = W.expected(K, V, ks, vs, clean[0], clean[1], [3], [3 + n], R, "int8", lambda b, h, i: int(pick[0, i]))
+    plan.quant_write(cache, x[0], x[1], i32([3 + n]), ws, from_len=i32([3]), take=take.to(DEV))
+    assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL
+    W.same(cache, want)
+    assert not cache.K[0, :, 10].any()
