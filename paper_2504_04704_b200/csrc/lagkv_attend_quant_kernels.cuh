@@ -479,13 +479,13 @@ lagkv_attend_quant_kernel(const __grid_constant__ QuantAttendParams P) {
                 for (int k = 0; k < 4; ++k) G::load_v(x[k], tv, 16 * m + 2 * t + (k & 1) + 8 * (k >> 1), g);
                 if (FORM == FORM_E4M3 && draft) {
                     // Drafted rows that are NaN must reach the tokens that see them and no others, so not through 0 * NaN:
-                    // such codes leave the tile, and the results of those who see them become NaN.
+                    // such codes leave the tile, and the results of those who see them become NaN (all, for rows before the draft).
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
                         for (int v = 0; v < VW; ++v) x[k][v] &= ~C::nan_bytes(x[k][v]);
 #pragma unroll 1
-                    for (int r = max(0, base - r0 - 16 * m); r < min(16, lim - r0 - 16 * m); ++r) {
+                    for (int r = 0; r < min(16, lim - r0 - 16 * m); ++r) {
                         uint32_t y[VW];
                         G::load_v(y, tv, 16 * m + r, g);
                         bool odd = false;
@@ -497,7 +497,7 @@ lagkv_attend_quant_kernel(const __grid_constant__ QuantAttendParams P) {
                         for (int n = 0; n < NQ; ++n)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                if (!(smask[8 * n + 2 * t + e] >> (j & 63) & 1)) continue;
+                                if (j >= 0 && !(smask[8 * n + 2 * t + e] >> (j & 63) & 1)) continue;
 #pragma unroll
                                 for (int v = 0; v < VW; ++v)
 #pragma unroll

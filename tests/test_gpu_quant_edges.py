@@ -35,3 +35,22 @@ def test_every_entry_outside_the_source_is_recorded(binding, bad):
     assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL
     W.same(cache, want)
     assert not cache.K[0, :, 10].any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("T,G,room", [(2, 1, 0), (7, 2, 0), (7, 4, 0), (2, 4, ROOM), (7, 4, ROOM), (40, 4, ROOM)])
+@pytest.mark.parametrize("tree", [True, False])
+def test_nan_in_rows_before_the_draft_reaches_every_token(binding, dtype, D, T, G, room, tree):
+    """e4m3 NaN in a row that every token sees, beside the draft in one tile or not."""
+    c = A.case(binding, ("e4m3", dtype), 3, 2, G, D, 180, T, 16, seed=3, lens=[150, T + 9, 128 + T], tree=tree, room=room)
+    base = [n - T for n in c["lens"]]
+    c["cache"].V.view(torch.uint8)[0, :, base[0] - 1, 3::5] = 0x7f
+    c["cache"].V.view(torch.uint8)[1, 0, base[1] - 9, 1] = 0xff
+    c["cache"].V.view(torch.uint8)[2, 1, base[2] - 20, D - 1] = 0x7f
+    got = A.run(c)
+    out, lse, t_out, t_lse = A.reference(c)
+    odd = torch.isnan(out)
+    assert odd.any(-1).any(-1).all(-1).all() and torch.equal(torch.isnan(got["out"]), odd)
+    zero = lambda x: torch.where(odd, 0.0, x)  # noqa: E731
+    QU.assert_attention(dict(got, out=zero(got["out"])), (zero(out), lse, zero(t_out), t_lse))
