@@ -109,6 +109,10 @@ __device__ __forceinline__ float odd_quotient(double a, float b) {
     return double(f) == q ? f : __int_as_float(__float_as_int(f) | 1);
 }
 
+// 1 / s; 0 for a scale of 0, and for one below 2^-126, which only another writer leaves and under which new rows are zeros: its
+// inverse may be infinite, and 0 times that is no code.
+__device__ __forceinline__ float quant_inverse(float s) { return s >= 0x1p-126f ? 1.f / s : 0.f; }
+
 // Eight codes of x / s (e4m3: s a power of two).  int8: x * inv decides, see quant_factor(); with EXACT the remainder does.
 template <int FORM, bool EXACT>
 __device__ __forceinline__ uint2 quant_encode(const float (&x)[8], float s, float inv) {
@@ -141,7 +145,7 @@ __device__ __forceinline__ uint2 quant_encode(const float (&x)[8], float s, floa
 // bit of the factor; the values of one that does are looked at one by one.  Warp-collective.
 template <int DT>
 __device__ __forceinline__ bool quant_factor(float s, int lane, float* inv) {
-    float f = s > 0.f ? 1.f / s : 0.f;
+    float f = quant_inverse(s);
     auto wrong = [&](int n) {  // 0: the value nearest to the border above n gets its code, else which way it is off
         const float border = (float(n) + 0.5f) * s;
         uint32_t r;
@@ -330,7 +334,7 @@ lagkv_quant_write_kernel(const __grid_constant__ QuantParams P) {
             if (odd || (FORM == FORM_E4M3 && (__float_as_int(s) & 0x7fffff))) {
                 quant_with_care<DT, FORM>(P, src, take, from, a - from, e - from, to + (long long)(a - start) * P.ss, s, t, GT);
             } else {
-                float inv = s > 0.f ? 1.f / s : 0.f;
+                float inv = quant_inverse(s);
                 const bool plain = FORM == FORM_E4M3 || quant_factor<DT>(s, tid & 31, &inv);
                 const int mine = r0 < pass ? (e - a - r0 + pass - 1) / pass : 0;  // pieces of this thread, if positive
                 uint8_t* out = to + (long long)(a - start + r0) * P.ss + piece * 8;

@@ -54,3 +54,25 @@ def test_nan_in_rows_before_the_draft_reaches_every_token(binding, dtype, D, T, 
     assert odd.any(-1).any(-1).all(-1).all() and torch.equal(torch.isnan(got["out"]), odd)
     zero = lambda x: torch.where(odd, 0.0, x)  # noqa: E731
     QU.assert_attention(dict(got, out=zero(got["out"])), (zero(out), lse, zero(t_out), t_lse))
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+def test_scales_of_other_writers_below_the_least_normal_number(binding, form):
+    """Zeros behind older rows under a scale of 1e-40 keep that scale and are codes of 0; other rows make it grow."""
+    D, R, H = 64, 32, 8
+    g, K, V, ks, vs = W.start_state(1, H, 64, D, form, R, seed=5)
+    tiny = torch.tensor([1e-40, 1.1e-40, 1.2e-40, 1.3e-40, 3e-40, 7e-40, 2e-39, 2.0 ** -127], dtype=torch.float32).to(DEV)
+    ks[0, :, 0], vs[0, :, 0] = tiny, tiny.flip(0)
+    assert (ks[0, :, 0] > 0).all()
+    x = torch.zeros((2, 1, H, 9, D), dtype=BF16, device=DEV)
+    plan, cache = binding.Plan(1, H, D, sink=4, lag=64), binding.QuantCache(K, V, ks, vs, block_rows=R)
+    ws = plan.new_workspace()
+    want = W.expected(K, V, ks, vs, x[0], x[1], [11], [20], R, form)
+    plan.quant_write(cache, x[0], x[1], i32([20]), ws, from_len=i32([11]))
+    W.same(cache, want)
+    assert not cache.K[0, :, 11:20].float().any()
+    x += torch.exp2(torch.arange(-133, -125, device=DEV).float()).to(BF16).view(1, 1, H, 1, 1)
+    want = W.expected(want[0][0], want[1][0], want[0][1], want[1][1], x[0], x[1], [20], [29], R, form)
+    plan.quant_write(cache, x[0], x[1], i32([29]), ws, from_len=i32([20]))
+    W.same(cache, want)
+    assert plan.read_status(ws)[0] == 0
