@@ -499,6 +499,7 @@ typedef struct {
  * s = max(f, its scale); where that is larger the older codes become code*(old scale)/s, rounded again.  The codes are those of
  * exact quotients.  Other blocks, and rows behind seq_len[b], stay as they are.
  * Values that are not finite: LAGKV_EINVAL is recorded; they do not count in a, infinities become the largest code, NaN 0.
+ * Under a scale of 0 every code is 0, that of an infinity too (a block whose new rows hold no finite value but zeros).
  * Refused (LAGKV_EINVAL recorded, the sequence untouched): lengths outside 0 <= from_len <= seq_len <= S_cap, more new
  * rows than T (take_rows), positions behind T with at_positions.  A take entry outside [0, T): recorded, that row is 0.
  * A page outside the pool: recorded, its block is left out.  No page may be written through two table entries.

@@ -76,3 +76,25 @@ def test_scales_of_other_writers_below_the_least_normal_number(binding, form):
     plan.quant_write(cache, x[0], x[1], i32([29]), ws, from_len=i32([20]))
     W.same(cache, want)
     assert plan.read_status(ws)[0] == 0
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_nothing_finite_but_zeros(binding, form, dtype):
+    """A block of infinities, NaN and zeros has a scale of 0, under which every code is 0; beside older rows theirs holds."""
+    D, R = 128, 16
+    g, K, V, ks, vs = W.start_state(1, 1, 64, D, form, R, seed=7)
+    x = torch.zeros((1, 1, 40, D), dtype=dtype, device=DEV)
+    x[0, 0, 0, 1], x[0, 0, 1, 2], x[0, 0, 20, 3], x[0, 0, 21, 4] = float("inf"), float("nan"), float("-inf"), float("nan")
+    plan, cache = binding.Plan(1, 1, D, sink=4, lag=64, dtype=dtype), binding.QuantCache(K, V, ks, vs, block_rows=R)
+    ws = plan.new_workspace()
+    want = W.expected(K, V, ks, vs, x, x, [5], [45], R, form)
+    was = float(ks[0, 0, 0])
+    plan.quant_write(cache, x, x, i32([45]), ws, from_len=i32([5]))
+    assert plan.read_status(ws)[0] == binding.LAGKV_EINVAL
+    W.same(cache, want)
+    assert float(cache.K_scale[0, 0, 0]) == was and float(cache.K[0, 0, 5, 1]) == QU.TOP[form]
+    assert float(cache.K_scale[0, 0, 1]) == 0 and not cache.K[0, 0, 16:45].float().any()
+    out = torch.full((1, 1, 64, D), 3.0, dtype=dtype, device=DEV)
+    plan.quant_read(cache, i32([45]), ws, from_len=i32([16]), K_out=out)
+    assert not out[0, 0, 16:45].any()
