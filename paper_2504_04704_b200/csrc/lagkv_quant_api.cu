@@ -9,6 +9,7 @@
 #include "lagkv_attend_quant_tables.h"
 #include "lagkv_plan.h"
 #include "lagkv_quant_kernels.cuh"
+#include "lagkv_quant_rules.h"
 
 using namespace lagkv;
 
@@ -196,36 +197,9 @@ const AttendEntry* quant_entry(int D, int format, int rows, int* index) {
     return nullptr;
 }
 
-// Which unit a call takes: the least of (time of a short call) + units per KV head * rows of all caches * (time per row), which
-// are what calls of 8 KV heads and 128 channels took, in us, 1 sequence of 256 and 16 of 8192 rows:
-//     unit              8           16           32          128
-//     int8         10    87     11    61    13    82     14   106      (16 query rows; 128: 36 query rows)
-//     e4m3         10    79     11    58    13    79     15   104
-//   64 query rows: 10.6 317   11.7  206   13.8  156     14.7 107     (int8)
-// A sequence costs some 384 rows more than it has (64 x 512 rows, 36 query rows: 91, 79, 82 and 51 us).  The time per row of the first three follows
-// the channels (64 of them: 61, 45, 60 and 94 us where 128 take 87, 61, 82 and 107); the cap costs the last one most (24 KV heads
-// of 16411 rows of 64 channels, 35 query rows: 52, 44, 48 and 73 us, uncapped the last one 55).
-// Units of 256 rows read K and V once for two of 128, but have two groups of helpers only: 64 tokens over 2 x 8 x 131072 int8
-// rows in 295 us against 313; 207 and 207 over 16 x 8 x 8192, 145 against 124 over 64 x 8 x 512 (e4m3 234 against 205: not built).
+// The kernel that a call takes.
 const AttendEntry* find_quant(const lagkv_config& c, int format, int query_rows, int64_t S_cap, bool capped, int* index) {
-    if (format == LAGKV_QUANT_INT8 && query_rows > 128 && S_cap >= 32768 && c.D <= 128) return quant_entry(c.D, format, 256, index);
-    const int units[4] = {8, 16, 32, 128};
-    const double base[4] = {9.3, 10.6, 13.0, 16.5}, per_row[4] = {37e-6, 56e-6, 77e-6, 99e-6};
-    const double rows = double(c.B) * c.H_kv * (double(S_cap) + 384.0), narrow = 0.5 + c.D / 256.0, wide = (0.8 + c.D / 640.0) * (capped ? 1.4 : 1.0);
-    const AttendEntry* best = nullptr;
-    double least = 0.0;
-    for (int i = 0; i < 4; ++i) {
-        int at;
-        const AttendEntry* e = quant_entry(c.D, format, units[i], &at);
-        if (e == nullptr) continue;  // 256 channels: 8 and 16
-        const double time = base[i] + ((query_rows + units[i] - 1) / units[i]) * rows * per_row[i] * (e->wide ? wide : narrow);
-        if (best == nullptr || time < least) {
-            best = e;
-            least = time;
-            *index = at;
-        }
-    }
-    return best;
+    return quant_entry(c.D, format, quant_unit_rows((int64_t)c.B * c.H_kv, c.D, format == LAGKV_QUANT_INT8, query_rows, S_cap, capped), index);
 }
 
 // Workspace: [status block | partials | who shares which unit]

@@ -98,3 +98,59 @@ def test_nothing_finite_but_zeros(binding, form, dtype):
     out = torch.full((1, 1, 64, D), 3.0, dtype=dtype, device=DEV)
     plan.quant_read(cache, i32([45]), ws, from_len=i32([16]), K_out=out)
     assert not out[0, 0, 16:45].any()
+
+
+def room_of(heads):
+    """Capacity from which int8 calls of more than 128 query rows to a KV head take units of 256."""
+    return (1600000 // heads // 256 + 1) * 256
+
+
+INT8 = [A.KINDS[0], A.KINDS[2]]
+
+
+@pytest.mark.parametrize("kind", INT8, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D,T,G", [(64, 64, 8), (96, 48, 4), (128, 64, 8), (64, 35, 5), (128, 64, 3)])
+def test_units_of_256_query_rows(binding, kind, D, T, G):
+    """int8 caches with much room under many query rows, full units and others."""
+    A.test_every_type_and_head_dim(binding, kind, D, T, G, 1, 64, room_of(3))
+
+
+@pytest.mark.parametrize("kind", INT8, ids=["bf16", "fp16"])
+def test_units_of_256_query_rows_over_every_length(binding, kind):
+    A.test_lengths_around_every_tile(binding, kind, 60, room_of(28))
+    A.test_padded_batch_and_rows_that_see_nothing(binding, kind, 64, room_of(10))
+
+
+@pytest.mark.parametrize("kind", INT8, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("way", ["up", "down", "mixed", "zeros"])
+def test_units_of_256_query_rows_under_scales_far_apart(binding, kind, way):
+    A.test_scales_far_apart(binding, kind, 64, 4, room_of(4), way)
+
+
+@pytest.mark.parametrize("kind", A.KINDS, ids=A.KIND_IDS)
+@pytest.mark.parametrize("cap", [0.5, 30.0, 1e5])
+def test_caps_under_many_query_rows(binding, kind, cap):
+    """In units of 128 and, int8, of 256."""
+    A.test_capped_logits(binding, kind, 64, 4, ROOM, cap)
+    if kind[0] == "int8":
+        A.test_capped_logits(binding, kind, 33, 4, room_of(4), cap)
+
+
+@pytest.mark.parametrize("kind", A.KINDS[:2], ids=A.KIND_IDS[:2])
+def test_factors_and_ends_of_the_type_under_many_query_rows(binding, kind):
+    """In units of 128 and, int8, of 256."""
+    A.test_factors_and_large_logits(binding, kind, 32, 4, 2 * ROOM)
+    A.test_queries_at_the_ends_of_their_type(binding, kind, 32, 2 * ROOM)
+    if kind[0] == "int8":
+        A.test_factors_and_large_logits(binding, kind, 40, 4, room_of(2))
+        A.test_queries_at_the_ends_of_their_type(binding, kind, 60, room_of(2))
+
+
+@pytest.mark.parametrize("page,R", [(16, 16), (64, 64), (256, 128)])
+def test_units_of_256_query_rows_on_pages(binding, page, R):
+    A.test_pages(binding, "int8", 40, 4, room_of(6), page, R)
+
+
+@pytest.mark.parametrize("kind", A.KINDS[:1], ids=A.KIND_IDS[:1])
+def test_units_of_256_query_rows_replayed(binding, kind):
+    A.test_graph_replay_and_repeats(binding, kind, 64, 4, room_of(6))
