@@ -210,27 +210,8 @@ long long quant_units(const lagkv_config& c, const AttendEntry& e, int query_row
     return (long long)c.B * c.H_kv * ((query_rows + e.rows - 1) / e.rows);
 }
 
-// CTAs of a unit's cluster, where a call takes that form (1: it does not): one launch instead of two, and every unit gets
-// the same CTAs whatever its length.  In us, int8, 128 channels, 4 query rows to a KV head, without and in clusters of 4, 8, 16:
-//     1 x 8 heads x 256 rows   8.9   6.4   6.8   7.8      4 x 8 x 256    9.4   6.8   7.4  20.7
-//     1 x 8 x 1216             9.5   8.6   7.6   7.9      4 x 8 x 4096  14.5  14.0  12.4  26.3
-//     1 x 8 x 4096            12.0  13.5   9.9   9.9      8 x 8 x 256    9.9   7.4  13.5  33.6
-//     1 x 8 x 20000           17.6  41.5  24.2  20.6      8 x 8 x 1216  13.0  10.4  16.3  34.5
-// So: as long as all clusters are on the GPU at once, and up to 640 rows a CTA, above which equal shares of all rows win.
-int cluster_size(const AttendEntry& e, long long units, int64_t S_cap) {
-    if (e.cluster == nullptr) return 1;
-    int best = 1;
-    double least = 0.0;
-    const int sizes[3] = {4, 8, 16}, most[3] = {256, 256, 128};
-    const double base[3] = {6.0, 6.4, 6.9};
-    for (int i = 0; i < 3; ++i) {
-        const double rows = double(S_cap) / sizes[i], time = base[i] + rows * 7e-3;
-        if (units * sizes[i] > most[i] || rows > 640.0 || (best > 1 && time >= least)) continue;
-        best = sizes[i];
-        least = time;
-    }
-    return best;
-}
+// CTAs of a unit's cluster, where a call takes that form (1: it does not).
+int cluster_size(const AttendEntry& e, long long units, int64_t S_cap) { return e.cluster == nullptr ? 1 : quant_cluster_ctas(units, S_cap); }
 
 int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const lagkv_quant_cache* cache, const void* Q, int64_t S_cap,
                  const lagkv_paged_layout* layout, int64_t num_pages, const int32_t* seq_len, const int32_t* draft_len,

@@ -16,11 +16,13 @@ def rules(tmp_path_factory):
 extern "C" int unit(long long heads, int D, int int8, int rows, long long S, int capped) {
     return lagkv::quant_unit_rows(heads, D, int8 != 0, rows, S, capped != 0);
 }
+extern "C" int cluster(long long units, long long S) { return lagkv::quant_cluster_ctas(units, S); }
 """)
     subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{ROOT}/paper_2504_04704_b200/csrc", "-o", str(at / "rules.so"),
                     str(at / "rules.cpp")], check=True)
     lib = ctypes.CDLL(str(at / "rules.so"))
     lib.unit.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_int]
+    lib.cluster.argtypes = [ctypes.c_longlong, ctypes.c_longlong]
     return lib
 
 
@@ -88,3 +90,30 @@ def test_the_calls_of_the_gpu_tests_reach_every_unit(rules):
         for heads in (2, 4, 6, 10, 28):
             for capped in (0, 1):
                 assert rules.unit(heads, D, 1, 160, -(-wide // heads), capped) == 256
+
+
+# (KV heads of all sequences, rows), one token of 4 query heads to a KV head: time without and in clusters of 4, 8, 16
+CLUSTERS = [
+    ((8, 256), (7.89, 6.16, 6.24, 7.54)),
+    ((8, 640), (8.63, 7.03, 6.26, 7.61)),
+    ((8, 1216), (9.07, 8.06, 7.35, 7.87)),
+    ((8, 2048), (9.41, 9.33, 7.55, 8.10)),
+    ((8, 4096), (11.07, 12.95, 9.59, 9.40)),
+    ((8, 8192), (12.93, 20.10, 13.42, 11.98)),
+    ((8, 20000), (17.30, 41.26, 23.92, 19.85)),
+    ((1, 1216), (8.50, 8.03, 7.25, 6.76)),
+    ((4, 4096), (9.97, 12.93, 9.32, 8.26)),
+    ((32, 256), (8.54, 6.51, 7.02, 20.35)),
+    ((32, 2048), (11.89, 9.71, 8.80, 22.14)),
+    ((32, 4096), (13.98, 13.48, 11.66, 25.74)),
+    ((64, 256), (9.11, 7.06, 12.93, None)),
+    ((64, 1216), (12.54, 9.87, 15.73, None)),
+    ((64, 2560), (15.05, 12.89, 18.92, None)),
+]
+
+
+@pytest.mark.parametrize("call,times", CLUSTERS, ids=[" ".join(map(str, c)) for c, _ in CLUSTERS])
+def test_clusters(rules, call, times):
+    """The form of each call is the quickest measured, or within 3 % of it."""
+    took = times[(1, 4, 8, 16).index(rules.cluster(*call))]
+    assert took is not None and took <= 1.03 * min(t for t in times if t)
