@@ -34,6 +34,7 @@ struct lagkv_plan_s {
     bool app_tuned;   // lagkv_plan_tune() fixed the uniform append shape: no pair kernel
     std::atomic<unsigned long long> attend_ready{0};  // attention kernels whose shared memory limit is raised
     std::atomic<unsigned long long> quant_ready{0}, write_ready{0};  // the same for caches in 8 bits with scales
+    std::atomic<int> quant_clusters[64][3] = {};  // 1 + clusters of each size that fit the GPU at once; 0: not asked yet
     // lagkv_compress_prefill_host(): three streams and the events between them, made on first use
     std::mutex host_mu;
     bool host_ready = false;

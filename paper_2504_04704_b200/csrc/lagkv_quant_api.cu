@@ -210,8 +210,43 @@ long long quant_units(const lagkv_config& c, const AttendEntry& e, int query_row
     return (long long)c.B * c.H_kv * ((query_rows + e.rows - 1) / e.rows);
 }
 
-// CTAs of a unit's cluster, where a call takes that form (1: it does not).
-int cluster_size(const AttendEntry& e, long long units, int64_t S_cap) { return e.cluster == nullptr ? 1 : quant_cluster_ctas(units, S_cap); }
+struct ClusterLaunch {
+    cudaLaunchConfig_t config;
+    cudaLaunchAttribute attr;
+    ClusterLaunch(const AttendEntry& e, int ctas, long long units, cudaStream_t stream) {
+        std::memset(&config, 0, sizeof config);
+        config.gridDim = dim3(unsigned(units * ctas));
+        config.blockDim = dim3(e.threads);
+        config.dynamicSmemBytes = e.smem;
+        config.stream = stream;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = unsigned(ctas);
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        config.attrs = &attr;
+        config.numAttrs = 1;
+    }
+};
+// CTAs of a unit's cluster, where a call takes that form (1: it does not).  What fits the GPU is asked once; a size that the
+// device refuses is no error.
+int cluster_size(lagkv_plan_t plan, const AttendEntry& e, int index, long long units, int64_t S_cap) {
+    int fits[kClusterSizes] = {1 << 30, 1 << 30, 1 << 30};
+    if (e.cluster == nullptr || quant_cluster_ctas(units, S_cap, fits) == 1) return 1;
+    for (int i = 0; i < kClusterSizes; ++i) {
+        std::atomic<int>& known = plan->quant_clusters[index][i];
+        int n = known.load(std::memory_order_acquire) - 1;
+        if (n < 0) {
+            const ClusterLaunch launch(e, kClusterCtas[i], 1, nullptr);
+            if (!raise_smem_limit(e.cluster, e.smem) || cudaFuncSetAttribute(e.cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, e.cluster, &launch.config) != cudaSuccess || n < 0) {
+                n = 0;
+                cudaGetLastError();
+            }
+            known.store(n + 1, std::memory_order_release);
+        }
+        fits[i] = n;
+    }
+    return quant_cluster_ctas(units, S_cap, fits);
+}
 
 int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const lagkv_quant_cache* cache, const void* Q, int64_t S_cap,
                  const lagkv_paged_layout* layout, int64_t num_pages, const int32_t* seq_len, const int32_t* draft_len,
@@ -256,30 +291,17 @@ int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const 
     if (P.least > 4) P.least = 4;
     P.lead = e->wide ? kWideLead : kAttendLead;
     DeviceGuard guard(plan->cfg.device);
-    const int ctas = cluster_size(*e, units, P.S_cap);
-    if (ctas > 1) index += 18;  // behind the forms without clusters, of which no table has more
-    const void* fn = ctas > 1 ? e->cluster : e->fn;
-    if (!(plan->quant_ready.load(std::memory_order_acquire) >> index & 1)) {
-        if (!raise_smem_limit(fn, e->smem)) return LAGKV_ECUDA;
-        if (ctas > 1 && cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LAGKV_ECUDA;
-        plan->quant_ready.fetch_or(1ull << index, std::memory_order_release);
-    }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const int ctas = cluster_size(plan, *e, index, units, P.S_cap);
     if (ctas > 1) {
-        cudaLaunchConfig_t launch;
-        std::memset(&launch, 0, sizeof launch);
-        launch.gridDim = dim3(unsigned(units * ctas));
-        launch.blockDim = dim3(e->threads);
-        launch.dynamicSmemBytes = e->smem;
-        launch.stream = stream;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = unsigned(ctas);
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        launch.attrs = &attr;
-        launch.numAttrs = 1;
+        const ClusterLaunch launch(*e, ctas, units, stream);
         void* cluster_args[] = {&P};
-        return cudaLaunchKernelExC(&launch, fn, cluster_args) == cudaSuccess ? check_launch() : LAGKV_ECUDA;
+        if (cudaLaunchKernelExC(&launch.config, e->cluster, cluster_args) == cudaSuccess) return check_launch();
+        cudaGetLastError();  // refused after all: the form without clusters serves the call
+    }
+    if (!(plan->quant_ready.load(std::memory_order_acquire) >> index & 1)) {
+        if (!raise_smem_limit(e->fn, e->smem)) return LAGKV_ECUDA;
+        plan->quant_ready.fetch_or(1ull << index, std::memory_order_release);
     }
     CUtensorMap map_k, map_v;
     if (e->wide) {
@@ -290,7 +312,7 @@ int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const 
         if (rc != LAGKV_OK) return rc;
     }
     void* args[] = {&P, &map_k, &map_v};
-    if (cudaLaunchKernel(fn, dim3((unsigned)P.ctas), dim3(e->threads), args, e->smem, stream) != cudaSuccess) return LAGKV_ECUDA;
+    if (cudaLaunchKernel(e->fn, dim3((unsigned)P.ctas), dim3(e->threads), args, e->smem, stream) != cudaSuccess) return LAGKV_ECUDA;
     rc = launch_join(*e, &P, query_rows, units, stream);
     return rc == LAGKV_OK ? check_launch() : rc;
 }

@@ -154,3 +154,19 @@ def test_units_of_256_query_rows_on_pages(binding, page, R):
 @pytest.mark.parametrize("kind", A.KINDS[:1], ids=A.KIND_IDS[:1])
 def test_units_of_256_query_rows_replayed(binding, kind):
     A.test_graph_replay_and_repeats(binding, kind, 64, 4, room_of(6))
+
+
+@pytest.mark.parametrize("H,S", [(2, 300), (8, 4096), (2, 20000)])
+def test_the_first_call_of_a_plan_may_be_captured(binding, H, S):
+    """What a plan asks the runtime once, it may ask while a stream is captured: clusters of CTAs, and the form without."""
+    c = A.case(binding, ("int8", BF16), 1, H, 4, 128, S, 1, 64, seed=6, lens=[S])
+    out, side, graph = torch.empty_like(c["Q"]), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            c["plan"].attend_quant(c["Q"], c["cache"], c["seq"], c["ws"], out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        QU.assert_attention({"out": out}, A.reference(c))

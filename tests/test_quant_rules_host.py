@@ -16,13 +16,16 @@ def rules(tmp_path_factory):
 extern "C" int unit(long long heads, int D, int int8, int rows, long long S, int capped) {
     return lagkv::quant_unit_rows(heads, D, int8 != 0, rows, S, capped != 0);
 }
-extern "C" int cluster(long long units, long long S) { return lagkv::quant_cluster_ctas(units, S); }
+extern "C" int cluster(long long units, long long S, int a, int b, int c) {
+    const int fits[3] = {a, b, c};
+    return lagkv::quant_cluster_ctas(units, S, fits);
+}
 """)
     subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{ROOT}/paper_2504_04704_b200/csrc", "-o", str(at / "rules.so"),
                     str(at / "rules.cpp")], check=True)
     lib = ctypes.CDLL(str(at / "rules.so"))
     lib.unit.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_int]
-    lib.cluster.argtypes = [ctypes.c_longlong, ctypes.c_longlong]
+    lib.cluster.argtypes = [ctypes.c_longlong] * 2 + [ctypes.c_int] * 3
     return lib
 
 
@@ -115,5 +118,15 @@ CLUSTERS = [
 @pytest.mark.parametrize("call,times", CLUSTERS, ids=[" ".join(map(str, c)) for c, _ in CLUSTERS])
 def test_clusters(rules, call, times):
     """The form of each call is the quickest measured, or within 3 % of it."""
-    took = times[(1, 4, 8, 16).index(rules.cluster(*call))]
+    took = times[(1, 4, 8, 16).index(rules.cluster(*call, 64, 32, 8))]
     assert took is not None and took <= 1.03 * min(t for t in times if t)
+
+
+def test_clusters_that_do_not_fit_are_not_taken(rules):
+    """A device or context that runs fewer clusters of a size at once gets another size, or the form without."""
+    assert rules.cluster(8, 4096, 64, 32, 8) == 16
+    assert rules.cluster(8, 4096, 64, 32, 7) == 8
+    assert rules.cluster(8, 4096, 64, 32, 0) == 8
+    assert rules.cluster(8, 4096, 64, 7, 7) == 1                   # 4 CTAs would have too many rows each
+    assert rules.cluster(8, 1216, 64, 0, 0) == 4
+    assert rules.cluster(8, 1216, 7, 7, 7) == 1 and rules.cluster(1, 1, 0, 0, 0) == 1
