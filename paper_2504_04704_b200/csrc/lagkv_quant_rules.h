@@ -59,17 +59,18 @@ inline int quant_unit_rows(int64_t kv_heads, int D, bool int8, int query_rows, i
 //     1 x 8 x 20000           17.3  41.3  23.9  19.9      8 x 8 x 256    9.1   7.1  12.9
 //     1 x 4 x 1216             8.7   8.1   7.3   6.8      8 x 8 x 1216  12.5   9.9  15.7
 // So: as long as all clusters are on the GPU at once (`fits`: of each size, as the runtime says for the kernel and the device; 0: none), and up to
-// 640 rows a CTA, above which equal shares of all rows win.  More clusters of 16 begin later.  Over one to 64 heads, 64 to 10240 rows and 64 to 256 channels the size taken is 0.4 % behind the best one on average.
+// 640 rows a CTA, above which equal shares of all rows win.  More than four clusters of 16 begin later.  Over one to 64 heads, 64 to 10240 rows and 64 to 256 channels the size taken is 0.1 % behind the best
+// one on average.
 constexpr int kClusterSizes = 3, kClusterCtas[kClusterSizes] = {4, 8, 16};
 inline int quant_cluster_ctas(int64_t units, int64_t S_cap, const int (&fits)[kClusterSizes]) {
     const int most[kClusterSizes] = {256, 256, 128};  // CTAs in all that were measured as worth it on 148 SMs
-    const double base[kClusterSizes] = {6.0, 6.3, 6.5}, each[kClusterSizes] = {0.0, 0.0, 0.008};
+    const double base[kClusterSizes] = {6.0, 6.3, 6.6}, each[kClusterSizes] = {0.0, 0.0, 0.0133};  // us; and for each CTA from the 65th on
     int best = 1;
     double least = 0.0;
     for (int i = 0; i < kClusterSizes; ++i) {
         const double rows = double(S_cap) / kClusterCtas[i];
         if (units > fits[i] || units * kClusterCtas[i] > most[i] || rows > 640.0) continue;
-        const double time = base[i] + each[i] * double(units * kClusterCtas[i]) + rows * 7e-3;
+        const double more = double(units * kClusterCtas[i] - 64), time = base[i] + (more > 0.0 ? each[i] * more : 0.0) + rows * 7e-3;
         if (best > 1 && time >= least) continue;
         best = kClusterCtas[i];
         least = time;

@@ -105,7 +105,10 @@ CLUSTERS = [
     ((8, 8192), (12.93, 20.10, 13.42, 11.98)),
     ((8, 20000), (17.30, 41.26, 23.92, 19.85)),
     ((1, 1216), (8.50, 8.03, 7.25, 6.76)),
+    ((4, 640), (8.30, 6.77, 6.27, 7.02)),
+    ((4, 1216), (8.69, 8.05, 7.29, 6.76)),
     ((4, 4096), (9.97, 12.93, 9.32, 8.26)),
+    ((8, 2560), (10.09, 10.15, 8.32, 9.08)),
     ((32, 256), (8.54, 6.51, 7.02, 20.35)),
     ((32, 2048), (11.89, 9.71, 8.80, 22.14)),
     ((32, 4096), (13.98, 13.48, 11.66, 25.74)),
