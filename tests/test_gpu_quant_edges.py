@@ -17,6 +17,11 @@ def binding():
     return b
 
 
+def room_of(heads):
+    """Capacity from which int8 calls of more than 128 query rows to a KV head take units of 256."""
+    return (1600000 // heads // 256 + 1) * 256
+
+
 @pytest.mark.parametrize("bad", [-1, -2, -3, -2 ** 31, 40, 2 ** 31 - 1])
 def test_every_entry_outside_the_source_is_recorded(binding, bad):
     """Whatever number it is: recorded, and its row is 0."""
@@ -100,9 +105,87 @@ def test_nothing_finite_but_zeros(binding, form, dtype):
     assert not out[0, 0, 16:45].any()
 
 
-def room_of(heads):
-    """Capacity from which int8 calls of more than 128 query rows to a KV head take units of 256."""
-    return (1600000 // heads // 256 + 1) * 256
+@pytest.mark.parametrize("kind", A.KINDS, ids=A.KIND_IDS)
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("T,G,room", [(3, 2, 0), (2, 4, ROOM), (4, 4, ROOM), (7, 4, ROOM), (20, 4, ROOM), (64, 4, room_of(6))])
+def test_strides_in_every_kernel(binding, kind, D, T, G, room):
+    """Codes and queries as projections leave them, tokens first, rows padded: clusters, units of 8, 16, 32, 128 and 256."""
+    B, H, S, R = 2, 3, 210, 32
+    c = A.case(binding, kind, B, H, G, D, S, T, R, seed=1, lens=[210, 100], room=room)
+    A.poison(c)
+    want = A.reference(c)
+    cache = c["cache"]
+    K, V = (torch.full((B, x.shape[2], H, D + 16), 0x7f, dtype=torch.uint8, device=DEV).view(x.dtype)[..., :D].transpose(1, 2) for x in (cache.K, cache.V))
+    for to, x in ((K, cache.K), (V, cache.V)):
+        to.view(torch.uint8).copy_(x.view(torch.uint8))
+    c["cache"] = binding.QuantCache(K, V, cache.K_scale, cache.V_scale, block_rows=R)
+    Q = torch.full((B, T, H * G, D + 8), float("nan"), dtype=c["Q"].dtype, device=DEV)[..., :D].copy_(c["Q"])
+    heads_first = torch.full((B, H * G, T, D + 24), float("nan"), dtype=c["Q"].dtype, device=DEV)[..., :D].transpose(1, 2).copy_(c["Q"])
+    for q in (Q, heads_first):
+        c["Q"] = q
+        QU.assert_attention(A.run(c), want)
+
+
+@pytest.mark.parametrize("form,dtype", [("int8", BF16), ("e4m3", FP16)], ids=["int8-bf16", "e4m3-fp16"])
+@pytest.mark.parametrize("D", [64, 96, 256])
+@pytest.mark.parametrize("T,G,room", [(1, 7, 0), (2, 4, ROOM), (4, 4, ROOM), (8, 4, 2 * ROOM), (20, 4, 2 * ROOM), (64, 4, room_of(4))])
+@pytest.mark.parametrize("page,R", [(16, 16), (64, 32), (128, 128)])
+def test_attention_on_pages_of_every_head_dim(binding, form, dtype, D, T, G, room, page, R):
+    """The same bits as from the contiguous cache, which is held against the statement; an entry outside the pool is recorded."""
+    B, H, S = 2, 2, 384
+    room = room // page * page
+    c = A.case(binding, (form, dtype), B, H, G, D, S, T, R, seed=page + T, lens=[S, 200 + T], room=room)
+    nb = S // page
+    pages = B * nb + 2
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(1))[:B * nb].view(B, nb).to(torch.int32).to(DEV)
+    cache = c["cache"]
+    pool = binding.QuantCache(*(QU.pool_of(x[:, :, :S].contiguous(), page, table, pages) for x in (cache.K, cache.V)), cache.K_scale, cache.V_scale, block_rows=R)
+    if room:  # entries of blocks that no sequence reaches
+        table = torch.cat([table, torch.full((B, room // page - nb), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+    call = lambda tab: c["plan"].attend_quant_paged(c["Q"], pool, tab, c["seq"], c["ws"], draft_len=c["draft"], tree_mask=c["mask"], want_lse=True)  # noqa: E731
+    got, flat = call(table), A.run(c)
+    QU.assert_attention(flat, A.reference(c))
+    assert torch.equal(flat["out"], got["out"]) and torch.equal(flat["lse"], got["lse"])
+    bad = table.clone()
+    bad[0, 1] = pages
+    lost = call(bad)
+    assert c["plan"].read_status(c["ws"])[0] == binding.LAGKV_EINVAL
+    assert torch.equal(lost["out"][1], got["out"][1])
+    K, V = (QU.row_values(x[:1, :, :S], s[:1, :, :S // R], R) for x, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)))
+    want = QU.attention_reference(c["Q"][:1], K, V, [S], [c["drafts"][0]], None if c["mask"] is None else c["mask"][:1], form=form,
+                                  V_scale=cache.V_scale[:1].nan_to_num(nan=0.0), gone=slice(page, 2 * page))
+    QU.assert_attention({"out": lost["out"][:1], "lse": lost["lse"][:1]}, want)
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("D", [64, 96, 256])
+@pytest.mark.parametrize("page,R", [(16, 16), (64, 32), (128, 128)])
+def test_writing_and_reading_pages_of_every_head_dim(binding, form, D, page, R):
+    """Ragged spans through a random table, read back whole and row by row."""
+    B, H, nb = 3, 2, 256 // page
+    S = nb * page
+    g, K, V, ks, vs = W.start_state(B, H, S, D, form, R, seed=page)
+    x = (torch.randn((2, B, H, 120, D), generator=g, device=DEV) * 2).to(FP16)
+    pages = B * nb + 3
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(1))[:B * nb].view(B, nb).to(torch.int32).to(DEV)
+    plan = binding.Plan(B, H, D, sink=4, lag=64, dtype=FP16)
+    cache = binding.QuantCache(QU.pool_of(K, page, table, pages), QU.pool_of(V, page, table, pages), ks, vs, block_rows=R)
+    ws = plan.new_workspace()
+    starts, ends = [0, 37, 200], [120, 130, S]
+    want = W.expected(K, V, ks, vs, x[0], x[1], starts, ends, R, form)
+    plan.quant_write_paged(cache, table, x[0], x[1], i32(ends), ws, from_len=i32(starts))
+    W.same(cache, want, table, page)
+    values = [(c.float() * s.float().repeat_interleave(R, -1)[..., :S, None]).to(FP16) for c, s in want]
+    out = torch.full((2, B, H, S, D), 3.0, dtype=FP16, device=DEV)
+    plan.quant_read_paged(cache, table, i32(ends), ws, from_len=i32(starts), K_out=out[0], V_out=out[1])
+    idx = torch.stack([torch.randint(0, e, (H, 33), generator=torch.Generator().manual_seed(e)) for e in ends]).to(torch.int32)
+    picks = plan.quant_read_paged(cache, table, i32(ends), ws, idx=idx.to(DEV))
+    for t, p, value in zip(out, picks, values):
+        for b in range(B):
+            assert torch.equal(t[b, :, starts[b]:ends[b]].cpu(), value[b, :, starts[b]:ends[b]])
+            assert (t[b, :, :starts[b]] == 3).all() and (t[b, :, ends[b]:] == 3).all()
+        assert torch.equal(p.cpu(), value.gather(2, idx.long()[..., None].expand(B, H, 33, D)))
+    assert plan.read_status(ws)[0] == 0
 
 
 INT8 = [A.KINDS[0], A.KINDS[2]]
