@@ -267,11 +267,12 @@ def _dense_strides(t, name: str):
 
 class QuantCache:
     """A cache in 8 bits with block scales (``lagkv_quant_cache``): codes ``K``, ``V`` as ``torch.int8`` or
-    ``torch.float8_e4m3fn``, ``[B, H, S_cap, D]`` or pools ``[num_pages, H, page_size, D]``, and their scales
-    ``K_scale``, ``V_scale``, fp32 ``[B, H, blocks]``, one for each ``block_rows`` rows of a sequence (of the
-    sequence on paged caches too: a fork copies its scales along with its table row).  The tensors are taken for good: what is
-    in them may change, but attributes cannot be assigned, and a tensor whose memory was exchanged (``set_``, ``resize_``,
-    ``.data``) is refused by every call.  Other tensors need another ``QuantCache``."""
+    ``torch.float8_e4m3fn``, ``[B, H, S_cap, D]`` or pools ``[num_pages, H, page_size, D]``, of any strides that are multiples
+    of 16, the same for both (K and V of a page may lie side by side), and their scales ``K_scale``, ``V_scale``, fp32
+    ``[B, H, blocks]``, one for each ``block_rows`` rows of a sequence (of the sequence on paged caches too: a fork copies its
+    scales along with its table row).  The tensors are taken for good: what is in them may change, but attributes cannot be
+    assigned, and a tensor whose memory was exchanged (``set_``, ``resize_``, ``.data``) is refused by every call.  Other
+    tensors need another ``QuantCache``."""
 
     def __init__(self, K, V, K_scale, V_scale, block_rows=64):
         if K.dtype not in _QUANT_FORMATS or V.dtype != K.dtype or K.shape != V.shape or K.dim() != 4 or K.device != V.device:
@@ -284,10 +285,13 @@ class QuantCache:
             raise TypeError("K and V must have the same strides")
         addresses = (K.data_ptr(), V.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr())
         arg = lagkv_quant_cache(*addresses, _QUANT_FORMATS[K.dtype], block_rows, K_scale.shape[2], *strides)
-        # the tensors, and what the calls of a decode step pass and compare
+        paged = lagkv_quant_cache(*addresses, _QUANT_FORMATS[K.dtype], block_rows, K_scale.shape[2], 0, 0, 0) if any(strides) else arg
+        ref = ctypes.byref(arg)
+        # the tensors, and what the calls of a decode step pass and compare; on pages the layout carries the strides
         self.__dict__.update(
             K=K, V=V, K_scale=K_scale, V_scale=V_scale, block_rows=block_rows, strides=strides, device=K.get_device(),
-            shape=tuple(K.shape), scale_shape=tuple(K_scale.shape), rows=K.shape[2], arg=arg, ref=ctypes.byref(arg),
+            shape=tuple(K.shape), scale_shape=tuple(K_scale.shape), rows=K.shape[2], arg=arg, ref=ref,
+            paged=paged, paged_ref=ref if paged is arg else ctypes.byref(paged),
             addresses=addresses, address_of=(K.data_ptr, V.data_ptr, K_scale.data_ptr, V_scale.data_ptr))
 
     def __setattr__(self, name, value):
@@ -775,12 +779,16 @@ class Plan:
             raise TypeError(f"the cache must be on device {self.device}")
         if heads != H or channels != D or cache.scale_shape[:2] != (B, H) or not paged and n != B:
             raise TypeError(f"the cache must be [{B}, {H}, S_cap, {D}], or pages [num_pages, {H}, page_size, {D}], with scales [{B}, {H}, blocks]")
-        if paged and any(cache.strides):
-            raise TypeError("paged codes must be contiguous")
         a, b, c, d = cache.address_of
         if (a(), b(), c(), d()) != cache.addresses:
             raise TypeError("a tensor of the cache has other memory than when the QuantCache was made: make another one")
-        return cache.ref
+        return cache.paged_ref if paged else cache.ref
+
+    def _quant_pool(self, cache, block_table):
+        """Layout and page count of the cache's pools; pools that are not contiguous carry their strides in the layout."""
+        if not any(cache.strides):
+            return self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        return self._paged_pool(cache.K, cache.V, block_table, cache.strides + (cache.rows,), cache.shape[0], cache.K.dtype)
 
     def _quant_source(self, K, V, from_len, seq_len, take, at_positions):
         (B, H, D), shape, dtype, dev = self._dims, K.shape, self.dtype, self.device
@@ -817,7 +825,7 @@ class Plan:
     def quant_write_paged(self, cache, block_table, K, V, seq_len, workspace, from_len=None, take=None, at_positions=False) -> None:
         """``lagkv_quant_write_paged``: the same into pools of pages."""
         q = self._check_quant(cache, True)
-        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        lay, pages = self._quant_pool(cache, block_table)
         src = self._quant_source(K, V, from_len, seq_len, take, at_positions)
         rc = self.lib.lagkv_quant_write_paged(
             self.handle, q, ctypes.byref(lay), pages, ctypes.byref(src), _addr(K), _addr(V), _addr(from_len), _addr(seq_len),
@@ -864,7 +872,7 @@ class Plan:
     def quant_read_paged(self, cache, block_table, seq_len, workspace, from_len=None, idx=None, K_out=None, V_out=None):
         """``lagkv_quant_read_paged``: the same from pools of pages."""
         q = self._check_quant(cache, True)
-        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        lay, pages = self._quant_pool(cache, block_table)
         K_out, V_out, rows = self._quant_out(seq_len, from_len, idx, K_out, V_out)
         rc = self.lib.lagkv_quant_read_paged(
             self.handle, q, ctypes.byref(lay), pages, _addr(from_len), _addr(seq_len), _addr(idx), int(rows), _addr(K_out), _addr(V_out),
@@ -903,7 +911,7 @@ class Plan:
         """``lagkv_attend_quant_paged``: the same over pools of pages."""
         q = self._query(Q, scale, k_scale, v_scale)
         qc = self._check_quant(cache, True)
-        lay, pages = self._paged_pool(cache.K, cache.V, block_table, None, None, cache.K.dtype)
+        lay, pages = self._quant_pool(cache, block_table)
         B = self.cfg.B
         self._check_ints(seq_len, "seq_len", (B,))
         self._check_ints(draft_len, "draft_len", (B,))

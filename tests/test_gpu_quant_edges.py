@@ -253,3 +253,50 @@ def test_the_first_call_of_a_plan_may_be_captured(binding, H, S):
         out.zero_()
         graph.replay()
         QU.assert_attention({"out": out}, A.reference(c))
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("D,page,R", [(64, 16, 16), (128, 64, 32), (96, 128, 128)])
+@pytest.mark.parametrize("tokens_first", [False, True])
+def test_pools_with_strides(binding, form, D, page, R, tokens_first):
+    """K and V of a page side by side, heads or tokens first, rows padded: written, read and attended to like contiguous pools."""
+    B, H, G, S = 2, 3, 4, 256
+    g, K, V, ks, vs = W.start_state(B, H, S, D, form, R, seed=page)
+    nb = S // page
+    pages = B * nb + 3
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(1))[:B * nb].view(B, nb).to(torch.int32).to(DEV)
+    plan = binding.Plan(B, H, D, sink=4, lag=64)
+    ws = plan.new_workspace()
+    dense = binding.QuantCache(QU.pool_of(K, page, table, pages), QU.pool_of(V, page, table, pages), ks, vs, block_rows=R)
+    if tokens_first:
+        store = torch.full((pages, page, 2, H, D + 16), 0x55, dtype=torch.uint8, device=DEV)
+        both = [store[:, :, i, :, :D].transpose(1, 2) for i in range(2)]
+    else:
+        store = torch.full((pages, 2, H, page, D + 16), 0x55, dtype=torch.uint8, device=DEV)
+        both = [store[:, i, :, :, :D] for i in range(2)]
+    for to, x in zip(both, (dense.K, dense.V)):
+        to.copy_(x.view(torch.uint8))
+    cache = binding.QuantCache(*(t.view(dense.K.dtype) for t in both), ks.clone(), vs.clone(), block_rows=R)
+    x = (torch.randn((2, B, H, 90, D), generator=g, device=DEV) * 2).to(BF16)
+    starts, ends = [0, 37], [90, 111]
+    for c in (dense, cache):
+        plan.quant_write_paged(c, table, x[0], x[1], i32(ends), ws, from_len=i32(starts))
+    assert torch.equal(cache.K_scale, dense.K_scale) and torch.equal(cache.V_scale, dense.V_scale)
+    for a, b in ((cache.K, dense.K), (cache.V, dense.V)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert (store[..., D:] == 0x55).all()
+    out = torch.zeros((4, B, H, S, D), dtype=BF16, device=DEV)
+    plan.quant_read_paged(dense, table, i32([S, S]), ws, K_out=out[0], V_out=out[1])
+    plan.quant_read_paged(cache, table, i32([S, S]), ws, K_out=out[2], V_out=out[3])
+    assert torch.equal(out[:2], out[2:]) and plan.read_status(ws)[0] == 0
+    for T, room in ((1, 0), (2, ROOM), (20, ROOM), (64, room_of(B * H))):
+        wide = torch.cat([table, torch.full((B, max(0, room // page - nb)), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+        blocks = -(-wide.shape[1] * page // R)
+        scales = lambda c: [torch.nn.functional.pad(s, (0, blocks - s.shape[2])) for s in (c.K_scale, c.V_scale)]  # noqa: E731
+        Q = torch.randn((B, T, H * G, D), generator=g, device=DEV).to(BF16)
+        aws = plan.new_attend_quant_workspace(T, H * G)
+        got = [plan.attend_quant_paged(Q, binding.QuantCache(c.K, c.V, *scales(c), block_rows=R), wide, i32([S, 200]), aws, want_lse=True) for c in (dense, cache)]
+        assert plan.read_status(aws)[0] == 0
+        assert torch.equal(got[0]["out"], got[1]["out"]) and torch.equal(got[0]["lse"], got[1]["lse"])
+        kv = [QU.row_values(QU.dense_of(c, table, page), s, R) for c, s in ((dense.K, dense.K_scale), (dense.V, dense.V_scale))]
+        QU.assert_attention(got[1], QU.attention_reference(Q, *kv, [S, 200], [T, T], None, form=form, V_scale=dense.V_scale))

@@ -111,3 +111,21 @@ def test_cache_object_keeps_its_tensors(binding):
         t.data = t.clone()
         with pytest.raises(TypeError):
             plan._check_quant(cache, False)
+
+
+def test_pools_with_strides_carry_them_in_the_layout(binding):
+    """What a paged call passes for pools that are not contiguous; strides that reach behind the memory are refused."""
+    plan = binding.Plan(2, 3, 64, 4, 64, device=-1)
+    store = torch.zeros((5, 2, 3, 16, 80), dtype=torch.int8)
+    K, V = store[:, 0, :, :, :64], store[:, 1, :, :, :64]
+    scales = torch.zeros((2, 2, 3, 4))
+    cache = binding.QuantCache(K, V, scales[0], scales[1], block_rows=16)
+    ref = plan._check_quant(cache, True)
+    arg = cache.paged
+    assert ref is cache.paged_ref and (arg.stride_b, arg.stride_h, arg.stride_s) == (0, 0, 0) and arg.K == K.data_ptr() and arg.V == V.data_ptr()
+    assert (cache.arg.stride_b, cache.arg.stride_h, cache.arg.stride_s) == K.stride()[:3]
+    table = torch.zeros((2, 4), dtype=torch.int32)
+    plan._paged = lambda pool, tab, strides: strides               # a table on the host goes no further
+    assert plan._quant_pool(cache, table) == (K.stride()[:3] + (16,), 5)
+    dense = torch.zeros((2, 5, 3, 16, 64), dtype=torch.int8)
+    assert plan._quant_pool(binding.QuantCache(dense[0], dense[1], scales[0], scales[1], block_rows=16), table) == (None, 5)
