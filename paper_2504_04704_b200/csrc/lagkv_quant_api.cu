@@ -226,26 +226,30 @@ struct ClusterLaunch {
         config.numAttrs = 1;
     }
 };
-// CTAs of a unit's cluster, where a call takes that form (1: it does not).  What fits the GPU is asked once; a size that the
-// device refuses is no error.
+// CTAs of a unit's cluster, where a call takes that form (1: it does not).  How many of the size that the rule wants fit the GPU is
+// asked once, which costs some microseconds; a size that the device refuses is no error.
 int cluster_size(lagkv_plan_t plan, const AttendEntry& e, int index, long long units, int64_t S_cap) {
-    int fits[kClusterSizes] = {1 << 30, 1 << 30, 1 << 30};
-    if (e.cluster == nullptr || quant_cluster_ctas(units, S_cap, fits) == 1) return 1;
+    if (e.cluster == nullptr) return 1;
+    int fits[kClusterSizes];
     for (int i = 0; i < kClusterSizes; ++i) {
-        std::atomic<int>& known = plan->quant_clusters[index][i];
-        int n = known.load(std::memory_order_acquire) - 1;
-        if (n < 0) {
-            const ClusterLaunch launch(e, kClusterCtas[i], 1, nullptr);
-            if (!raise_smem_limit(e.cluster, e.smem) || cudaFuncSetAttribute(e.cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-                cudaOccupancyMaxActiveClusters(&n, e.cluster, &launch.config) != cudaSuccess || n < 0) {
-                n = 0;
-                cudaGetLastError();
-            }
-            known.store(n + 1, std::memory_order_release);
+        const int known = plan->quant_clusters[index][i].load(std::memory_order_acquire);
+        fits[i] = known == 0 ? 1 << 30 : known - 1;
+    }
+    for (;;) {
+        const int ctas = quant_cluster_ctas(units, S_cap, fits);
+        int i = 0;
+        while (i < kClusterSizes && kClusterCtas[i] != ctas) ++i;
+        if (i == kClusterSizes || fits[i] < 1 << 30) return ctas;
+        const ClusterLaunch launch(e, ctas, 1, nullptr);
+        int n = 0;
+        if (!raise_smem_limit(e.cluster, e.smem) || cudaFuncSetAttribute(e.cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, e.cluster, &launch.config) != cudaSuccess || n < 0) {
+            n = 0;
+            cudaGetLastError();
         }
         fits[i] = n;
+        plan->quant_clusters[index][i].store(n + 1, std::memory_order_release);
     }
-    return quant_cluster_ctas(units, S_cap, fits);
 }
 
 int attend_quant(lagkv_plan_t plan, const lagkv_query* query, double cap, const lagkv_quant_cache* cache, const void* Q, int64_t S_cap,
