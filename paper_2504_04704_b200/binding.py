@@ -290,7 +290,7 @@ class QuantCache:
         # the tensors, and what the calls of a decode step pass and compare; on pages the layout carries the strides
         self.__dict__.update(
             K=K, V=V, K_scale=K_scale, V_scale=V_scale, block_rows=block_rows, strides=strides, device=K.get_device(),
-            shape=tuple(K.shape), scale_shape=tuple(K_scale.shape), rows=K.shape[2], arg=arg, ref=ref,
+            shape=tuple(K.shape), rows=K.shape[2], kind=(*K_scale.shape[:2], K.shape[1], K.shape[3]), arg=arg, ref=ref,
             paged=paged, paged_ref=ref if paged is arg else ctypes.byref(paged),
             addresses=addresses, address_of=(K.data_ptr, V.data_ptr, K_scale.data_ptr, V_scale.data_ptr))
 
@@ -319,6 +319,7 @@ class Plan:
         self.lib = lib
         self.device = int(device)
         self._dims = (int(B), int(H_kv), int(D))
+        self._quant_kind = (int(B), int(H_kv), int(H_kv), int(D))
         self.k = int(lib.lagkv_keep_count(self.handle))
 
     def close(self):
@@ -774,10 +775,10 @@ class Plan:
                           *(torch.zeros(scales, dtype=torch.float32, device=dev) for _ in "KV"), block_rows=block_rows)
 
     def _check_quant(self, cache, paged: bool):
-        (B, H, D), (n, heads, _, channels) = self._dims, cache.shape
         if cache.device != self.device:
             raise TypeError(f"the cache must be on device {self.device}")
-        if heads != H or channels != D or cache.scale_shape[:2] != (B, H) or not paged and n != B:
+        if cache.kind != self._quant_kind or not paged and cache.shape[0] != self._dims[0]:
+            B, H, D = self._dims
             raise TypeError(f"the cache must be [{B}, {H}, S_cap, {D}], or pages [num_pages, {H}, page_size, {D}], with scales [{B}, {H}, blocks]")
         a, b, c, d = cache.address_of
         if (a(), b(), c(), d()) != cache.addresses:
