@@ -5,7 +5,7 @@
 //     x_r = scale * log2(e) * s_K * (q . c_r)   (capped: cap * tanh(x / cap)),   p_r = 2^(x_r - ref),
 //     out = sum (p_r s_V) d_r / sum p_r.
 // K scales enter the fp32 logits.  V scales enter the probabilities before these are rounded to fp16 (half a
-// step, 2^-12, like the rounding of a probability anywhere here), relative to a power of two 2^ve that follows the largest scale seen,
+// step, 2^-11 of the value at most, like the rounding of a probability anywhere here), relative to a power of two 2^ve that follows the largest scale seen,
 // so that the rounded values lie where fp16 is finest whatever the scales.
 //
 // The products are transposed against lagkv_attend_kernel's: S^T[rows x queries] = C Q^T and O^T[channels x queries] =
@@ -17,8 +17,8 @@
 // that of operands by movmatrix.
 // Bound by HBM: a tile of 32 rows of 128 channels (8 KB) costs a warp some 300 instructions (e4m3) or 480 (int8).  One token,
 // 32 x 8 heads of up to 32768 int8 rows of 128 channels: 265 us, 95 % of the copy rate; 16 x 4 heads of up to 16384 rows in pages of 64:
-// 43.3 us where the bytes take 31.5, the rest is start, tail and joining.  Units of 16 and 32 query rows: bound by issue, 6 x 4
-// heads of up to 16411 rows of 64 channels under 35 capped query rows 50 us (bytes 6.1).
+// 44 us where the bytes take 31.5, the rest is start, tail and joining.  Units of 16 and 32 query rows: bound by issue, 6 x 4
+// heads of up to 16411 rows of 64 channels under 35 capped query rows, three units of 16, 46 to 51 us (bytes 6.1).
 //
 // Calls of few units (a user or two) take the form with a cluster of CTAs for each unit, which join what they have found through
 // distributed shared memory: one launch, no partials in memory (1 x 8 x 1216 int8 rows 7.4 us instead of 9.1).

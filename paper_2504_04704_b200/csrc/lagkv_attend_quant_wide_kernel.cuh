@@ -12,7 +12,7 @@
 // The roles' loops run side by side out of one instruction cache, and with 140 KB of code its misses set the pace.  So one
 // warp walks the share of the work and tells the others the units (WideTask), waits and loads of queries are out of line, and
 // what few items need (caps, hidden rows) is a rolled loop over tensor memory.
-// 94 KB of code instead of 140: 32 tokens of 4 heads over 16 x 8 x 9728 rows of 128 channels 112 us instead of 136 (bytes 38.6; an
+// 94 KB of code instead of 140: 32 tokens of 4 heads over 16 x 8 x 9728 rows of 128 channels 112 us instead of 119 (bytes 38.6; an
 // fp8 cache without scales 130), 64 tokens over 2 x 8 x 131072 int8 rows 295 us (products 150).  No unit is full:
 // tensor cores 27 %, DRAM 30 %, exponentials 28 % of their rates in the former; what is left are the chains of the softmax warps.
 #pragma once
